@@ -11,6 +11,7 @@
 
 #include <type_traits>
 
+#include "ppd_device.h"
 #include "ppd_internal.h"
 
 #ifndef PPD_PINGPONG
@@ -19,52 +20,9 @@
 
 namespace ppd {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-#define NEG_INF (-__builtin_inff())
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-    f32x2 f = {a, b};
-    bf16x2 r = __builtin_convertvector(f, bf16x2);  // round to nearest even
-    return __builtin_bit_cast(uint32_t, r);
-}
-
-__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
-
-__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 // Query row of a column of a row block (columns are row-major over the G query heads of the group): col / G
 // with inv = 65536 / G + 1, exact for col < 4096 and G <= 16.
 __device__ __forceinline__ int col_row(int col, int inv) { return (int)(((unsigned)col * (unsigned)inv) >> 16); }
-
-__device__ __forceinline__ float xor_shuffle(float v, int mask) { return __shfl_xor(v, mask, 64); }
-
-// max / sum of v over lanes l and l^32 (v_permlane32_swap: no LDS round trip).  The instruction exchanges
-// the upper half of its first register with the lower half of its second.  It is written as inline asm on
-// two copies of v (the builtin's second result was folded into the first by the compiler when both inputs
-// hold the same value); the s_nop cover the VALU-write -> permlane-read wait states on both sides.
-__device__ __forceinline__ void swap_halves(float v, float* lo, float* hi) {
-    float a = v, b = v;
-    asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 1" : "+v"(a), "+v"(b));
-    *lo = a;  // {v[0..31], v[0..31]}
-    *hi = b;  // {v[32..63], v[32..63]}
-}
-__device__ __forceinline__ float max_halves(float v) {
-    float lo, hi;
-    swap_halves(v, &lo, &hi);
-    return fmaxf(lo, hi);
-}
-__device__ __forceinline__ float sum_halves(float v) {
-    float lo, hi;
-    swap_halves(v, &lo, &hi);
-    return lo + hi;
-}
 
 // The running maximum is only raised (and the accumulators rescaled) when it would grow by more than this many
 // powers of two; until then probabilities may exceed 1, by at most 2^kLazyRescale.  The final o / l is unchanged.
@@ -93,20 +51,6 @@ __device__ __forceinline__ int64_t checked_page(const KParams& P, int page) {
     return page;
 }
 
-// FP8 pages hold OCP FP8 E4M3 codes (1 sign, 4 exponent bits of bias 7, 3 mantissa bits).  Every code's value is a
-// bf16 number, so the tiles turn codes into bf16 MFMA operands exactly; the tensor's scale is applied once, to the
-// scores (K) and to the final output (V).
-// Four codes of a dword -> four bf16, in order (the conversion instruction takes the two codes of one 16-bit half).
-__device__ __forceinline__ u32x2 fp8x4_to_bf16x4(uint32_t w) {
-    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
-    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
-    return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
-}
-__device__ __forceinline__ u32x4 fp8x8_to_bf16x8(u32x2 w) {
-    const u32x2 a = fp8x4_to_bf16x4(w[0]), b = fp8x4_to_bf16x4(w[1]);
-    return u32x4{a[0], a[1], b[0], b[1]};
-}
-
 // Clamp to the code's range with the NaN-propagating minimum and maximum: magnitudes from 448 on (infinities included)
 // become 448, a NaN stays one.
 __device__ __forceinline__ float e4m3_clamp(float y) {
@@ -127,14 +71,6 @@ __device__ __forceinline__ uint32_t e4m3_codes(uint32_t lo, uint32_t hi, float i
     // the instruction gives every NaN the same sign: the codes take theirs from the inputs (inv > 0)
     const uint32_t signs = __builtin_amdgcn_perm(hi, lo, 0x07050301u);  // the upper byte of each bf16
     return ((uint32_t)w & 0x7F7F7F7Fu) | (signs & 0x80808080u);
-}
-
-// Zeroes the bf16 elements e of a granule of 8 tokens whose position first + e is >= kv_total (never written).
-__device__ __forceinline__ u32x4 zero_unwritten(u32x4 v, int first, int kv_total) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (first + e >= kv_total) v[e >> 1] &= (e & 1) ? 0x0000FFFFu : 0xFFFF0000u;
-    return v;
 }
 
 // ---------------------------------------------------------------------------------------------------
