@@ -228,6 +228,63 @@ ppd_status ppd_mixed_attention_static(ppd_ctx *ctx, const void *q, const void *k
                                       int32_t max_pages, const int32_t *L, const int32_t *n, int32_t B, float scale,
                                       void *out, void *stream);
 
+/* ---- Drafting and eviction ----
+ * Speculative decoding on the decode node drafts a tree of tokens per sequence, verifies all of them in one step and keeps one path;
+ * contexts that outgrow the pool are cut down to the tokens that attention looks at.  Four calls, on pools of either element
+ * format, all asynchronous on `stream` and under the conventions above (a plan changed under capture is refused, as by
+ * ppd_mixed_attention; ppd_kv_select and ppd_kv_compact have no plan and can always be captured). */
+
+/* Attention for a tree of drafted tokens over the cache.  Sequence i has L_i cached tokens and n_i drafted nodes, whose K/V have been
+ * appended at positions L_i .. L_i + n_i - 1 (in any order in which the caller numbers them).  Row j sees the keys 0 .. L_i - 1 and
+ * node k exactly if bit k of its mask is set; a row does not see itself unless its own bit is.  A row that sees nothing (L_i = 0
+ * and no bit) gives zeros.  What a row does not see has no influence on it, infinities and NaN among the nodes included.
+ *   q, out        device bf16 [T][Hq][D], T = sum n_i, rows grouped by sequence in batch order
+ *   tree_mask     device uint64 [T][mask_words], 8-byte aligned; bit k % 64 of word k / 64 of a row is node k; bits from n_i on are
+ *                 ignored; 1 <= mask_words <= 16 and n_i <= 64 * mask_words
+ *   the rest      as for ppd_mixed_attention */
+ppd_status ppd_tree_attention(ppd_ctx *ctx, const void *q, const void *kv_pages, const int32_t *page_tables,
+                              int32_t max_pages, const uint64_t *tree_mask, int32_t mask_words, const int32_t *L,
+                              const int32_t *n, int32_t B, float scale, void *out, void *stream);
+
+/* Causal attention (row j of a sequence sees keys 0 .. L_i + j: decode rows, or the last rows of a prompt) that also adds up how much
+ * every key of the sequence was looked at, for each KV head over the rows and the G query heads of its group:
+ *   weights[i][h][t] = (t < L_i ? weights[i][h][t] : 0) + sum over rows j and heads of the group of the probability of key t
+ * for t < L_i + n_i; entries behind are not touched, so appended tokens need no clearing.
+ *   weights       device float [B][Hkv][weight_stride], 4-byte aligned, weight_stride >= L_i + n_i
+ *   the rest      as for ppd_mixed_attention
+ * Sums are binary32 in a fixed order: bitwise the same from run to run. */
+ppd_status ppd_weighted_attention(ppd_ctx *ctx, const void *q, const void *kv_pages, const int32_t *page_tables,
+                                  int32_t max_pages, const int32_t *L, const int32_t *n, int32_t B, float scale,
+                                  void *out, float *weights, int64_t weight_stride, void *stream);
+
+/* Chooses the tokens that every (sequence, KV head) keeps: the first `sinks`, the last `recent`, and of the others the heaviest, so many
+ * that min(budget, length_i) are kept.  Equal weights: the lower position first.  NaN counts as heavier than infinity, and both
+ * zeros as equal.
+ *   weights       device float [B][Hkv][weight_stride]
+ *   length        HOST int32 [B], tokens of every sequence, 0 <= length_i <= weight_stride
+ *   budget        >= 1; sinks, recent >= 0; sinks + recent <= budget
+ *   keep          device int32 [B][Hkv][keep_stride], keep_stride >= min(budget, length_i): positions in ascending order; entries from
+ *                 min(budget, length_i) on are not touched */
+ppd_status ppd_kv_select(ppd_ctx *ctx, const float *weights, int64_t weight_stride, const int32_t *length, int32_t B,
+                         int32_t budget, int32_t sinks, int32_t recent, int32_t *keep, int64_t keep_stride, void *stream);
+
+/* Moves kept tokens to the front, in place, in the pages of num_layers layers: for i < count_b the K and V of token keep[i] go to
+ * position first_b + i, for every KV head.  The accepted path of a tree: keep = its positions, first_b = L_b, the same list for all heads
+ * and layers.  An eviction: the lists of ppd_kv_select, first_b = 0, count_b = min(budget, length_b).  Positions from
+ * first_b + count_b on keep what they hold; the caller shortens the sequence and frees its pages.  Pages that other sequences share
+ * must have been copied before.
+ *   kv_pages, layer_stride_elems, num_layers   as for ppd_kv_land
+ *   keep          device int32; the list of (layer l, sequence b, head h) starts at keep + l * keep_layer_stride + b * keep_seq_stride
+ *                 + h * keep_head_stride (a stride of 0: shared).  A list ascends strictly and has keep[i] >= first_b + i; an
+ *                 entry that does not, or lies outside the page table (or the weights), is left where it is and raises device error
+ *                 flag bit 3
+ *   first, count  HOST int32 [B]
+ *   weights       device float [num_layers][B][Hkv][weight_stride] moved along with the tokens, or NULL */
+ppd_status ppd_kv_compact(ppd_ctx *ctx, void *kv_pages, int64_t layer_stride_elems, int32_t num_layers,
+                          const int32_t *page_tables, int32_t max_pages, const int32_t *keep, int64_t keep_layer_stride,
+                          int64_t keep_seq_stride, int64_t keep_head_stride, const int32_t *first, const int32_t *count,
+                          int32_t B, float *weights, int64_t weight_stride, void *stream);
+
 /* Statistics of the plan built by the last ppd_mixed_attention call on this context. */
 ppd_status ppd_get_plan_stats(const ppd_ctx *ctx, ppd_plan_stats *stats);
 
@@ -241,7 +298,7 @@ ppd_status ppd_plan_build(const ppd_shape *shape, const int32_t *L, const int32_
 
 /* Synchronises `stream`, then returns and clears the sticky device error flags (bit 0: append slot out of
  * range, bit 1: page id out of range, bit 2: duplicate slot within an append -- looked for only under
- * PPD_DEBUG_SLOTS=1) in *flags. */
+ * PPD_DEBUG_SLOTS=1 --, bit 3: an entry of a ppd_kv_compact list out of order or range) in *flags. */
 ppd_status ppd_device_error_flags(ppd_ctx *ctx, void *stream, uint32_t *flags);
 
 /* With option "timing" set: waits for the mixed-attention kernel of the last ppd_mixed_attention call and

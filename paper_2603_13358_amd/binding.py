@@ -47,6 +47,7 @@ class PlanStats(ctypes.Structure):
 
 EXPORTS = ["ppd_create", "ppd_destroy", "ppd_last_error", "ppd_set_option", "ppd_kv_append", "ppd_kv_land",
            "ppd_transfer_delay_s", "ppd_mixed_attention", "ppd_mixed_attention_static",
+           "ppd_tree_attention", "ppd_weighted_attention", "ppd_kv_select", "ppd_kv_compact",
            "ppd_get_plan_stats", "ppd_plan_build", "ppd_device_error_flags", "ppd_last_kernel_ms", "ppd_timed_kernels_ms",
            "ppd_route_score", "ppd_route_table_build", "ppd_route_cell", "ppd_route_decide", "ppd_route_decide_batch", "ppd_version"]
 
@@ -77,6 +78,10 @@ def load_library():
     lib.ppd_transfer_delay_s.restype = ctypes.c_double
     lib.ppd_mixed_attention.argtypes = [vp, vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp]
     lib.ppd_mixed_attention_static.argtypes = lib.ppd_mixed_attention.argtypes
+    lib.ppd_tree_attention.argtypes = [vp, vp, vp, vp, i32, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp]
+    lib.ppd_weighted_attention.argtypes = [vp, vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp, i64, vp]
+    lib.ppd_kv_select.argtypes = [vp, vp, i64, vp, i32, i32, i32, i32, vp, i64, vp]
+    lib.ppd_kv_compact.argtypes = [vp, vp, i64, i32, vp, i32, vp, i64, i64, i64, vp, vp, i32, vp, i64, vp]
     lib.ppd_get_plan_stats.argtypes = [vp, ctypes.POINTER(PlanStats)]
     lib.ppd_plan_build.argtypes = [ctypes.POINTER(Shape), vp, vp, i32, i32, i32, i32, i32, i32,
                                    ctypes.POINTER(WorkItem), i64, ctypes.POINTER(PlanStats)]
@@ -179,6 +184,77 @@ def ppd_mixed_attention(ctx, q, kv_pages, page_tables, L, n, scale, out, max_pag
 def ppd_mixed_attention_static(ctx, q, kv_pages, page_tables, L, n, scale, out, max_pages=None, stream=None):
     ppd_mixed_attention(ctx, q, kv_pages, page_tables, L, n, scale, out, max_pages=max_pages, stream=stream,
                         static=True)
+
+
+def _ptr(x):
+    """A tensor's address, or an address or None as it is."""
+    return x.data_ptr() if hasattr(x, "data_ptr") else x
+
+
+def _lengths(*arrays):
+    """Host int32 arrays of one length."""
+    arrays = [_host_i32(a).reshape(-1) for a in arrays]
+    if any(a.shape != arrays[0].shape for a in arrays):
+        raise PPDError(-3, "the host arrays differ in length")
+    return arrays
+
+
+def ppd_tree_attention(ctx, q, kv_pages, page_tables, L, n, tree_mask, scale, out, max_pages=None, mask_words=None, stream=None):
+    """tree_mask: int64 or uint64 [rows][words], or an address with mask_words."""
+    lib = load_library()
+    L, n = _lengths(L, n)
+    max_pages = page_tables.shape[1] if max_pages is None else max_pages
+    mask_words = tree_mask.shape[1] if mask_words is None else mask_words
+    status = lib.ppd_tree_attention(ctx, _ptr(q), _ptr(kv_pages), _ptr(page_tables), max_pages, _ptr(tree_mask), mask_words, L.ctypes.data, n.ctypes.data,
+                                    L.shape[0], scale, _ptr(out), stream)
+    if status != 0:
+        _check(status, ctx)
+
+
+def ppd_weighted_attention(ctx, q, kv_pages, page_tables, L, n, scale, out, weights, max_pages=None, weight_stride=None, stream=None):
+    """weights: float32 [sequences][KV heads][stride]."""
+    lib = load_library()
+    L, n = _lengths(L, n)
+    max_pages = page_tables.shape[1] if max_pages is None else max_pages
+    weight_stride = weights.shape[-1] if weight_stride is None else weight_stride
+    status = lib.ppd_weighted_attention(ctx, _ptr(q), _ptr(kv_pages), _ptr(page_tables), max_pages, L.ctypes.data, n.ctypes.data, L.shape[0], scale,
+                                        _ptr(out), _ptr(weights), weight_stride, stream)
+    if status != 0:
+        _check(status, ctx)
+
+
+def ppd_kv_select(ctx, weights, length, budget, sinks, recent, keep, weight_stride=None, keep_stride=None, stream=None):
+    """weights: float32 [sequences][KV heads][stride]; keep: int32 [sequences][KV heads][stride]."""
+    lib = load_library()
+    length, = _lengths(length)
+    weight_stride = weights.shape[-1] if weight_stride is None else weight_stride
+    keep_stride = keep.shape[-1] if keep_stride is None else keep_stride
+    status = lib.ppd_kv_select(ctx, _ptr(weights), weight_stride, length.ctypes.data, length.shape[0], budget, sinks, recent, _ptr(keep), keep_stride, stream)
+    if status != 0:
+        _check(status, ctx)
+
+
+def ppd_kv_compact(ctx, kv_pages, page_tables, keep, first, count, layer_stride_elems=0, num_layers=1, weights=None, keep_strides=None, max_pages=None,
+                   weight_stride=None, stream=None):
+    """keep: int32 [sequences][n] (shared by heads and layers), [sequences][KV heads][n] (shared by layers) or [layers][sequences][KV heads][n],
+    or an address with keep_strides = (layer, sequence, head).  weights: float32 [sequences][KV heads][stride], with a layer axis in front
+    if there are several, or None."""
+    lib = load_library()
+    first, count = _lengths(first, count)
+    max_pages = page_tables.shape[1] if max_pages is None else max_pages
+    if keep_strides is None:
+        strides = tuple(keep.stride())
+        if len(strides) not in (2, 3, 4) or strides[-1] != 1 and keep.shape[-1] > 1:
+            raise PPDError(-3, "keep has two, three or four axes, the last contiguous")
+        if keep.shape[-1] < (count.max() if count.size else 0):
+            raise PPDError(-3, "keep has fewer entries than count")
+        keep_strides = (0, strides[0], 0) if len(strides) == 2 else (0,) + strides[:2] if len(strides) == 3 else strides[:3]
+    if weight_stride is None:
+        weight_stride = 0 if weights is None else weights.shape[-1]
+    status = lib.ppd_kv_compact(ctx, _ptr(kv_pages), layer_stride_elems, num_layers, _ptr(page_tables), max_pages, _ptr(keep), *keep_strides,
+                                first.ctypes.data, count.ctypes.data, first.shape[0], _ptr(weights), weight_stride, stream)
+    if status != 0:
+        _check(status, ctx)
 
 
 def ppd_get_plan_stats(ctx):
@@ -307,6 +383,18 @@ class Context:
 
     def mixed_attention_static(self, q, kv_pages, page_tables, L, n, scale, out, stream=None):
         ppd_mixed_attention_static(self.handle, q, kv_pages, page_tables, L, n, scale, out, stream=stream)
+
+    def tree_attention(self, q, kv_pages, page_tables, L, n, tree_mask, scale, out, stream=None):
+        ppd_tree_attention(self.handle, q, kv_pages, page_tables, L, n, tree_mask, scale, out, stream=stream)
+
+    def weighted_attention(self, q, kv_pages, page_tables, L, n, scale, out, weights, stream=None):
+        ppd_weighted_attention(self.handle, q, kv_pages, page_tables, L, n, scale, out, weights, stream=stream)
+
+    def kv_select(self, weights, length, budget, sinks, recent, keep, stream=None):
+        ppd_kv_select(self.handle, weights, length, budget, sinks, recent, keep, stream=stream)
+
+    def kv_compact(self, kv_pages, page_tables, keep, first, count, layer_stride_elems=0, num_layers=1, weights=None, stream=None):
+        ppd_kv_compact(self.handle, kv_pages, page_tables, keep, first, count, layer_stride_elems, num_layers, weights, stream=stream)
 
     def plan_stats(self):
         return ppd_get_plan_stats(self.handle)

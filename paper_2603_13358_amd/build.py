@@ -9,8 +9,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libppd.so")
 CALL = os.path.join(HERE, "ppd_call" + sysconfig.get_config_var("EXT_SUFFIX"))  # of this interpreter
 CALL_SOURCE = os.path.join(CSRC, "ppd_call.c")
-SOURCES = ["ppd_api.hip", "ppd_kernels.hip", "ppd_plan.cpp", "ppd_route.cpp"]
-HEADERS = ["ppd_internal.h", "ppd_context.h", "ppd_device.h", os.path.join("..", "..", "include", "ppd.h")]
+SOURCES = ["ppd_api.hip", "ppd_kernels.hip", "ppd_plan.cpp", "ppd_route.cpp",
+           "ppd_ops_api.hip", "ppd_tree_kernels.hip", "ppd_cache_kernels.hip", "ppd_tree_plan.cpp"]
+HEADERS = ["ppd_internal.h", "ppd_context.h", "ppd_device.h", "ppd_ops.h", os.path.join("..", "..", "include", "ppd.h")]
 
 # Packed-FP32 instructions are switched off for all device code (the host pass does not know the feature
 # and says so; that warning is harmless).

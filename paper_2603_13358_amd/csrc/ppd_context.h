@@ -73,7 +73,7 @@ struct ppd_ctx {
     bool timing = false;
     std::vector<std::pair<hipEvent_t, hipEvent_t>> ev_pairs;
     size_t ev_used = 0;
-    // drafting and eviction (ppd_tree.hip): their plan and workspace, made by the first call that needs one
+    // drafting and eviction (ppd_ops_api.hip): their plan and workspace, made by the first call that needs one
     void* tree = nullptr;
     void (*free_tree)(void*) = nullptr;
 };

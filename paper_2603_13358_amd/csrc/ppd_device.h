@@ -49,6 +49,16 @@ __device__ __forceinline__ float sum_halves(float v) {
     return lo + hi;
 }
 
+// The running maximum is only raised (and the accumulators rescaled) when it would grow by more than this many
+// powers of two; until then probabilities may exceed 1, by at most 2^kLazyRescale.  The final o / l is unchanged.
+// (Row-block tiles do not look for the maximum: there the bound is on the sum of a lane's 32 probabilities.)
+#ifndef kLazyRescale
+#define kLazyRescale 8.0f
+#endif
+constexpr float power_of_two(float e) { return e >= 1.0f ? 2.0f * power_of_two(e - 1.0f) : 1.0f; }
+constexpr float kMaxLazyP = power_of_two(kLazyRescale);
+static_assert((int)kLazyRescale == kLazyRescale, "a whole number of powers of two");
+
 // FP8 pages hold OCP FP8 E4M3 codes (1 sign, 4 exponent bits of bias 7, 3 mantissa bits).  Every code's value is a
 // bf16 number, so the tiles turn codes into bf16 MFMA operands exactly; the tensor's scale is applied once, to the
 // scores (K) and to the final output (V).

@@ -24,16 +24,6 @@ namespace ppd {
 // with inv = 65536 / G + 1, exact for col < 4096 and G <= 16.
 __device__ __forceinline__ int col_row(int col, int inv) { return (int)(((unsigned)col * (unsigned)inv) >> 16); }
 
-// The running maximum is only raised (and the accumulators rescaled) when it would grow by more than this many
-// powers of two; until then probabilities may exceed 1, by at most 2^kLazyRescale.  The final o / l is unchanged.
-// (Row-block tiles do not look for the maximum: there the bound is on the sum of a lane's 32 probabilities.)
-#ifndef kLazyRescale
-#define kLazyRescale 8.0f
-#endif
-constexpr float power_of_two(float e) { return e >= 1.0f ? 2.0f * power_of_two(e - 1.0f) : 1.0f; }
-constexpr float kMaxLazyP = power_of_two(kLazyRescale);
-static_assert((int)kLazyRescale == kLazyRescale, "a whole number of powers of two");
-
 // Raw page-table entry of logical page `pi` of a sequence; pi is clamped so that no access leaves the page
 // table row.  The value is NOT inspected here: a caller that prefetches it must not wait for the load.
 __device__ __forceinline__ int load_page_id(const int32_t* pt_row, int pi, int last_page) {

@@ -1,0 +1,399 @@
+// gfx950 kernels of tree and weighted attention over the page pool.
+//
+//   out[j, h] = sum_t p_t v_t,   p = softmax over the visible t of scale * q[j, h] . k_t
+//   weights[b, kvh, t] (+)= sum over the sequence's rows j and the group's heads h of p_t
+//
+// As in the mixed kernels the products are the transposed ones, S^T = K Q^T and O^T = V^T P^T: the accumulators of the first
+// are the operands of the second, and every quantity of a row's softmax lives in the lanes that own its column.
+#include <hip/hip_runtime.h>
+
+#include "ppd_device.h"
+#include "ppd_ops.h"
+
+namespace ppd {
+
+namespace {
+
+template <bool FP8> struct Granule;  // eight elements of the pool as they are loaded
+template <> struct Granule<false> { typedef u32x4 type; };
+template <> struct Granule<true> { typedef u32x2 type; };
+
+__device__ __forceinline__ u32x4 operand(u32x4 g) { return g; }
+__device__ __forceinline__ u32x4 operand(u32x2 g) { return fp8x8_to_bf16x8(g); }
+
+__device__ __forceinline__ bool not_finite(uint32_t bf16_bits) { return (bf16_bits & 0x7F80u) == 0x7F80u; }
+
+// Page ids of the tile's keys, checked, to LDS: an id outside the pool raises the sticky flag and is replaced by page 0.
+__device__ __forceinline__ void stage_pages(const TreeParams& P, int seq, int kv_begin, int kv_total, int count, int* ids) {
+    const int32_t* row = P.page_tables + (int64_t)seq * P.max_pages;
+    const int last = (kv_total - 1) / kPage, first = kv_begin / kPage;
+    for (int i = threadIdx.x; i < count; i += blockDim.x) {
+        int id = row[first + i < last ? first + i : last];
+        if (id < 0 || id >= P.num_pages) {
+            atomicOr(P.err_flags, 2u);
+            id = 0;
+        }
+        ids[i] = id;
+    }
+}
+
+// Which of the 32 keys from `base` on the row may see, a bit each: all cached ones, and of the new ones those in its mask, or,
+// without masks, those up to itself.
+__device__ __forceinline__ uint32_t visible_keys(const TreeParams& P, const TreeItem& it, int jrow, int base) {
+    const int valid = it.kv_total - base, off = base - it.L;  // new token of the first key; above -32 where this is called
+    uint32_t seen;
+    if (P.mask) {
+        const uint64_t* words = P.mask + (int64_t)(it.grow0 + jrow) * P.mask_words;
+        if (off < 0) {
+            const uint32_t cached = -off >= 32 ? ~0u : (1u << -off) - 1u;
+            seen = cached | (-off >= 32 ? 0u : (uint32_t)(words[0] << -off));
+        } else {
+            const int w = off >> 6, b = off & 63;
+            uint64_t v = w < P.mask_words ? words[w] >> b : 0;
+            if (b > 32 && w + 1 < P.mask_words) v |= words[w + 1] << (64 - b);
+            seen = (uint32_t)v;
+        }
+    } else {
+        const int upto = jrow - off + 1;
+        seen = upto >= 32 ? ~0u : upto <= 0 ? 0u : (1u << upto) - 1u;
+    }
+    if (valid < 32) seen &= valid <= 0 ? 0u : (1u << valid) - 1u;
+    return seen;
+}
+
+}  // namespace
+
+// A tree tile: up to 32 query columns against a range of keys.  Four waves, each with every fourth slab of 32 keys, which it
+// takes from the pool straight into registers in the layouts of the matrix instructions' operands: no LDS, no barrier.  The
+// waves' results meet in LDS at the end.
+template <int HD, bool FP8>
+__global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreeParams P) {
+    typedef typename Granule<FP8>::type Raw;
+    constexpr int EB = FP8 ? 1 : 2, KS = HD / 16, DB = HD / 32;
+    constexpr int CB = 16;          // columns that meet in LDS at a time
+    constexpr int ROW = HD + 4;     // floats of a staged column: the padding spreads the columns over the banks
+    __shared__ int ids[kMaxTreeChunk / kPage];
+    __shared__ __attribute__((aligned(16))) float stage[kTreeWaves][CB * ROW];
+    __shared__ float stage_ml[kTreeWaves][CB][2];
+
+    const TreeItem it = P.items[blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int h = lane >> 5, l32 = lane & 31;
+    const int col = it.col0 + (l32 < it.ncols ? l32 : it.ncols - 1);
+    const int jrow = col / P.G, head = it.kvh * P.G + (col - jrow * P.G);
+    const float c = P.scale_log2e;
+
+    const int slabs = (it.kv_end - it.kv_begin + kSlab - 1) / kSlab;
+    stage_pages(P, it.seq, it.kv_begin, it.kv_total, slabs * 2, ids);
+    bf16x8 qreg[KS];
+    {
+        const uint16_t* qp = P.q + ((int64_t)(it.grow0 + jrow) * P.Hq + head) * HD + h * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qreg[ks] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + ks * 16));
+    }
+    __syncthreads();
+
+    // Row r of the K operand is token 8*bit2(r) + 4*bit3(r) + (r & 3) of page bit4(r): registers 8p .. 8p+7 of a lane are then eight
+    // consecutive tokens of page p, which is what the second product takes.
+    const int k_tok = ((l32 >> 2) & 1) * 8 + ((l32 >> 3) & 1) * 4 + (l32 & 3);
+    const char* const pool = static_cast<const char*>(P.pool) + (int64_t)it.kvh * (kPage * HD) * EB;
+    const char* const k_lane = pool + (h * 16 + k_tok) * (8 * EB);
+    const char* const v_lane = pool + ((int64_t)P.Hkv * (kPage * HD) + (h * HD + l32) * 8) * EB;
+    const int64_t page_bytes = P.page_stride * EB;
+
+    Raw kr[KS], vr[2][DB];
+    auto load_k = [&](int s) {
+        const char* p = k_lane + (int64_t)ids[s * 2 + (l32 >> 4)] * page_bytes;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kr[ks] = *reinterpret_cast<const Raw*>(p + ks * (2 * 16 * 8 * EB));
+    };
+    auto load_v = [&](int s) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const char* vp = v_lane + (int64_t)__builtin_amdgcn_readfirstlane(ids[s * 2 + p]) * page_bytes;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) vr[p][db] = *reinterpret_cast<const Raw*>(vp + db * (32 * 8 * EB));
+        }
+    };
+
+    f32x16 oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
+    float m_run = NEG_INF, l_run = 0.f;
+
+    if (wave < slabs) {
+        load_k(wave);
+        load_v(wave);
+    }
+    for (int s = wave; s < slabs; s += kTreeWaves) {
+        const int base = it.kv_begin + s * kSlab;
+        f32x16 sc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(operand(kr[ks])), qreg[ks], sc, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        const bool more = s + kTreeWaves < slabs;
+        if (more) load_k(s + kTreeWaves);
+        __builtin_amdgcn_sched_barrier(0);
+        u32x4 vv[2][DB];
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) vv[p][db] = operand(vr[p][db]);
+        uint32_t seen = ~0u;
+        bool strange = false;  // a new token's V that is not finite: not every row may see it
+        if (base + kSlab > it.L) {
+            seen = visible_keys(P, it, jrow, base);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!((seen >> ((i >> 3) * 16 + h * 8 + (i & 7))) & 1u)) sc[i] = NEG_INF;
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int pos = base + p * 16 + h * 8 + e;
+                        const uint32_t bits = (e & 1) ? vv[p][db][e >> 1] >> 16 : vv[p][db][e >> 1] & 0xFFFFu;
+                        const bool odd = pos >= it.L && not_finite(bits);
+                        strange |= odd && pos < it.kv_total;
+                        if (odd || pos >= it.kv_total) vv[p][db][e >> 1] &= (e & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+                    }
+        }
+        // The exponentials are taken against the running reference as it is; only where a lane's sum of 16 of them is above
+        // 2^kLazyRescale (or not a number: no reference yet) is the maximum looked for and everything rescaled.
+        u32x4 pw[2];
+        float psum = 0.f;
+        auto exponentials = [&](float mc) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float p0 = fast_exp2(__builtin_fmaf(sc[2 * e], c, -mc));
+                const float p1 = fast_exp2(__builtin_fmaf(sc[2 * e + 1], c, -mc));
+                psum += p0 + p1;
+                pw[e >> 2][e & 3] = pack_bf16(p0, p1);
+            }
+        };
+        exponentials(m_run * c);
+        if (__any(!(psum <= kMaxLazyP))) {
+            float mx = sc[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+            mx = max_halves(mx);
+            const float m_new = fmaxf(m_run, mx);
+            const float m_use = m_new == NEG_INF ? 0.f : m_new;
+            const float alpha = fast_exp2(m_run * c - m_use * c);  // m_run = -inf gives 0
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
+            m_run = m_new;
+            psum = 0.f;
+            exponentials(m_use * c);
+        }
+        l_run += psum;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vv[p][db]), as_bf16x8(pw[p]), oacc[db], 0, 0, 0);
+        if (__any(strange)) {
+            // Elements that are not finite were left out of the product, where rows that do not see them would have taken NaN from
+            // them; rows that do get them here, whatever their probability.
+            for (int t = 0; t < kSlab; ++t) {
+                const int pos = base + t;
+                if (pos < it.L || pos >= it.kv_total || !__any((seen >> t) & 1u)) continue;
+                const char* vt = pool + ((int64_t)ids[s * 2 + (t >> 4)] * P.page_stride + (int64_t)P.Hkv * (kPage * HD) + ((t >> 3) & 1) * (HD * 8) + (t & 7)) * EB;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int d = db * 32 + (i >> 2) * 8 + h * 4 + (i & 3);
+                        uint32_t bits;
+                        if constexpr (FP8) bits = fp8x4_to_bf16x4(*reinterpret_cast<const uint8_t*>(vt + d * 8))[0] & 0xFFFFu;
+                        else bits = *reinterpret_cast<const uint16_t*>(vt + d * 16);
+                        if (((seen >> t) & 1u) && not_finite(bits)) oacc[db][i] += __builtin_bit_cast(float, bits << 16);
+                    }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) load_v(s + kTreeWaves);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
+    const float l_tot = sum_halves(l_run);
+    for (int c0 = 0; c0 < it.ncols; c0 += CB) {
+        __syncthreads();
+        if (l32 >= c0 && l32 < c0 + CB) {
+            float* to = &stage[wave][(l32 - c0) * ROW + h * 4];
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<f32x4*>(to + db * 32 + i * 8) = f32x4{oacc[db][4 * i], oacc[db][4 * i + 1], oacc[db][4 * i + 2], oacc[db][4 * i + 3]};
+            if (h == 0) {
+                stage_ml[wave][l32 - c0][0] = m_run;
+                stage_ml[wave][l32 - c0][1] = l_tot;
+            }
+        }
+        __syncthreads();
+        const int nc = it.ncols - c0 < CB ? it.ncols - c0 : CB;
+        for (int idx = tid; idx < nc * (HD / 4); idx += kTreeThreads) {
+            const int cl = idx / (HD / 4), d = (idx % (HD / 4)) * 4;
+            float mm = NEG_INF;
+#pragma unroll
+            for (int w = 0; w < kTreeWaves; ++w) mm = fmaxf(mm, stage_ml[w][cl][0]);
+            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+            float l = 0.f;
+#pragma unroll
+            for (int w = 0; w < kTreeWaves; ++w) {
+                const float mw = stage_ml[w][cl][0];
+                const float f = mw == NEG_INF ? 0.f : fast_exp2((mw - mm) * c);
+                l += f * stage_ml[w][cl][1];
+                if (mw != NEG_INF) o += f * *reinterpret_cast<const f32x4*>(&stage[w][cl * ROW + d]);
+            }
+            const int cc = c0 + cl;
+            if (it.split) {
+                float* to = P.partials + it.part_off;
+                *reinterpret_cast<f32x4*>(to + cc * HD + d) = o;
+                if (d == 0) *reinterpret_cast<f32x2*>(to + it.ncols * HD + cc * 2) = f32x2{mm, l};
+            } else {
+                const int oc = it.col0 + cc, row = oc / P.G;
+                const int64_t at = (int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (oc - row * P.G);
+                const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing gives zeros
+                const f32x4 r = o * (inv * P.v_scale);
+                *reinterpret_cast<u32x2*>(P.out + at * HD + d) = u32x2{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
+                if (P.stats && d == 0) *reinterpret_cast<f32x2*>(P.stats + at * 2) = f32x2{mm == NEG_INF ? 0.f : mm, inv};
+            }
+        }
+    }
+}
+
+// Joins the partials of split key ranges, splits in order.
+constexpr int kJoinCols = 8;
+template <int HD>
+__global__ __launch_bounds__(256) void ppd_tree_join_kernel(const TreeParams P) {
+    const TreeGroup g = P.groups[blockIdx.x];
+    constexpr int LANES = HD / 4;
+    const int col = blockIdx.y * kJoinCols + threadIdx.x / LANES, d = (threadIdx.x % LANES) * 4;
+    if (threadIdx.x >= kJoinCols * LANES || col >= g.ncols) return;
+    const float c = P.scale_log2e;
+    const float* base = P.partials + g.part_off;
+    float mm = NEG_INF;
+    for (int j = 0; j < g.nsplit; ++j) mm = fmaxf(mm, base[g.part_stride * j + g.ncols * HD + col * 2]);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    for (int j = 0; j < g.nsplit; ++j) {
+        const float* p = base + g.part_stride * j;
+        const f32x2 ml = *reinterpret_cast<const f32x2*>(p + g.ncols * HD + col * 2);
+        if (ml[0] == NEG_INF) continue;
+        const float f = fast_exp2((ml[0] - mm) * c);
+        l += f * ml[1];
+        o += f * *reinterpret_cast<const f32x4*>(p + col * HD + d);
+    }
+    const int oc = g.col0 + col, row = oc / P.G;
+    const int64_t at = (int64_t)(g.grow0 + row) * P.Hq + g.kvh * P.G + (oc - row * P.G);
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const f32x4 r = o * (inv * P.v_scale);
+    *reinterpret_cast<u32x2*>(P.out + at * HD + d) = u32x2{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
+    if (P.stats && d == 0) *reinterpret_cast<f32x2*>(P.stats + at * 2) = f32x2{mm == NEG_INF ? 0.f : mm, inv};
+}
+
+// Adds up the weights: S = Q K^T with the keys as columns, so that a lane owns a key and the sum over the queries runs over its own
+// registers.  A wave holds K of 64 keys, read once, and goes over the sequence's query columns, 32 at a time.  The reference
+// and one over the sum of every row come from the attention before.
+template <int HD, bool FP8>
+__global__ __launch_bounds__(256) void ppd_weigh_kernel(const TreeParams P) {
+    typedef typename Granule<FP8>::type Raw;
+    constexpr int EB = FP8 ? 1 : 2, KS = HD / 16, SLABS = kWeighKeys / 4 / kSlab;
+    __shared__ int ids[kWeighKeys / kPage];
+    __shared__ f32x2 ml[2][32];
+    __shared__ int rows[2][32];
+    const WeighItem it = P.weighs[blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int h = lane >> 5, l32 = lane & 31;
+    stage_pages(P, it.seq, it.kv_begin, it.kv_total, kWeighKeys / kPage, ids);
+    __syncthreads();
+    const char* const pool = static_cast<const char*>(P.pool) + ((int64_t)it.kvh * (kPage * HD) + (h * 16 + (l32 & 15)) * 8) * EB;
+    u32x4 kreg[SLABS][KS];
+#pragma unroll
+    for (int s = 0; s < SLABS; ++s) {
+        const char* p = pool + (int64_t)ids[(wave * SLABS + s) * 2 + (l32 >> 4)] * P.page_stride * EB;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kreg[s][ks] = operand(*reinterpret_cast<const Raw*>(p + ks * (2 * 16 * 8 * EB)));
+    }
+    const float c = P.scale_log2e;
+    float sum[SLABS];
+#pragma unroll
+    for (int s = 0; s < SLABS; ++s) sum[s] = 0.f;
+    const int base = it.kv_begin + wave * (SLABS * kSlab);
+    const bool tail = base + SLABS * kSlab > it.L;  // new tokens among the wave's keys: not every row sees them
+    for (int c0 = 0, at = 0; c0 < it.cols; c0 += 32, at ^= 1) {
+        if (tid < 32) {
+            const int cc = c0 + tid, row = cc / P.G;
+            const bool live = cc < it.cols;
+            ml[at][tid] = live ? *reinterpret_cast<const f32x2*>(P.stats + ((int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G)) * 2) : f32x2{0.f, 0.f};
+            rows[at][tid] = row;
+        }
+        __syncthreads();  // the buffer written two rounds on is read by nobody any more
+        const int cc = c0 + l32 < it.cols ? c0 + l32 : it.cols - 1, row = cc / P.G;
+        const uint16_t* qp = P.q + ((int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G)) * HD + h * 8;
+        bf16x8 qreg[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qreg[ks] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + ks * 16));
+#pragma unroll
+        for (int s = 0; s < SLABS; ++s) {
+            f32x16 sc;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qreg[ks], as_bf16x8(kreg[s][ks]), sc, 0, 0, 0);
+            const int key = base + s * kSlab + l32;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = (i & 3) + 8 * (i >> 2) + 4 * h;
+                const f32x2 w = ml[at][r];
+                if (c0 + r < it.cols && (!tail || key <= it.L + rows[at][r])) sum[s] += fast_exp2((sc[i] - w[0]) * c) * w[1];
+            }
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < SLABS; ++s) {
+        const float total = sum_halves(sum[s]);
+        const int key = base + s * kSlab + l32;
+        if (h == 0 && key < it.kv_total) {
+            float* to = P.weights + ((int64_t)it.seq * P.Hkv + it.kvh) * P.weight_stride + key;
+            *to = key < it.L ? *to + total : total;
+        }
+    }
+}
+
+#define PPD_BY_FORM(KERNEL, GRID, THREADS)                                                                                        \
+    do {                                                                                                                          \
+        if (head_dim == 128 && fp8_pages) hipLaunchKernelGGL((KERNEL<128, true>), GRID, dim3(THREADS), 0, hs, p);                 \
+        else if (head_dim == 128) hipLaunchKernelGGL((KERNEL<128, false>), GRID, dim3(THREADS), 0, hs, p);                        \
+        else if (fp8_pages) hipLaunchKernelGGL((KERNEL<64, true>), GRID, dim3(THREADS), 0, hs, p);                                \
+        else hipLaunchKernelGGL((KERNEL<64, false>), GRID, dim3(THREADS), 0, hs, p);                                              \
+    } while (0)
+
+int launch_tree(const TreeParams& p, int head_dim, bool fp8_pages, void* stream) {
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    PPD_BY_FORM(ppd_tree_kernel, dim3((unsigned)p.n_items), kTreeThreads);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.n_groups == 0) return (int)e;
+    const dim3 grid((unsigned)p.n_groups, (kTreeCols + kJoinCols - 1) / kJoinCols);
+    if (head_dim == 128) hipLaunchKernelGGL(ppd_tree_join_kernel<128>, grid, dim3(256), 0, hs, p);
+    else hipLaunchKernelGGL(ppd_tree_join_kernel<64>, grid, dim3(256), 0, hs, p);
+    return (int)hipGetLastError();
+}
+
+int launch_weigh(const TreeParams& p, int head_dim, bool fp8_pages, void* stream) {
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    PPD_BY_FORM(ppd_weigh_kernel, dim3((unsigned)p.n_weighs), 256);
+    return (int)hipGetLastError();
+}
+
+}  // namespace ppd
