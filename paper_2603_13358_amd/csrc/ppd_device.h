@@ -81,4 +81,26 @@ __device__ __forceinline__ u32x4 zero_unwritten(u32x4 v, int first, int kv_total
     return v;
 }
 
+// Which of the 64 keys from new token `off` on (off > -64; below 0 are cached ones) a row may see, a bit each: all cached ones, and of
+// the new ones those in its mask, or, where `words` is NULL, those up to `own`.  Keys from `valid` on are not there.
+__device__ __forceinline__ uint64_t visible_keys(const uint64_t* words, int n_words, int own, int off, int valid) {
+    uint64_t seen;
+    if (words) {
+        if (off < 0) {
+            seen = (words[0] << -off) | ((1ull << -off) - 1);
+        } else {
+            const int w = off >> 6, b = off & 63;
+            seen = w < n_words ? words[w] >> b : 0;
+            if (b > 0 && w + 1 < n_words) seen |= words[w + 1] << (64 - b);
+        }
+    } else {
+        const int count = own - off + 1;
+        seen = count >= 64 ? ~0ull : count <= 0 ? 0 : (1ull << count) - 1;
+    }
+    if (valid < 64) seen &= valid <= 0 ? 0 : (1ull << valid) - 1;
+    return seen;
+}
+
+__device__ __forceinline__ bool not_finite_bf16(uint32_t bits) { return (bits & 0x7F80u) == 0x7F80u; }
+
 }  // namespace ppd

@@ -13,6 +13,7 @@
 
 #include "ppd_device.h"
 #include "ppd_internal.h"
+#include "ppd_ops.h"
 
 #ifndef PPD_PINGPONG
 #define PPD_PINGPONG 1  // 0: all waves take the loop barrier at the end of the iteration; 1: waves 4..7 mid-iteration
@@ -123,9 +124,13 @@ __device__ __forceinline__ u32x4 lds_read16(uint32_t base, int offset) {
 // loop's matrix and vector phases are the ones of bf16 pages.  The operand rings then need three stages each (the tile
 // being written, the one the early waves read and the one the late waves read), which with the staging ring is the same
 // LDS as the four-stage rings of bf16 pages.
-template <int HD, bool HALF, bool FP8 = false>
-__device__ __forceinline__ void mfma_item(const KParams& P, const ppd_work_item& it, char* smem) {
-    static_assert(!(FP8 && HALF), "FP8 pages are read by the full-tile loop only");
+//
+// TREE (P is a TreeBlockParams): which new tokens a row sees is in its mask, or, without masks, those up to itself; a new token's V
+// element that is not finite is kept out of the products, where the zero probability of a row that does not see it would make NaN
+// of it, and added to the rows that do see it afterwards; a row that sees nothing gives zeros.
+template <int HD, bool HALF, bool FP8 = false, bool TREE = false, class KP = KParams>
+__device__ __forceinline__ void mfma_item(const KP& P, const ppd_work_item& it, char* smem) {
+    static_assert(!((FP8 || TREE) && HALF), "FP8 pages and trees are worked by the full-tile loop only");
     static_assert(!FP8 || kStages == 3, "the staging of FP8 tiles is written for a prefetch distance of 3");
     constexpr int EB = FP8 ? 1 : 2;            // bytes per pool element
     constexpr int PB = kPage * HD * 2;         // bytes of one (page, head) block of K or of V as bf16 operands in LDS
@@ -160,6 +165,10 @@ __device__ __forceinline__ void mfma_item(const KParams& P, const ppd_work_item&
     const int head = it.kvh * G + (colc - jrow * G);
     const int limit = it.L + it.row0 + jrow;  // last key position this column may see
     const bool wave_active = wave * 32 < ncols;
+    [[maybe_unused]] auto tree_words = [&]() -> const uint64_t* {  // TREE: this lane's row of the masks
+        if constexpr (TREE) return P.mask ? P.mask + (int64_t)(it.grow0 + jrow) * P.mask_words : nullptr;
+        else return nullptr;
+    };
     const int wmin_limit = it.L + it.row0 + col_row((wave * 32) < ncols ? wave * 32 : ncols - 1, P.invG);
 
     // Q^T operand: column = lane % 32, d = ks*16 + (lane/32)*8 .. +8
@@ -198,6 +207,19 @@ __device__ __forceinline__ void mfma_item(const KParams& P, const ppd_work_item&
     int* lds_ids = reinterpret_cast<int*>(smem + IDS_AT);
     for (int i = tid; i < ntiles * 4; i += kThreads)
         lds_ids[i] = (int)checked_page(P, load_page_id(pt_row, first_page + i, last_page));
+    [[maybe_unused]] int* const strange = lds_ids + kMaxMfmaChunk / kPage - 1;  // TREE: its tiles have fewer keys, the last id's place is free
+    if constexpr (TREE)
+        if (tid == 0) *strange = 0;
+    // TREE: a granule of 8 tokens of one d from position `first` on without what was never written and what is not finite
+    [[maybe_unused]] auto finite_part = [&](u32x4 v, int first) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool odd = first + e >= it.L && not_finite_bf16(v[e >> 1] >> ((e & 1) * 16));
+            if (odd && first + e < it.kv_total) *strange = 1;
+            if (odd || first + e >= it.kv_total) v[e >> 1] &= (e & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+        }
+        return v;
+    };
     struct RawPages { int p[ROUNDS]; };  // the ids as they come from LDS (vector registers)
     const uint32_t page_bytes = (uint32_t)P.page_stride * EB;
     auto tile_pages_raw = [&](int ti) {
@@ -247,10 +269,16 @@ __device__ __forceinline__ void mfma_item(const KParams& P, const ppd_work_item&
         u32x4 lo = fp8x8_to_bf16x8(u32x2{raw[0], raw[1]}), hi = fp8x8_to_bf16x8(u32x2{raw[2], raw[3]});
         if (is_v) {
             const int tile_base = it.kv_begin + tile * kTileTokens;
-            if (tile_base + kTileTokens > it.kv_total) {
+            if (tile_base + kTileTokens > (TREE ? it.L : it.kv_total)) {
                 const int g0 = 2 * tid, g1 = 2 * tid + 1;  // bf16 granules of the tile: page g / GPP, (octet, d) = g % GPP
-                lo = zero_unwritten(lo, tile_base + (g0 / GPP) * 16 + ((g0 % GPP) / HD) * 8, it.kv_total);
-                hi = zero_unwritten(hi, tile_base + (g1 / GPP) * 16 + ((g1 % GPP) / HD) * 8, it.kv_total);
+                const int t0 = tile_base + (g0 / GPP) * 16 + ((g0 % GPP) / HD) * 8, t1 = tile_base + (g1 / GPP) * 16 + ((g1 % GPP) / HD) * 8;
+                if constexpr (TREE) {
+                    lo = finite_part(lo, t0);
+                    hi = finite_part(hi, t1);
+                } else {
+                    lo = zero_unwritten(lo, t0, it.kv_total);
+                    hi = zero_unwritten(hi, t1, it.kv_total);
+                }
             }
         }
         u32x4* dst = reinterpret_cast<u32x4*>(smem + dst_byte + tid * 32);
@@ -261,13 +289,14 @@ __device__ __forceinline__ void mfma_item(const KParams& P, const ppd_work_item&
     // loaded itself, after its own loads have landed).  Only the sequence's last tile needs it.
     auto fix_v_tail = [&](int ti, int lds_byte) {
         const int tile_base = it.kv_begin + ti * kTileTokens;
-        if (tile_base + kTileTokens > it.kv_total) {
+        if (tile_base + kTileTokens > (TREE ? it.L : it.kv_total)) {
 #pragma unroll
             for (int r = 0; r < ROUNDS; ++r) {
                 const int gid = r * kThreads + tid;
                 const int s = gid / GPP, within = gid % GPP;
                 u32x4* cell = reinterpret_cast<u32x4*>(smem + lds_byte + gid * 16);
-                *cell = zero_unwritten(*cell, tile_base + s * 16 + (within / HD) * 8, it.kv_total);
+                if constexpr (TREE) *cell = finite_part(*cell, tile_base + s * 16 + (within / HD) * 8);
+                else *cell = zero_unwritten(*cell, tile_base + s * 16 + (within / HD) * 8, it.kv_total);
             }
         }
     };
@@ -410,7 +439,16 @@ __device__ __forceinline__ void mfma_item(const KParams& P, const ppd_work_item&
         };
         if (wave_active) {
             const int tile_base = it.kv_begin + ti * kTileTokens;
-            if (tile_base + kTileTokens - 1 > wmin_limit) {  // causal boundary crosses this tile
+            if constexpr (TREE) {
+                if (tile_base + kTileTokens > it.L) {
+                    const uint64_t seen = visible_keys(tree_words(), P.mask_words, it.row0 + jrow, tile_base - it.L, it.kv_total - tile_base) >> (h * 8);
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!((seen >> ((tb * 2 + (i >> 3)) * 16 + (i & 7))) & 1)) s_cur[tb][i] = NEG_INF;
+                }
+            } else if (tile_base + kTileTokens - 1 > wmin_limit) {  // causal boundary crosses this tile
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
@@ -630,6 +668,25 @@ __device__ __forceinline__ void mfma_item(const KParams& P, const ppd_work_item&
 
     }
     // epilogue: O^T register i of block db is d = db*32 + (i/4)*8 + h*4 + i%4 of column `col`
+    if constexpr (TREE) {
+        if (*strange && wave_active) {  // set, if at all, before the barrier in front of the tile
+            for (int pos = it.L > it.kv_begin ? it.L : it.kv_begin; pos < it.kv_end; ++pos) {
+                const bool seen = visible_keys(tree_words(), P.mask_words, it.row0 + jrow, pos - it.L, 1) & 1;
+                if (!__any(seen)) continue;
+                const char* vt = pool_v + ((int64_t)lds_ids[(pos - it.kv_begin) >> 4] * P.page_stride + ((pos >> 3) & 1) * (HD * 8) + (pos & 7)) * EB;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const char* at = vt + (db * 32 + (i >> 2) * 8 + h * 4 + (i & 3)) * (8 * EB);
+                        uint32_t bits;
+                        if constexpr (FP8) bits = fp8x4_to_bf16x4(*reinterpret_cast<const uint8_t*>(at))[0] & 0xFFFFu;
+                        else bits = *reinterpret_cast<const uint16_t*>(at);
+                        if (seen && not_finite_bf16(bits)) oacc[db][i] += bf16_bits_to_f32(bits);
+                    }
+            }
+        }
+    }
     const float l_tot = sum_halves(l_run);
     if (it.part_off < 0) {
         // A lane holds 8-byte pieces of 32 different result rows: stored from here, every instruction would touch 32
@@ -642,7 +699,10 @@ __device__ __forceinline__ void mfma_item(const KParams& P, const ppd_work_item&
         static_assert(kWaves * 32 * RS <= NSK * KBYTES, "the staged columns fit the K ring");
         char* const stage = smem + wave * (32 * RS);
         char* const out0 = reinterpret_cast<char*>(P.out) + ((int64_t)it.grow0 * P.Hq + it.kvh * G) * (HD * 2);
-        const float inv = P.v_scale / l_tot;
+        const float inv = TREE && l_tot == 0.f ? 0.f : P.v_scale / l_tot;
+        if constexpr (TREE)
+            if (P.stats && h == 0 && col < ncols)
+                *reinterpret_cast<f32x2*>(P.stats + ((int64_t)(it.grow0 + jrow) * P.Hq + head) * 2) = f32x2{m_run, 1.0f / l_tot};
         if (wave_active) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -2025,6 +2085,15 @@ __global__ __launch_bounds__(kSmallThreads) void ppd_kv_append_kernel(const uint
     }
 }
 
+// Tree and weighted attention of more than kTreeCols query columns: a workgroup to a row block (tree tiles of fewer columns are
+// ppd_tree_kernel's).
+template <int HD, bool FP8>
+__global__ __launch_bounds__(kThreads, 2) void ppd_tree_block_kernel(const TreeBlockParams P) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const ppd_work_item it = P.items[blockIdx.x];
+    mfma_item<HD, false, FP8, true>(P, it, smem);
+}
+
 // ---------------------------------------------------------------------------------------------------
 static size_t ring_lds_bytes(int head_dim) {
     return (size_t)(2 * kStages + (PPD_PINGPONG ? 1 : 0) + (PPD_PINGPONG ? 1 : 0)) * 4 * kPage * head_dim * 2 +
@@ -2094,7 +2163,18 @@ int prepare_mixed_kernels() {
     allow(reinterpret_cast<const void*>(&ppd_pipelined_kernel<64>), pipelined_lds_bytes<64>());
     allow(reinterpret_cast<const void*>(&ppd_mfma_kernel<128>), ring_lds_bytes(128));
     allow(reinterpret_cast<const void*>(&ppd_mfma_kernel<64>), ring_lds_bytes(64));
+    allow(reinterpret_cast<const void*>(&ppd_tree_block_kernel<128, false>), ring_lds_bytes(128));
+    allow(reinterpret_cast<const void*>(&ppd_tree_block_kernel<64, false>), ring_lds_bytes(64));
+    allow(reinterpret_cast<const void*>(&ppd_tree_block_kernel<128, true>), ring_lds_bytes(128));
+    allow(reinterpret_cast<const void*>(&ppd_tree_block_kernel<64, true>), ring_lds_bytes(64));
     return (int)e;
+}
+
+int launch_tree_blocks(const TreeBlockParams& p, int head_dim, bool fp8_pages, void* stream) {
+    auto* const kernel = head_dim == 128 ? (fp8_pages ? &ppd_tree_block_kernel<128, true> : &ppd_tree_block_kernel<128, false>)
+                                         : (fp8_pages ? &ppd_tree_block_kernel<64, true> : &ppd_tree_block_kernel<64, false>);
+    hipLaunchKernelGGL(kernel, dim3(p.n_items), dim3(kThreads), ring_lds_bytes(head_dim), static_cast<hipStream_t>(stream), p);
+    return (int)hipGetLastError();
 }
 
 int launch_mixed(const KParams& p, int head_dim, int grid, void* stream, bool fp8_pages) {

@@ -15,26 +15,28 @@ constexpr int kTreeThreads = 64 * kTreeWaves;
 constexpr int kSlab = 32;            // keys a wave works at a time: two pages
 constexpr int kTreeStep = kSlab * kTreeWaves;  // split boundaries are multiples of it
 constexpr int kMaxTreeChunk = 8192;  // keys per tree tile at most (its page ids are staged in LDS)
+constexpr int kMaxTreeBlockChunk = 16384;  // the same of a row block
 constexpr int kMaxMaskWords = 16;    // 64-bit words of a row's tree mask at most
 constexpr int kWeighKeys = 256;      // keys of a workgroup that adds up attention weights
 constexpr int kSelectBatch = 512;    // sequences per launch of the select kernel (their lengths are kernel arguments)
 constexpr int kCompactBatch = 256;   // the same for the move (two lists)
 
-// A tile of tree attention: query columns [col0, col0 + ncols) of one sequence and KV head (row-major over the G heads of the
-// group) against keys [kv_begin, kv_end).
+// A tile of tree attention: all `ncols` query columns of one sequence and KV head (row-major over the G heads of the group), at most
+// kTreeCols, against keys [kv_begin, kv_end).
 struct TreeItem {
     int32_t seq, kvh;
     int32_t grow0;             // the sequence's first row in q, out and the masks
-    int32_t col0, ncols;
+    int32_t ncols;
     int32_t L, kv_total;
     int32_t kv_begin, kv_end;
-    int32_t split;             // not 0: the result is a partial at part_off
-    int64_t part_off;          // floats
+    int64_t part_off;          // floats, of this tile's partial; -1 where the tile has all keys and writes `out`
 };
 
 // Columns whose key range was split over nsplit tiles with consecutive partials ([ncols][D] sums, then [ncols] (m, l) pairs).
 struct TreeGroup {
-    int32_t kvh, grow0, col0, ncols;
+    int32_t kvh;
+    int32_t grow0;             // of the sequence
+    int32_t col0, ncols;
     int32_t nsplit, unused;
     int64_t part_off, part_stride;
 };
@@ -46,11 +48,12 @@ struct WeighItem {
 };
 
 struct TreePlan {
-    std::vector<TreeItem> items;
+    std::vector<TreeItem> items;           // tiles of sequences with at most kTreeCols query columns
+    std::vector<ppd_work_item> blocks;     // row blocks of the others
     std::vector<TreeGroup> groups;
     std::vector<WeighItem> weighs;
     int64_t partial_floats = 0;
-    int32_t rows = 0;
+    int32_t rows = 0, join_cols = 0;
 };
 
 // Builds the tile list of a tree or weighted attention call, whose lengths the caller has checked; false if it has more than kMaxTiles tiles.
@@ -76,8 +79,16 @@ struct TreeParams {
     int32_t max_pages;
     int32_t Hq, Hkv, G;
     int32_t n_items, n_groups, n_weighs;
+    int32_t join_cols;         // most columns of a group
     float scale_log2e;         // softmax scale * log2(e), times the K scale of FP8 pages
     float v_scale;
+};
+
+// Arguments of the row-block kernel: those of the mixed kernel, and what a tree adds.
+struct TreeBlockParams : KParams {
+    const uint64_t* mask;
+    float* stats;
+    int32_t mask_words;
 };
 
 struct SelectParams {
@@ -105,6 +116,8 @@ struct CompactParams {
 
 // Launchers; stream is a hipStream_t, the result a hipError_t.
 int launch_tree(const TreeParams& p, int head_dim, bool fp8_pages, void* stream);
+int launch_tree_blocks(const TreeBlockParams& p, int head_dim, bool fp8_pages, void* stream);
+int launch_tree_join(const TreeParams& p, int head_dim, void* stream);
 int launch_weigh(const TreeParams& p, int head_dim, bool fp8_pages, void* stream);
 int launch_select(const SelectParams& p, void* stream);
 int launch_compact(const CompactParams& p, int head_dim, bool fp8_pages, int layers, void* stream);

@@ -71,8 +71,8 @@ ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, const int32_t* L, const 
     if (!ppd::build_tree_plan(ctx->shape, L, n, B, weighted, ctx->num_cus, &t->plan))
         return fail(ctx, PPD_ERR_RANGE, "the batch has more tiles than one launch takes");
     const ppd::TreePlan& plan = t->plan;
-    const size_t items = bytes_of(plan.items), groups = bytes_of(plan.groups), weighs = bytes_of(plan.weighs);
-    const size_t total = items + groups + weighs, upload = (total + 15) / 16 * 16;
+    const size_t items = bytes_of(plan.items), blocks = bytes_of(plan.blocks), groups = bytes_of(plan.groups), weighs = bytes_of(plan.weighs);
+    const size_t total = items + blocks + groups + weighs, upload = (total + 15) / 16 * 16;
     Staging& sg = t->staging[t->next_slot];
     wait_staging_read(sg);
     t->next_slot = (t->next_slot + 1) % kStagingSlots;
@@ -93,9 +93,10 @@ ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, const int32_t* L, const 
     if (st == PPD_OK && weighted) st = grow_device(ctx, &t->d_stats, &t->d_stats_bytes, (size_t)plan.rows * ctx->shape.num_q_heads * 2 * sizeof(float), hs);
     if (st != PPD_OK) return st;
     char* host = static_cast<char*>(sg.host);
-    std::memcpy(host, plan.items.data(), items);
-    if (groups) std::memcpy(host + items, plan.groups.data(), groups);
-    if (weighs) std::memcpy(host + items + groups, plan.weighs.data(), weighs);
+    if (items) std::memcpy(host, plan.items.data(), items);
+    if (blocks) std::memcpy(host + items, plan.blocks.data(), blocks);
+    if (groups) std::memcpy(host + items + blocks, plan.groups.data(), groups);
+    if (weighs) std::memcpy(host + items + blocks + groups, plan.weighs.data(), weighs);
     std::memset(host + total, 0, upload - total);
     const uint4* src = reinterpret_cast<const uint4*>(host);
     uint4* dst = static_cast<uint4*>(t->d_plan);
@@ -172,8 +173,9 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
     p.page_tables = page_tables;
     p.mask = weighted ? nullptr : mask;
     p.items = reinterpret_cast<const ppd::TreeItem*>(d_plan);
-    p.groups = reinterpret_cast<const ppd::TreeGroup*>(d_plan + bytes_of(plan.items));
-    p.weighs = reinterpret_cast<const ppd::WeighItem*>(d_plan + bytes_of(plan.items) + bytes_of(plan.groups));
+    const char* const d_groups = d_plan + bytes_of(plan.items) + bytes_of(plan.blocks);
+    p.groups = reinterpret_cast<const ppd::TreeGroup*>(d_groups);
+    p.weighs = reinterpret_cast<const ppd::WeighItem*>(d_groups + bytes_of(plan.groups));
     p.partials = static_cast<float*>(t->d_partials);
     p.stats = weighted ? static_cast<float*>(t->d_stats) : nullptr;
     p.weights = weights;
@@ -189,19 +191,53 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
     p.n_items = (int32_t)plan.items.size();
     p.n_groups = (int32_t)plan.groups.size();
     p.n_weighs = (int32_t)plan.weighs.size();
+    p.join_cols = plan.join_cols;
     // Strictly positive, so that a scale of 0 gives 2^(-inf * c) = 0 for keys that are not seen.
     p.scale_log2e = std::max(1e-30f, (float)((double)scale * (double)ctx->k_scale * 1.4426950408889634));
     p.v_scale = ctx->v_scale;
     const int D = ctx->shape.head_dim;
-    int rc = ppd::launch_tree(p, D, ctx->fp8_pages, stream);
-    if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch tree attention");
+    int rc = 0;
+    if (!plan.blocks.empty()) {
+        ppd::TreeBlockParams b;
+        std::memset(&b, 0, sizeof b);
+        b.q = p.q;
+        b.out = p.out;
+        b.pool = static_cast<const uint16_t*>(kv_pages);
+        b.page_tables = page_tables;
+        b.items = reinterpret_cast<const ppd_work_item*>(d_plan + bytes_of(plan.items));
+        b.partials = p.partials;
+        b.counters = ctx->d_counters;
+        b.num_pages = p.num_pages;
+        b.page_stride = p.page_stride;
+        b.n_items = (int32_t)plan.blocks.size();
+        b.max_pages = max_pages;
+        b.Hq = p.Hq;
+        b.Hkv = p.Hkv;
+        b.G = p.G;
+        b.invG = 65536 / p.G + 1;
+        b.scale_log2e = p.scale_log2e;
+        b.v_scale = p.v_scale;
+        b.mask = p.mask;
+        b.stats = p.stats;
+        b.mask_words = mask_words;
+        rc = ppd::launch_tree_blocks(b, D, ctx->fp8_pages, stream);
+        if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch tree row blocks");
+    }
+    if (p.n_items > 0) {
+        rc = ppd::launch_tree(p, D, ctx->fp8_pages, stream);
+        if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch tree attention");
+    }
+    if (p.n_groups > 0) {
+        rc = ppd::launch_tree_join(p, D, stream);
+        if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch join of tree tiles");
+    }
     if (weighted) {
         rc = ppd::launch_weigh(p, D, ctx->fp8_pages, stream);
         if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch weights");
     }
     if (ctx->log_calls)
-        std::fprintf(stderr, "ppd: %s_attention%s B=%d tiles=%d joined groups=%d plan=%s\n", weighted ? "weighted" : "tree", ctx->fp8_pages ? " (FP8 pages)" : "",
-                     (int)B, (int)p.n_items, (int)p.n_groups, reuse ? "reused" : "built");
+        std::fprintf(stderr, "ppd: %s_attention%s B=%d tiles=%d row blocks=%d joined groups=%d plan=%s\n", weighted ? "weighted" : "tree", ctx->fp8_pages ? " (FP8 pages)" : "",
+                     (int)B, (int)p.n_items, (int)plan.blocks.size(), (int)p.n_groups, reuse ? "reused" : "built");
     return PPD_OK;
 }
 

@@ -21,8 +21,6 @@ template <> struct Granule<true> { typedef u32x2 type; };
 __device__ __forceinline__ u32x4 operand(u32x4 g) { return g; }
 __device__ __forceinline__ u32x4 operand(u32x2 g) { return fp8x8_to_bf16x8(g); }
 
-__device__ __forceinline__ bool not_finite(uint32_t bf16_bits) { return (bf16_bits & 0x7F80u) == 0x7F80u; }
-
 // Page ids of the tile's keys, checked, to LDS: an id outside the pool raises the sticky flag and is replaced by page 0.
 __device__ __forceinline__ void stage_pages(const TreeParams& P, int seq, int kv_begin, int kv_total, int count, int* ids) {
     const int32_t* row = P.page_tables + (int64_t)seq * P.max_pages;
@@ -35,30 +33,6 @@ __device__ __forceinline__ void stage_pages(const TreeParams& P, int seq, int kv
         }
         ids[i] = id;
     }
-}
-
-// Which of the 32 keys from `base` on the row may see, a bit each: all cached ones, and of the new ones those in its mask, or,
-// without masks, those up to itself.
-__device__ __forceinline__ uint32_t visible_keys(const TreeParams& P, const TreeItem& it, int jrow, int base) {
-    const int valid = it.kv_total - base, off = base - it.L;  // new token of the first key; above -32 where this is called
-    uint32_t seen;
-    if (P.mask) {
-        const uint64_t* words = P.mask + (int64_t)(it.grow0 + jrow) * P.mask_words;
-        if (off < 0) {
-            const uint32_t cached = -off >= 32 ? ~0u : (1u << -off) - 1u;
-            seen = cached | (-off >= 32 ? 0u : (uint32_t)(words[0] << -off));
-        } else {
-            const int w = off >> 6, b = off & 63;
-            uint64_t v = w < P.mask_words ? words[w] >> b : 0;
-            if (b > 32 && w + 1 < P.mask_words) v |= words[w + 1] << (64 - b);
-            seen = (uint32_t)v;
-        }
-    } else {
-        const int upto = jrow - off + 1;
-        seen = upto >= 32 ? ~0u : upto <= 0 ? 0u : (1u << upto) - 1u;
-    }
-    if (valid < 32) seen &= valid <= 0 ? 0u : (1u << valid) - 1u;
-    return seen;
 }
 
 }  // namespace
@@ -79,9 +53,10 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
     const TreeItem it = P.items[blockIdx.x];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, l32 = lane & 31;
-    const int col = it.col0 + (l32 < it.ncols ? l32 : it.ncols - 1);
+    const int col = l32 < it.ncols ? l32 : it.ncols - 1;
     const int jrow = col / P.G, head = it.kvh * P.G + (col - jrow * P.G);
     const float c = P.scale_log2e;
+    const uint64_t* const words = P.mask ? P.mask + (int64_t)(it.grow0 + jrow) * P.mask_words : nullptr;
 
     const int slabs = (it.kv_end - it.kv_begin + kSlab - 1) / kSlab;
     stage_pages(P, it.seq, it.kv_begin, it.kv_total, slabs * 2, ids);
@@ -146,7 +121,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
         uint32_t seen = ~0u;
         bool strange = false;  // a new token's V that is not finite: not every row may see it
         if (base + kSlab > it.L) {
-            seen = visible_keys(P, it, jrow, base);
+            seen = (uint32_t)visible_keys(words, P.mask_words, jrow, base - it.L, it.kv_total - base);
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (!((seen >> ((i >> 3) * 16 + h * 8 + (i & 7))) & 1u)) sc[i] = NEG_INF;
@@ -158,7 +133,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
                     for (int e = 0; e < 8; ++e) {
                         const int pos = base + p * 16 + h * 8 + e;
                         const uint32_t bits = (e & 1) ? vv[p][db][e >> 1] >> 16 : vv[p][db][e >> 1] & 0xFFFFu;
-                        const bool odd = pos >= it.L && not_finite(bits);
+                        const bool odd = pos >= it.L && not_finite_bf16(bits);
                         strange |= odd && pos < it.kv_total;
                         if (odd || pos >= it.kv_total) vv[p][db][e >> 1] &= (e & 1) ? 0x0000FFFFu : 0xFFFF0000u;
                     }
@@ -215,7 +190,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
                         uint32_t bits;
                         if constexpr (FP8) bits = fp8x4_to_bf16x4(*reinterpret_cast<const uint8_t*>(vt + d * 8))[0] & 0xFFFFu;
                         else bits = *reinterpret_cast<const uint16_t*>(vt + d * 16);
-                        if (((seen >> t) & 1u) && not_finite(bits)) oacc[db][i] += __builtin_bit_cast(float, bits << 16);
+                        if (((seen >> t) & 1u) && not_finite_bf16(bits)) oacc[db][i] += __builtin_bit_cast(float, bits << 16);
                     }
             }
         }
@@ -256,13 +231,13 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
                 if (mw != NEG_INF) o += f * *reinterpret_cast<const f32x4*>(&stage[w][cl * ROW + d]);
             }
             const int cc = c0 + cl;
-            if (it.split) {
+            if (it.part_off >= 0) {
                 float* to = P.partials + it.part_off;
                 *reinterpret_cast<f32x4*>(to + cc * HD + d) = o;
                 if (d == 0) *reinterpret_cast<f32x2*>(to + it.ncols * HD + cc * 2) = f32x2{mm, l};
             } else {
-                const int oc = it.col0 + cc, row = oc / P.G;
-                const int64_t at = (int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (oc - row * P.G);
+                const int row = cc / P.G;
+                const int64_t at = (int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G);
                 const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing gives zeros
                 const f32x4 r = o * (inv * P.v_scale);
                 *reinterpret_cast<u32x2*>(P.out + at * HD + d) = u32x2{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
@@ -272,27 +247,46 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
     }
 }
 
-// Joins the partials of split key ranges, splits in order.
-constexpr int kJoinCols = 8;
+// Joins the partials of split key ranges, splits in order.  Bound by latency: the (m, l) pairs of a workgroup's columns go to LDS all at
+// once, and a lane asks for eight splits' values before it adds the first.  One lane after the other over 32 splits took 24 us.
+constexpr int kJoinPairs = 2048;
 template <int HD>
 __global__ __launch_bounds__(256) void ppd_tree_join_kernel(const TreeParams P) {
+    constexpr int LANES = HD / 4, COLS = 256 / LANES, AT_ONCE = 8;
+    __shared__ f32x2 ml[kJoinPairs];
     const TreeGroup g = P.groups[blockIdx.x];
-    constexpr int LANES = HD / 4;
-    const int col = blockIdx.y * kJoinCols + threadIdx.x / LANES, d = (threadIdx.x % LANES) * 4;
-    if (threadIdx.x >= kJoinCols * LANES || col >= g.ncols) return;
+    const int c0 = blockIdx.y * COLS, cl = threadIdx.x / LANES, col = c0 + cl, d = (threadIdx.x % LANES) * 4;
+    if (c0 >= g.ncols) return;
     const float c = P.scale_log2e;
     const float* base = P.partials + g.part_off;
+    const float* pairs = base + (int64_t)g.ncols * HD;
+    const bool staged = g.nsplit * COLS <= kJoinPairs;
+    if (staged) {
+        for (int i = threadIdx.x; i < g.nsplit * COLS; i += 256) {
+            const int cc = c0 + i % COLS;
+            if (cc < g.ncols) ml[i] = *reinterpret_cast<const f32x2*>(pairs + g.part_stride * (i / COLS) + cc * 2);
+        }
+    }
+    __syncthreads();
+    if (col >= g.ncols) return;
+    auto pair = [&](int j) { return staged ? ml[j * COLS + cl] : *reinterpret_cast<const f32x2*>(pairs + g.part_stride * j + col * 2); };
     float mm = NEG_INF;
-    for (int j = 0; j < g.nsplit; ++j) mm = fmaxf(mm, base[g.part_stride * j + g.ncols * HD + col * 2]);
+    for (int j = 0; j < g.nsplit; ++j) mm = fmaxf(mm, pair(j)[0]);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     float l = 0.f;
-    for (int j = 0; j < g.nsplit; ++j) {
-        const float* p = base + g.part_stride * j;
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(p + g.ncols * HD + col * 2);
-        if (ml[0] == NEG_INF) continue;
-        const float f = fast_exp2((ml[0] - mm) * c);
-        l += f * ml[1];
-        o += f * *reinterpret_cast<const f32x4*>(p + col * HD + d);
+    for (int j0 = 0; j0 < g.nsplit; j0 += AT_ONCE) {
+        f32x4 v[AT_ONCE];
+#pragma unroll
+        for (int t = 0; t < AT_ONCE; ++t) v[t] = *reinterpret_cast<const f32x4*>(base + g.part_stride * (j0 + t < g.nsplit ? j0 + t : j0) + (int64_t)col * HD + d);
+#pragma unroll
+        for (int t = 0; t < AT_ONCE; ++t) {
+            if (j0 + t >= g.nsplit) continue;
+            const f32x2 w = pair(j0 + t);
+            if (w[0] == NEG_INF) continue;
+            const float f = fast_exp2((w[0] - mm) * c);
+            l += f * w[1];
+            o += f * v[t];
+        }
     }
     const int oc = g.col0 + col, row = oc / P.G;
     const int64_t at = (int64_t)(g.grow0 + row) * P.Hq + g.kvh * P.G + (oc - row * P.G);
@@ -382,9 +376,13 @@ __global__ __launch_bounds__(256) void ppd_weigh_kernel(const TreeParams P) {
 int launch_tree(const TreeParams& p, int head_dim, bool fp8_pages, void* stream) {
     hipStream_t hs = static_cast<hipStream_t>(stream);
     PPD_BY_FORM(ppd_tree_kernel, dim3((unsigned)p.n_items), kTreeThreads);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.n_groups == 0) return (int)e;
-    const dim3 grid((unsigned)p.n_groups, (kTreeCols + kJoinCols - 1) / kJoinCols);
+    return (int)hipGetLastError();
+}
+
+int launch_tree_join(const TreeParams& p, int head_dim, void* stream) {
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    const int cols = 256 / (head_dim / 4);  // per workgroup
+    const dim3 grid((unsigned)p.n_groups, (unsigned)((p.join_cols + cols - 1) / cols));
     if (head_dim == 128) hipLaunchKernelGGL(ppd_tree_join_kernel<128>, grid, dim3(256), 0, hs, p);
     else hipLaunchKernelGGL(ppd_tree_join_kernel<64>, grid, dim3(256), 0, hs, p);
     return (int)hipGetLastError();

@@ -5,76 +5,119 @@
 
 namespace ppd {
 
+namespace {
+
+// What a kind of tile costs: `start_keys` is its start and end in keys' time, `slots` how many are resident.
+struct TileKind {
+    int32_t max_chunk, step;
+    double start_keys, join_keys, slots;
+};
+
+// Keys per tile, about: every sequence's range is cut evenly into as many tiles as this needs.  A launch lasts as long as its even
+// share and, where there is more than one round, half of what the longest tile sticks out; with one round as long as that tile.
+// Splitting costs the launch that joins the partials.
+int32_t choose_chunk(const TileKind& kind, const std::vector<std::pair<int32_t, double>>& ranges) {  // keys, and how many tiles have this range
+    int32_t longest = 1;
+    for (const auto& r : ranges) longest = std::max(longest, r.first);
+    int32_t chunk = kind.max_chunk;
+    double best = -1;
+    for (double c = std::min<double>(kind.max_chunk, longest); c >= kind.step; c *= 0.84) {
+        double tiles = 0, sum = 0, most = 0;
+        bool split = false;
+        for (const auto& r : ranges) {
+            const double pieces = (double)((r.first + (int64_t)c - 1) / (int64_t)c);
+            const double cost = r.first / pieces + kind.start_keys;
+            tiles += pieces * r.second;
+            sum += pieces * r.second * cost;
+            most = std::max(most, cost);
+            split |= pieces > 1;
+        }
+        if (tiles > kMaxTiles) break;
+        const double est = (tiles <= kind.slots ? most : sum / kind.slots + 0.5 * most) + (split ? kind.join_keys : 0);
+        if (best < 0 || est < best) {
+            best = est;
+            chunk = (int32_t)c;
+        }
+        if (tiles > 16 * kind.slots) break;
+    }
+    return chunk;
+}
+
+}  // namespace
+
 bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int32_t B, bool weighted, int num_cus, TreePlan* plan) {
     const int G = s.num_q_heads / s.num_kv_heads, Hkv = s.num_kv_heads, D = s.head_dim;
     plan->items.clear();
+    plan->blocks.clear();
     plan->groups.clear();
     plan->weighs.clear();
     plan->partial_floats = 0;
-    // Two workgroups are resident on a compute unit.  A tile costs its keys and a start of about kTileKeys keys' time; the launch
-    // lasts as long as its even share and, for what the last tiles stick out, half a tile.
-    constexpr int kTileKeys = 256;
-    const double slots = 2.0 * num_cus;
-    double keys = 0, fewest = 0;
-    int32_t longest = 1;
+    plan->join_cols = 0;
+    const TileKind narrow = {kMaxTreeChunk, kTreeStep, 256, 256, 2.0 * num_cus};
+    const TileKind wide = {kMaxTreeBlockChunk, kTileTokens, 192, 192, 1.0 * num_cus};
+    const int block_rows = kMfmaCols / G;
+    double fewest = 0;
+    std::vector<std::pair<int32_t, double>> narrow_ranges, wide_ranges;
     for (int i = 0; i < B; ++i) {
-        const int64_t blocks = ((int64_t)n[i] * G + kTreeCols - 1) / kTreeCols;
-        keys += (double)blocks * Hkv * ((double)L[i] + n[i]);
-        fewest += (double)blocks * Hkv * (((double)L[i] + n[i]) / kMaxTreeChunk + 1);
-        longest = std::max(longest, L[i] + n[i]);
+        const bool is_wide = (int64_t)n[i] * G > kTreeCols;
+        const double blocks = is_wide ? (double)((n[i] + (int64_t)block_rows - 1) / block_rows) : 1.0;
+        (is_wide ? wide_ranges : narrow_ranges).push_back({L[i] + n[i], blocks * Hkv});
+        fewest += blocks * Hkv * (((double)L[i] + n[i]) / kMaxTreeChunk + 1);
     }
     if (fewest > kMaxTiles) return false;
-    int32_t chunk = kMaxTreeChunk;
-    double best = -1;
-    for (int32_t c = kMaxTreeChunk; c >= kTreeStep; c /= 2) {
-        double tiles = 0;
-        for (int i = 0; i < B; ++i) {
-            const int64_t total = (int64_t)L[i] + n[i];
-            tiles += (double)(((int64_t)n[i] * G + kTreeCols - 1) / kTreeCols) * Hkv * (double)((total + c - 1) / c);
-        }
-        if (tiles > kMaxTiles) break;
-        const double est = (keys + tiles * kTileKeys) / slots + 0.5 * (std::min(c, longest) + kTileKeys);
-        const double rounds_floor = std::min(c, longest) + kTileKeys;  // no launch is shorter than its longest tile
-        const double cost = std::max(est, rounds_floor);
-        if (best < 0 || cost < best) {
-            best = cost;
-            chunk = c;
-        }
-    }
+    const int32_t narrow_chunk = narrow_ranges.empty() ? 0 : choose_chunk(narrow, narrow_ranges);
+    const int32_t wide_chunk = wide_ranges.empty() ? 0 : choose_chunk(wide, wide_ranges);
     int32_t grow0 = 0;
     for (int i = 0; i < B; ++i) {
         const int32_t total = L[i] + n[i];
-        const int64_t cols = (int64_t)n[i] * G;
-        const int32_t nsplit = (total + chunk - 1) / chunk;
+        const bool is_wide = (int64_t)n[i] * G > kTreeCols;
+        const TileKind& kind = is_wide ? wide : narrow;
+        const int32_t chunk = is_wide ? wide_chunk : narrow_chunk;
+        const int32_t pieces = (total + chunk - 1) / chunk;
+        const int32_t piece = std::min(kind.max_chunk, ((total + pieces - 1) / pieces + kind.step - 1) / kind.step * kind.step);
+        const int32_t nsplit = (total + piece - 1) / piece;
+        const int32_t blocks = is_wide ? (n[i] + block_rows - 1) / block_rows : 1, rows = (n[i] + blocks - 1) / blocks;
         for (int h = 0; h < Hkv; ++h) {
-            for (int64_t c0 = 0; c0 < cols; c0 += kTreeCols) {
-                const int32_t nc = (int32_t)std::min<int64_t>(kTreeCols, cols - c0);
-                const int64_t stride = (int64_t)nc * (D + 2);
-                if (nsplit > 1) plan->groups.push_back({h, grow0, (int32_t)c0, nc, nsplit, 0, plan->partial_floats, stride});
+            for (int32_t row0 = 0; row0 < n[i]; row0 += rows) {
+                const int32_t nrows = std::min(rows, n[i] - row0), cols = nrows * G;
+                const int64_t stride = (int64_t)cols * (D + 2);
+                if (nsplit > 1) {
+                    plan->groups.push_back({h, grow0, row0 * G, cols, nsplit, 0, plan->partial_floats, stride});
+                    plan->join_cols = std::max(plan->join_cols, cols);
+                }
                 for (int32_t p = 0; p < nsplit; ++p) {
-                    TreeItem it{};
-                    it.seq = i;
-                    it.kvh = h;
-                    it.grow0 = grow0;
-                    it.col0 = (int32_t)c0;
-                    it.ncols = nc;
-                    it.L = L[i];
-                    it.kv_total = total;
-                    it.kv_begin = p * chunk;
-                    it.kv_end = std::min(total, (p + 1) * chunk);
-                    it.split = nsplit > 1;
-                    it.part_off = plan->partial_floats + p * stride;
-                    plan->items.push_back(it);
+                    const int32_t begin = p * piece, end = std::min(total, (p + 1) * piece);
+                    const int64_t part = nsplit > 1 ? plan->partial_floats + p * stride : -1;
+                    if (is_wide) {
+                        ppd_work_item it{};
+                        it.kind = 1;
+                        it.seq = i;
+                        it.kvh = h;
+                        it.row0 = row0;
+                        it.nrows = nrows;
+                        it.grow0 = grow0 + row0;
+                        it.L = L[i];
+                        it.kv_total = total;
+                        it.kv_begin = begin;
+                        it.kv_end = end;
+                        it.group = nsplit > 1 ? (int32_t)plan->groups.size() - 1 : -1;
+                        it.part_off = part;
+                        plan->blocks.push_back(it);
+                    } else {
+                        plan->items.push_back({i, h, grow0, cols, L[i], total, begin, end, part});
+                    }
                 }
                 if (nsplit > 1) plan->partial_floats += stride * nsplit;
             }
             if (weighted)
-                for (int32_t t = 0; t < total; t += kWeighKeys) plan->weighs.push_back({i, h, grow0, (int32_t)cols, L[i], total, t, 0});
+                for (int32_t t = 0; t < total; t += kWeighKeys) plan->weighs.push_back({i, h, grow0, n[i] * G, L[i], total, t, 0});
         }
         grow0 += n[i];
     }
     plan->rows = grow0;
-    std::stable_sort(plan->items.begin(), plan->items.end(), [](const TreeItem& a, const TreeItem& b) { return a.kv_end - a.kv_begin > b.kv_end - b.kv_begin; });
+    auto longest_first = [](const auto& a, const auto& b) { return a.kv_end - a.kv_begin > b.kv_end - b.kv_begin; };
+    std::stable_sort(plan->items.begin(), plan->items.end(), longest_first);
+    std::stable_sort(plan->blocks.begin(), plan->blocks.end(), longest_first);
     return true;
 }
 

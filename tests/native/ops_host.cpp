@@ -25,6 +25,7 @@ std::function<void()> sim_bind(const void* f, void** args) {
 }
 
 static std::vector<ppd::TreeParams> g_tree, g_weigh;
+static std::vector<ppd::TreeBlockParams> g_blocks;
 static std::vector<ppd::SelectParams> g_select;
 static std::vector<ppd::CompactParams> g_compact;
 
@@ -38,6 +39,8 @@ int launch_merge(const MergeParams&, void*) { return 0; }
 int launch_kv_append(const uint16_t*, const uint16_t*, void*, const int64_t*, int64_t, int, int, int64_t, int, int64_t, uint32_t*,
                      void*, bool, float, float) { return 0; }
 int launch_tree(const TreeParams& p, int, bool, void*) { g_tree.push_back(p); return 0; }
+int launch_tree_blocks(const TreeBlockParams& p, int, bool, void*) { g_blocks.push_back(p); return 0; }
+int launch_tree_join(const TreeParams&, int, void*) { return 0; }
 int launch_weigh(const TreeParams& p, int, bool, void*) { g_weigh.push_back(p); return 0; }
 int launch_select(const SelectParams& p, void*) { g_select.push_back(p); return 0; }
 int launch_compact(const CompactParams& p, int, bool, int, void*) { g_compact.push_back(p); return 0; }
@@ -51,6 +54,9 @@ int launch_compact(const CompactParams& p, int, bool, int, void*) { g_compact.pu
             std::_Exit(1);                                            \
         }                                                             \
     } while (0)
+
+// calls of the wide kind here have row blocks, so every call launches them once
+static size_t attentions() { return g_blocks.size(); }
 
 alignas(16) static char device[64];
 static const int32_t* const tables = reinterpret_cast<const int32_t*>(device);
@@ -74,7 +80,7 @@ static void refusals() {
         return ppd_tree_attention(ctx, q, pool, pt, max_pages, mask, words, l, m, B, scale, out, nullptr);
     };
     CHECK(tree(device, device, tables, 7, masks, 1, L, n, 2, 1.f, device) == PPD_OK);
-    CHECK(g_tree.size() == 1);
+    CHECK(attentions() == 1);
     CHECK(tree(device, device, tables, 7, masks, 1, L, n, 0, 1.f, device) == PPD_OK);
     CHECK(ppd_tree_attention(nullptr, device, device, tables, 7, masks, 1, L, n, 2, 1.f, device, nullptr) == PPD_ERR_NULL);
     CHECK(tree(nullptr, device, tables, 7, masks, 1, L, n, 2, 1.f, device) == PPD_ERR_NULL);
@@ -102,7 +108,7 @@ static void refusals() {
     CHECK(tree(device, device, tables, 7, masks, 2, L, more, 2, 1.f, device) == PPD_OK);
     CHECK(tree(device, device, tables, 7, masks, 1, below, n, 2, 1.f, device) == PPD_ERR_RANGE);
     CHECK(tree(device, device, tables, INT32_MAX, masks, 1, far, n, 2, 1.f, device) == PPD_ERR_RANGE);
-    CHECK(std::string(ppd_last_error(ctx)).size() > 0 && g_tree.size() == 2);
+    CHECK(std::string(ppd_last_error(ctx)).size() > 0 && attentions() == 2);
 
     auto weighted = [&](float* w, int64_t stride) { return ppd_weighted_attention(ctx, device, device, tables, 7, L, n, 2, 1.f, device, w, stride, nullptr); };
     CHECK(weighted(floats, 105) == PPD_OK && g_weigh.size() == 1);
@@ -192,7 +198,7 @@ static void refusals() {
 // has more page ids than its LDS, and every key is weighed once.
 static void plans() {
     std::mt19937 rng(3);
-    int split = 0, whole = 0;
+    int split = 0, whole = 0, blocks = 0;
     for (int trial = 0; trial < 200; ++trial) {
         const int hkv = 1 + rng() % 8, G = 1 + rng() % 8, dim = rng() % 2 ? 128 : 64;
         const ppd_shape s = {hkv * G, hkv, dim, 16, 1 << 20};
@@ -206,22 +212,34 @@ static void plans() {
         for (size_t i = 0; i < L.size(); ++i) grow0[i + 1] = grow0[i] + n[i];
         CHECK(p.rows == grow0.back());
         std::map<std::tuple<int, int, int>, std::map<int, int>> ranges;  // (sequence, head, first column) -> begin -> end
+        std::map<std::tuple<int, int, int>, int> widths;
         std::set<int64_t> offsets;
-        for (const auto& it : p.items) {
-            CHECK(it.seq >= 0 && it.seq < (int)L.size() && it.kvh >= 0 && it.kvh < hkv);
-            CHECK(it.L == L[it.seq] && it.kv_total == L[it.seq] + n[it.seq] && it.grow0 == grow0[it.seq]);
-            CHECK(it.ncols >= 1 && it.ncols <= ppd::kTreeCols && it.col0 >= 0 && it.col0 + it.ncols <= n[it.seq] * G);
-            CHECK(it.kv_begin >= 0 && it.kv_begin % ppd::kSlab == 0 && it.kv_begin < it.kv_end && it.kv_end <= it.kv_total);
-            CHECK((it.kv_end - it.kv_begin + ppd::kSlab - 1) / ppd::kSlab * 2 <= ppd::kMaxTreeChunk / 16);
-            CHECK(ranges[std::make_tuple(it.seq, it.kvh, it.col0)].emplace(it.kv_begin, it.kv_end).second);
-            if (it.split) {
-                CHECK(it.part_off >= 0 && it.part_off + (int64_t)it.ncols * (dim + 2) <= p.partial_floats && offsets.insert(it.part_off).second);
-                CHECK(it.part_off % 2 == 0);
+        auto tile = [&](int seq, int kvh, int col0, int ncols, int Li, int kv_total, int begin, int end, int64_t part_off) {
+            CHECK(seq >= 0 && seq < (int)L.size() && kvh >= 0 && kvh < hkv);
+            CHECK(Li == L[seq] && kv_total == L[seq] + n[seq]);
+            CHECK(ncols >= 1 && col0 >= 0 && col0 + ncols <= n[seq] * G);
+            CHECK(begin >= 0 && begin < end && end <= kv_total);
+            CHECK(ranges[std::make_tuple(seq, kvh, col0)].emplace(begin, end).second);
+            widths[std::make_tuple(seq, kvh, col0)] = ncols;
+            if (part_off >= 0) {
+                CHECK(part_off + (int64_t)ncols * (dim + 2) <= p.partial_floats && offsets.insert(part_off).second && part_off % 2 == 0);
                 ++split;
             } else {
-                CHECK(it.kv_begin == 0 && it.kv_end == it.kv_total);
+                CHECK(begin == 0 && end == kv_total);
                 ++whole;
             }
+        };
+        for (const auto& it : p.items) {
+            tile(it.seq, it.kvh, 0, it.ncols, it.L, it.kv_total, it.kv_begin, it.kv_end, it.part_off);
+            CHECK(it.grow0 == grow0[it.seq] && it.ncols <= ppd::kTreeCols && it.ncols == n[it.seq] * G && it.kv_begin % ppd::kSlab == 0);
+            CHECK((it.kv_end - it.kv_begin + ppd::kSlab - 1) / ppd::kSlab * 2 <= ppd::kMaxTreeChunk / 16);
+        }
+        for (const auto& it : p.blocks) {
+            tile(it.seq, it.kvh, it.row0 * G, it.nrows * G, it.L, it.kv_total, it.kv_begin, it.kv_end, it.part_off);
+            CHECK(it.grow0 == grow0[it.seq] + it.row0 && it.nrows * G <= ppd::kMfmaCols && it.kv_begin % ppd::kTileTokens == 0);
+            // the last id's place in LDS is the flag's
+            CHECK((it.kv_end - it.kv_begin + ppd::kTileTokens - 1) / ppd::kTileTokens * 4 < ppd::kMaxMfmaChunk / 16 - 1);
+            ++blocks;
         }
         int64_t columns = 0;
         for (const auto& r : ranges) {
@@ -231,10 +249,10 @@ static void plans() {
                 at = e;
             }
             CHECK(at == L[std::get<0>(r.first)] + n[std::get<0>(r.first)]);
+            columns += widths[r.first];
         }
-        for (const auto& it : p.items)
-            if (it.kv_begin == 0) columns += it.ncols;
         CHECK(columns == (int64_t)p.rows * G * hkv);
+        for (const auto& g : p.groups) CHECK(g.ncols <= p.join_cols);
         std::set<int64_t> joined;
         for (const auto& g : p.groups)
             for (int j = 0; j < g.nsplit; ++j) CHECK(offsets.count(g.part_off + j * g.part_stride) && joined.insert(g.part_off + j * g.part_stride).second);
@@ -250,7 +268,7 @@ static void plans() {
         for (size_t i = 0; i < L.size(); ++i) keys += (int64_t)hkv * (L[i] + n[i]);
         CHECK(weighed == (weighted ? keys : 0));
     }
-    CHECK(split > 1000 && whole > 1000);
+    CHECK(split > 1000 && whole > 1000 && blocks > 1000 && blocks < split + whole - 1000);
     // a batch beyond what one launch takes is refused, not built
     const ppd_shape s = {8192, 1024, 128, 16, 1 << 16};
     std::vector<int32_t> L(4096, 100), n(4096, 64);
@@ -297,7 +315,7 @@ static void streams() {
     auto tree = [&](hipStream_t s) { return ppd_tree_attention(ctx, device, device, tables, 80, masks, 1, L, n, 2, 1.f, device, s); };
     auto weighted = [&](hipStream_t s) { return ppd_weighted_attention(ctx, device, device, tables, 64, L, n, 2, 1.f, device, floats, 1005, s); };
     sim.capturing = true;
-    CHECK(tree(a) == PPD_ERR_RANGE && g_tree.empty());
+    CHECK(tree(a) == PPD_ERR_RANGE && attentions() == 0);
     sim.capturing = false;
     CHECK(tree(a) == PPD_OK && a->waiting() == 1);
     CHECK(tree(a) == PPD_OK && a->waiting() == 1);  // the plan is there
@@ -309,14 +327,16 @@ static void streams() {
     CHECK(g_weigh.size() == 1 && g_weigh[0].n_weighs == 8 * (4 + 1));
     b->run();
     const ppd::TreeParams& p = g_weigh[0];
+    CHECK(p.n_items > 0 && g_blocks.back().n_items > 0);
     for (int i = 0; i < p.n_items; ++i) CHECK(p.items[i].L == L[p.items[i].seq]);
+    for (int i = 0; i < g_blocks.back().n_items; ++i) CHECK(g_blocks.back().items[i].L == L[g_blocks.back().items[i].seq]);
     for (int i = 0; i < p.n_weighs; ++i) CHECK(p.weighs[i].L == L[p.weighs[i].seq]);
     L[0] = 1001;
     sim.launch_status = hipErrorLaunchFailure;
     CHECK(tree(b) == PPD_ERR_HIP);
     sim.launch_status = hipSuccess;
-    const size_t before = g_tree.size();
-    CHECK(tree(b) == PPD_OK && b->waiting() == 1 && g_tree.size() == before + 1);
+    const size_t before = attentions();
+    CHECK(tree(b) == PPD_OK && b->waiting() == 1 && attentions() == before + 1);
     // mixed attention on another stream waits as well: both share the words that count an upload's workgroups
     CHECK(ppd_mixed_attention(ctx, device, device, tables, 64, L, n, 2, 1.f, device, a) == PPD_OK && b->waiting() == 0);
     a->run();
