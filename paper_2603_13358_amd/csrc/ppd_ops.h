@@ -30,6 +30,7 @@ struct TreeItem {
     int32_t L, kv_total;
     int32_t kv_begin, kv_end;
     int64_t part_off;          // floats, of this tile's partial; -1 where the tile has all keys and writes `out`
+    int64_t score_off;         // floats, where the scores of the sequence and head go; -1: they are not kept
 };
 
 // Columns whose key range was split over nsplit tiles with consecutive partials ([ncols][D] sums, then [ncols] (m, l) pairs).
@@ -45,19 +46,26 @@ struct TreeGroup {
 struct WeighItem {
     int32_t seq, kvh, grow0, cols;
     int32_t L, kv_total, kv_begin, unused;
+    int64_t score_off;         // floats: scores [column][score_stride], or -1: they are computed again
 };
+
+// Keys of a row of kept scores: whole slabs, whose every key is written.
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+constexpr int32_t score_stride(int32_t kv_total) { return (kv_total + kSlab - 1) / kSlab * kSlab; }
 
 struct TreePlan {
     std::vector<TreeItem> items;           // tiles of sequences with at most kTreeCols query columns
     std::vector<ppd_work_item> blocks;     // row blocks of the others
     std::vector<TreeGroup> groups;
-    std::vector<WeighItem> weighs;
-    int64_t partial_floats = 0;
+    std::vector<WeighItem> weighs, score_weighs;  // from K, from kept scores
+    int64_t partial_floats = 0, score_floats = 0;
     int32_t rows = 0, join_cols = 0;
 };
 
 // Builds the tile list of a tree or weighted attention call, whose lengths the caller has checked; false if it has more than kMaxTiles tiles.
-bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int32_t B, bool weighted, int num_cus, TreePlan* plan);
+bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int32_t B, bool weighted, int kv_elem_bytes, int num_cus, TreePlan* plan);
 
 struct TreeParams {
     const uint16_t* q;
@@ -67,8 +75,9 @@ struct TreeParams {
     const uint64_t* mask;      // [rows][mask_words], or NULL: row j sees the new tokens up to itself
     const TreeItem* items;
     const TreeGroup* groups;
-    const WeighItem* weighs;
+    const WeighItem *weighs, *score_weighs;
     float* partials;
+    float* scores;
     float* stats;              // weighted attention: per row and query head the softmax reference and one over the sum
     float* weights;            // [B][Hkv][weight_stride]
     int64_t weight_stride;
@@ -78,7 +87,7 @@ struct TreeParams {
     int32_t mask_words;
     int32_t max_pages;
     int32_t Hq, Hkv, G;
-    int32_t n_items, n_groups, n_weighs;
+    int32_t n_items, n_groups, n_weighs, n_score_weighs;
     int32_t join_cols;         // most columns of a group
     float scale_log2e;         // softmax scale * log2(e), times the K scale of FP8 pages
     float v_scale;

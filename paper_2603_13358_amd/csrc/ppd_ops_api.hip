@@ -25,8 +25,10 @@ struct TreeState {
     size_t d_partials_bytes = 0;
     void* d_stats = nullptr;
     size_t d_stats_bytes = 0;
+    void* d_scores = nullptr;
+    size_t d_scores_bytes = 0;
     std::vector<int32_t> L, n;
-    bool weighted = false, on_device = false;
+    bool weighted = false, fp8_pages = false, on_device = false;
     ppd::TreePlan plan;
 };
 
@@ -39,6 +41,7 @@ void free_tree_state(void* p) {
     if (t->d_plan) (void)hipFree(t->d_plan);
     if (t->d_partials) (void)hipFree(t->d_partials);
     if (t->d_stats) (void)hipFree(t->d_stats);
+    if (t->d_scores) (void)hipFree(t->d_scores);
     delete t;
 }
 
@@ -68,11 +71,12 @@ size_t bytes_of(const std::vector<T>& v) { return v.size() * sizeof(T); }
 // Builds the plan, grows the workspace and enqueues the upload.
 ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, const int32_t* L, const int32_t* n, int32_t B, bool weighted, hipStream_t hs) {
     t->on_device = false;
-    if (!ppd::build_tree_plan(ctx->shape, L, n, B, weighted, ctx->num_cus, &t->plan))
+    if (!ppd::build_tree_plan(ctx->shape, L, n, B, weighted, ctx->fp8_pages ? 1 : 2, ctx->num_cus, &t->plan))
         return fail(ctx, PPD_ERR_RANGE, "the batch has more tiles than one launch takes");
     const ppd::TreePlan& plan = t->plan;
-    const size_t items = bytes_of(plan.items), blocks = bytes_of(plan.blocks), groups = bytes_of(plan.groups), weighs = bytes_of(plan.weighs);
-    const size_t total = items + blocks + groups + weighs, upload = (total + 15) / 16 * 16;
+    const size_t items = bytes_of(plan.items), blocks = bytes_of(plan.blocks), groups = bytes_of(plan.groups);
+    const size_t weighs = bytes_of(plan.weighs), score_weighs = bytes_of(plan.score_weighs);
+    const size_t total = items + blocks + groups + weighs + score_weighs, upload = (total + 15) / 16 * 16;
     Staging& sg = t->staging[t->next_slot];
     wait_staging_read(sg);
     t->next_slot = (t->next_slot + 1) % kStagingSlots;
@@ -91,12 +95,14 @@ ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, const int32_t* L, const 
     ppd_status st = grow_device(ctx, &t->d_plan, &t->d_plan_bytes, upload, hs);
     if (st == PPD_OK) st = grow_device(ctx, &t->d_partials, &t->d_partials_bytes, (size_t)plan.partial_floats * sizeof(float), hs);
     if (st == PPD_OK && weighted) st = grow_device(ctx, &t->d_stats, &t->d_stats_bytes, (size_t)plan.rows * ctx->shape.num_q_heads * 2 * sizeof(float), hs);
+    if (st == PPD_OK) st = grow_device(ctx, &t->d_scores, &t->d_scores_bytes, (size_t)plan.score_floats * sizeof(float), hs);
     if (st != PPD_OK) return st;
     char* host = static_cast<char*>(sg.host);
     if (items) std::memcpy(host, plan.items.data(), items);
     if (blocks) std::memcpy(host + items, plan.blocks.data(), blocks);
     if (groups) std::memcpy(host + items + blocks, plan.groups.data(), groups);
     if (weighs) std::memcpy(host + items + blocks + groups, plan.weighs.data(), weighs);
+    if (score_weighs) std::memcpy(host + items + blocks + groups + weighs, plan.score_weighs.data(), score_weighs);
     std::memset(host + total, 0, upload - total);
     const uint4* src = reinterpret_cast<const uint4*>(host);
     uint4* dst = static_cast<uint4*>(t->d_plan);
@@ -112,6 +118,7 @@ ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, const int32_t* L, const 
     t->L.assign(L, L + B);
     t->n.assign(n, n + B);
     t->weighted = weighted;
+    t->fp8_pages = ctx->fp8_pages;
     t->on_device = true;
     return PPD_OK;
 }
@@ -151,7 +158,7 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
     PPD_HIP(ctx, hipStreamIsCapturing(hs, &capturing));
     const bool in_capture = capturing != hipStreamCaptureStatusNone;
     if (!in_capture && ctx->have_plan_stream && ctx->plan_stream != hs) PPD_HIP(ctx, hipStreamSynchronize(ctx->plan_stream));
-    const bool reuse = t->on_device && t->weighted == weighted && (int32_t)t->L.size() == B &&
+    const bool reuse = t->on_device && t->weighted == weighted && t->fp8_pages == ctx->fp8_pages && (int32_t)t->L.size() == B &&
                        std::memcmp(t->L.data(), L, sizeof(int32_t) * B) == 0 && std::memcmp(t->n.data(), n, sizeof(int32_t) * B) == 0;
     if (!reuse) {
         if (in_capture)
@@ -176,6 +183,8 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
     const char* const d_groups = d_plan + bytes_of(plan.items) + bytes_of(plan.blocks);
     p.groups = reinterpret_cast<const ppd::TreeGroup*>(d_groups);
     p.weighs = reinterpret_cast<const ppd::WeighItem*>(d_groups + bytes_of(plan.groups));
+    p.score_weighs = p.weighs + plan.weighs.size();
+    p.scores = static_cast<float*>(t->d_scores);
     p.partials = static_cast<float*>(t->d_partials);
     p.stats = weighted ? static_cast<float*>(t->d_stats) : nullptr;
     p.weights = weights;
@@ -191,6 +200,7 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
     p.n_items = (int32_t)plan.items.size();
     p.n_groups = (int32_t)plan.groups.size();
     p.n_weighs = (int32_t)plan.weighs.size();
+    p.n_score_weighs = (int32_t)plan.score_weighs.size();
     p.join_cols = plan.join_cols;
     // Strictly positive, so that a scale of 0 gives 2^(-inf * c) = 0 for keys that are not seen.
     p.scale_log2e = std::max(1e-30f, (float)((double)scale * (double)ctx->k_scale * 1.4426950408889634));

@@ -58,6 +58,8 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
     const float c = P.scale_log2e;
     const uint64_t* const words = P.mask ? P.mask + (int64_t)(it.grow0 + jrow) * P.mask_words : nullptr;
 
+    float* const scores = it.score_off >= 0 ? P.scores + it.score_off + (int64_t)col * score_stride(it.kv_total) + h * 8 : nullptr;
+
     const int slabs = (it.kv_end - it.kv_begin + kSlab - 1) / kSlab;
     stage_pages(P, it.seq, it.kv_begin, it.kv_total, slabs * 2, ids);
     bf16x8 qreg[KS];
@@ -137,6 +139,11 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
                         strange |= odd && pos < it.kv_total;
                         if (odd || pos >= it.kv_total) vv[p][db][e >> 1] &= (e & 1) ? 0x0000FFFFu : 0xFFFF0000u;
                     }
+        }
+        if (scores && l32 < it.ncols) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4*>(scores + base + (i >> 1) * 16 + (i & 1) * 4) = f32x4{sc[4 * i], sc[4 * i + 1], sc[4 * i + 2], sc[4 * i + 3]};
         }
         // The exponentials are taken against the running reference as it is; only where a lane's sum of 16 of them is above
         // 2^kLazyRescale (or not a number: no reference yet) is the maximum looked for and everything rescaled.
@@ -296,20 +303,33 @@ __global__ __launch_bounds__(256) void ppd_tree_join_kernel(const TreeParams P) 
     if (P.stats && d == 0) *reinterpret_cast<f32x2*>(P.stats + at * 2) = f32x2{mm == NEG_INF ? 0.f : mm, inv};
 }
 
-// Adds up the weights: S = Q K^T with the keys as columns, so that a lane owns a key and the sum over the queries runs over its own
-// registers.  A wave holds K of 64 keys, read once, and goes over the sequence's query columns, 32 at a time.  The reference
-// and one over the sum of every row come from the attention before.
+// Adds up the weights of sequences with many query columns: S = Q K^T with the keys as columns, so that a lane owns a key and the sum
+// over the queries runs over its own registers.  A wave holds K of 64 keys, read once, and goes over the sequence's query columns, 32 at
+// a time, the next ones' Q on its way meanwhile.  The reference and one over the sum of every row come from the attention before.
+constexpr int kWeighCols = 256;  // columns whose references are in LDS at a time
 template <int HD, bool FP8>
-__global__ __launch_bounds__(256) void ppd_weigh_kernel(const TreeParams P) {
+__global__ __launch_bounds__(256, 2) void ppd_weigh_kernel(const TreeParams P) {
     typedef typename Granule<FP8>::type Raw;
     constexpr int EB = FP8 ? 1 : 2, KS = HD / 16, SLABS = kWeighKeys / 4 / kSlab;
     __shared__ int ids[kWeighKeys / kPage];
-    __shared__ f32x2 ml[2][32];
-    __shared__ int rows[2][32];
+    __shared__ f32x2 ml[kWeighCols];
+    __shared__ int rows[kWeighCols];
     const WeighItem it = P.weighs[blockIdx.x];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, l32 = lane & 31;
+    auto q_at = [&](int cc) {  // element offset of a column's query
+        cc = cc < it.cols ? cc : it.cols - 1;
+        const int row = cc / P.G;
+        return ((int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G));
+    };
+    u32x4 qnext[KS];
+    auto load_q = [&](int c0) {
+        const uint16_t* qp = P.q + q_at(c0 + l32) * HD + h * 8;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qnext[ks] = *reinterpret_cast<const u32x4*>(qp + ks * 16);
+    };
     stage_pages(P, it.seq, it.kv_begin, it.kv_total, kWeighKeys / kPage, ids);
+    load_q(0);
     __syncthreads();
     const char* const pool = static_cast<const char*>(P.pool) + ((int64_t)it.kvh * (kPage * HD) + (h * 16 + (l32 & 15)) * 8) * EB;
     u32x4 kreg[SLABS][KS];
@@ -325,32 +345,42 @@ __global__ __launch_bounds__(256) void ppd_weigh_kernel(const TreeParams P) {
     for (int s = 0; s < SLABS; ++s) sum[s] = 0.f;
     const int base = it.kv_begin + wave * (SLABS * kSlab);
     const bool tail = base + SLABS * kSlab > it.L;  // new tokens among the wave's keys: not every row sees them
-    for (int c0 = 0, at = 0; c0 < it.cols; c0 += 32, at ^= 1) {
-        if (tid < 32) {
-            const int cc = c0 + tid, row = cc / P.G;
-            const bool live = cc < it.cols;
-            ml[at][tid] = live ? *reinterpret_cast<const f32x2*>(P.stats + ((int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G)) * 2) : f32x2{0.f, 0.f};
-            rows[at][tid] = row;
+    for (int b0 = 0; b0 < it.cols; b0 += kWeighCols) {
+        const int b1 = b0 + kWeighCols < it.cols ? b0 + kWeighCols : it.cols;
+        if (b0 > 0) __syncthreads();
+        {
+            const int cc = b0 + tid;  // columns past the end count nothing
+            ml[tid] = cc < it.cols ? *reinterpret_cast<const f32x2*>(P.stats + q_at(cc) * 2) : f32x2{0.f, 0.f};
+            rows[tid] = cc < it.cols ? cc / P.G : -1;
         }
-        __syncthreads();  // the buffer written two rounds on is read by nobody any more
-        const int cc = c0 + l32 < it.cols ? c0 + l32 : it.cols - 1, row = cc / P.G;
-        const uint16_t* qp = P.q + ((int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G)) * HD + h * 8;
-        bf16x8 qreg[KS];
+        __syncthreads();
+        for (int c0 = b0; c0 < b1; c0 += 32) {
+            bf16x8 qreg[KS];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) qreg[ks] = as_bf16x8(*reinterpret_cast<const u32x4*>(qp + ks * 16));
+            for (int ks = 0; ks < KS; ++ks) qreg[ks] = as_bf16x8(qnext[ks]);
+            f32x16 sc[SLABS];
 #pragma unroll
-        for (int s = 0; s < SLABS; ++s) {
-            f32x16 sc;
+            for (int s = 0; s < SLABS; ++s)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+                for (int i = 0; i < 16; ++i) sc[s][i] = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qreg[ks], as_bf16x8(kreg[s][ks]), sc, 0, 0, 0);
-            const int key = base + s * kSlab + l32;
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int s = 0; s < SLABS; ++s) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qreg[ks], as_bf16x8(kreg[s][ks]), sc[s], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (c0 + 32 < it.cols) load_q(c0 + 32);
+            __builtin_amdgcn_sched_barrier(0);
+            const bool whole = !tail && c0 + 32 <= it.cols;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int r = (i & 3) + 8 * (i >> 2) + 4 * h;
-                const f32x2 w = ml[at][r];
-                if (c0 + r < it.cols && (!tail || key <= it.L + rows[at][r])) sum[s] += fast_exp2((sc[i] - w[0]) * c) * w[1];
+                const int r = c0 - b0 + (i & 3) + 8 * (i >> 2) + 4 * h;
+                const f32x2 w = ml[r];
+                const float mc = w[0] * c;
+#pragma unroll
+                for (int s = 0; s < SLABS; ++s) {
+                    const float p = fast_exp2(__builtin_fmaf(sc[s][i], c, -mc)) * w[1];
+                    if (whole || (rows[r] >= 0 && base + s * kSlab + l32 <= it.L + rows[r])) sum[s] += p;
+                }
             }
         }
     }
@@ -363,6 +393,26 @@ __global__ __launch_bounds__(256) void ppd_weigh_kernel(const TreeParams P) {
             *to = key < it.L ? *to + total : total;
         }
     }
+}
+
+// Adds up the weights of sequences with few query columns, whose scores ppd_tree_kernel has left in the workspace: a thread to a key.
+// The scores of G columns are 8 G bytes a key, written and read, where K again would be 2 D: 64 decodes of 1K-8K keys (32 query
+// heads, D = 128) READ AGAIN us that way.
+__global__ __launch_bounds__(kWeighKeys) void ppd_weigh_scores_kernel(const TreeParams P) {
+    const WeighItem it = P.score_weighs[blockIdx.x];
+    const int key = it.kv_begin + (int)threadIdx.x;
+    if (key >= it.kv_total) return;
+    const float c = P.scale_log2e;
+    const float* scores = P.scores + it.score_off + key;
+    const int stride = score_stride(it.kv_total);
+    float sum = 0.f;
+    for (int cc = 0; cc < it.cols; ++cc) {
+        const int row = cc / P.G;
+        const f32x2 w = *reinterpret_cast<const f32x2*>(P.stats + ((int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G)) * 2);
+        sum += fast_exp2(__builtin_fmaf(scores[(int64_t)cc * stride], c, -(w[0] * c))) * w[1];
+    }
+    float* to = P.weights + ((int64_t)it.seq * P.Hkv + it.kvh) * P.weight_stride + key;
+    *to = key < it.L ? *to + sum : sum;
 }
 
 #define PPD_BY_FORM(KERNEL, GRID, THREADS)                                                                                        \
@@ -390,7 +440,8 @@ int launch_tree_join(const TreeParams& p, int head_dim, void* stream) {
 
 int launch_weigh(const TreeParams& p, int head_dim, bool fp8_pages, void* stream) {
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    PPD_BY_FORM(ppd_weigh_kernel, dim3((unsigned)p.n_weighs), 256);
+    if (p.n_score_weighs > 0) hipLaunchKernelGGL(ppd_weigh_scores_kernel, dim3((unsigned)p.n_score_weighs), dim3(kWeighKeys), 0, hs, p);
+    if (p.n_weighs > 0) PPD_BY_FORM(ppd_weigh_kernel, dim3((unsigned)p.n_weighs), 256);
     return (int)hipGetLastError();
 }
 

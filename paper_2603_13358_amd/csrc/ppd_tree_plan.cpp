@@ -45,12 +45,14 @@ int32_t choose_chunk(const TileKind& kind, const std::vector<std::pair<int32_t, 
 
 }  // namespace
 
-bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int32_t B, bool weighted, int num_cus, TreePlan* plan) {
+bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int32_t B, bool weighted, int kv_elem_bytes, int num_cus, TreePlan* plan) {
     const int G = s.num_q_heads / s.num_kv_heads, Hkv = s.num_kv_heads, D = s.head_dim;
     plan->items.clear();
     plan->blocks.clear();
     plan->groups.clear();
     plan->weighs.clear();
+    plan->score_weighs.clear();
+    plan->score_floats = 0;
     plan->partial_floats = 0;
     plan->join_cols = 0;
     const TileKind narrow = {kMaxTreeChunk, kTreeStep, 256, 256, 2.0 * num_cus};
@@ -77,6 +79,8 @@ bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int
         const int32_t piece = std::min(kind.max_chunk, ((total + pieces - 1) / pieces + kind.step - 1) / kind.step * kind.step);
         const int32_t nsplit = (total + piece - 1) / piece;
         const int32_t blocks = is_wide ? (n[i] + block_rows - 1) / block_rows : 1, rows = (n[i] + blocks - 1) / blocks;
+        // Scores are kept where writing and reading them (8 bytes a column and key) moves less than reading K again.
+        const bool keep_scores = weighted && !is_wide && (int64_t)n[i] * G * 8 <= (int64_t)D * kv_elem_bytes;
         for (int h = 0; h < Hkv; ++h) {
             for (int32_t row0 = 0; row0 < n[i]; row0 += rows) {
                 const int32_t nrows = std::min(rows, n[i] - row0), cols = nrows * G;
@@ -104,13 +108,16 @@ bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int
                         it.part_off = part;
                         plan->blocks.push_back(it);
                     } else {
-                        plan->items.push_back({i, h, grow0, cols, L[i], total, begin, end, part});
+                        plan->items.push_back({i, h, grow0, cols, L[i], total, begin, end, part, keep_scores ? plan->score_floats : -1});
                     }
                 }
                 if (nsplit > 1) plan->partial_floats += stride * nsplit;
             }
-            if (weighted)
-                for (int32_t t = 0; t < total; t += kWeighKeys) plan->weighs.push_back({i, h, grow0, n[i] * G, L[i], total, t, 0});
+            if (weighted) {
+                std::vector<WeighItem>& list = keep_scores ? plan->score_weighs : plan->weighs;
+                for (int32_t t = 0; t < total; t += kWeighKeys) list.push_back({i, h, grow0, n[i] * G, L[i], total, t, 0, keep_scores ? plan->score_floats : -1});
+                if (keep_scores) plan->score_floats += (int64_t)n[i] * G * score_stride(total);
+            }
         }
         grow0 += n[i];
     }

@@ -199,6 +199,7 @@ static void refusals() {
 static void plans() {
     std::mt19937 rng(3);
     int split = 0, whole = 0, blocks = 0;
+    size_t with_scores = 0, without = 0;
     for (int trial = 0; trial < 200; ++trial) {
         const int hkv = 1 + rng() % 8, G = 1 + rng() % 8, dim = rng() % 2 ? 128 : 64;
         const ppd_shape s = {hkv * G, hkv, dim, 16, 1 << 20};
@@ -206,8 +207,9 @@ static void plans() {
         for (auto& x : L) x = (int32_t)(rng() % (1u << (1 + rng() % 17)));
         for (auto& x : n) x = 1 + (int32_t)(rng() % (1u << (rng() % 9)));
         const bool weighted = rng() % 2;
+        const int eb = 1 + rng() % 2;
         ppd::TreePlan p;
-        CHECK(ppd::build_tree_plan(s, L.data(), n.data(), (int)L.size(), weighted, 256, &p));
+        CHECK(ppd::build_tree_plan(s, L.data(), n.data(), (int)L.size(), weighted, eb, 256, &p));
         std::vector<int> grow0(L.size() + 1, 0);
         for (size_t i = 0; i < L.size(); ++i) grow0[i + 1] = grow0[i] + n[i];
         CHECK(p.rows == grow0.back());
@@ -259,7 +261,24 @@ static void plans() {
         CHECK(joined.size() == offsets.size());
         int64_t weighed = 0;
         std::set<std::tuple<int, int, int>> once;
-        for (const auto& w : p.weighs) {
+        std::vector<ppd::WeighItem> all = p.weighs;
+        all.insert(all.end(), p.score_weighs.begin(), p.score_weighs.end());
+        std::map<std::pair<int, int>, int64_t> kept;  // where the scores of a sequence and head go
+        for (const auto& it : p.items)
+            if (it.score_off >= 0) CHECK(weighted && kept.emplace(std::make_pair(it.seq, it.kvh), it.score_off).first->second == it.score_off);
+        std::map<int64_t, int64_t> areas;
+        for (const auto& k : kept) CHECK(areas.emplace(k.second, k.second + (int64_t)n[k.first.first] * G * ppd::score_stride(L[k.first.first] + n[k.first.first])).second);
+        int64_t area_end = 0;
+        for (const auto& a : areas) {
+            CHECK(a.first == area_end && a.first % 4 == 0);
+            area_end = a.second;
+        }
+        CHECK(area_end == p.score_floats);
+        for (const auto& w : p.weighs) CHECK(w.score_off < 0);
+        for (const auto& w : p.score_weighs) CHECK(kept.at(std::make_pair(w.seq, w.kvh)) == w.score_off);
+        with_scores += p.score_weighs.size();
+        without += p.weighs.size();
+        for (const auto& w : all) {
             CHECK(w.kv_begin % ppd::kWeighKeys == 0 && w.kv_begin < w.kv_total && w.kv_total == L[w.seq] + n[w.seq] && w.cols == n[w.seq] * G && w.grow0 == grow0[w.seq]);
             CHECK(once.insert(std::make_tuple(w.seq, w.kvh, w.kv_begin)).second);
             weighed += std::min(ppd::kWeighKeys, w.kv_total - w.kv_begin);
@@ -268,12 +287,12 @@ static void plans() {
         for (size_t i = 0; i < L.size(); ++i) keys += (int64_t)hkv * (L[i] + n[i]);
         CHECK(weighed == (weighted ? keys : 0));
     }
-    CHECK(split > 1000 && whole > 1000 && blocks > 1000 && blocks < split + whole - 1000);
+    CHECK(with_scores > 1000 && without > 1000 && split > 1000 && whole > 1000 && blocks > 1000 && blocks < split + whole - 1000);
     // a batch beyond what one launch takes is refused, not built
     const ppd_shape s = {8192, 1024, 128, 16, 1 << 16};
     std::vector<int32_t> L(4096, 100), n(4096, 64);
     ppd::TreePlan p;
-    CHECK(!ppd::build_tree_plan(s, L.data(), n.data(), 4096, true, 256, &p));
+    CHECK(!ppd::build_tree_plan(s, L.data(), n.data(), 4096, true, 2, 256, &p));
 }
 
 // Long batches go out in launches of what the kernel arguments hold, each with its own part of every array.
@@ -324,13 +343,14 @@ static void streams() {
     sim.capturing = false;
     CHECK(tree(b) == PPD_OK && a->waiting() == 0 && b->waiting() == 0);
     CHECK(weighted(b) == PPD_OK && b->waiting() == 1);  // another list: the keys to weigh
-    CHECK(g_weigh.size() == 1 && g_weigh[0].n_weighs == 8 * (4 + 1));
+    CHECK(g_weigh.size() == 1 && g_weigh[0].n_weighs + g_weigh[0].n_score_weighs == 8 * (4 + 1));
     b->run();
     const ppd::TreeParams& p = g_weigh[0];
     CHECK(p.n_items > 0 && g_blocks.back().n_items > 0);
     for (int i = 0; i < p.n_items; ++i) CHECK(p.items[i].L == L[p.items[i].seq]);
     for (int i = 0; i < g_blocks.back().n_items; ++i) CHECK(g_blocks.back().items[i].L == L[g_blocks.back().items[i].seq]);
     for (int i = 0; i < p.n_weighs; ++i) CHECK(p.weighs[i].L == L[p.weighs[i].seq]);
+    for (int i = 0; i < p.n_score_weighs; ++i) CHECK(p.score_weighs[i].L == L[p.score_weighs[i].seq]);
     L[0] = 1001;
     sim.launch_status = hipErrorLaunchFailure;
     CHECK(tree(b) == PPD_ERR_HIP);
