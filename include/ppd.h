@@ -232,7 +232,8 @@ ppd_status ppd_mixed_attention_static(ppd_ctx *ctx, const void *q, const void *k
  * Speculative decoding on the decode node drafts a tree of tokens per sequence, verifies all of them in one step and keeps one path;
  * contexts that outgrow the pool are cut down to the tokens that attention looks at.  Four calls, on pools of either element
  * format, all asynchronous on `stream` and under the conventions above (a plan changed under capture is refused, as by
- * ppd_mixed_attention; ppd_kv_select and ppd_kv_compact have no plan and can always be captured). */
+ * ppd_mixed_attention; ppd_kv_select of rows above 16384 tokens needs a workspace, and is refused under capture until a call as
+ * large has run eagerly; ppd_kv_compact can always be captured). */
 
 /* Attention for a tree of drafted tokens over the cache.  Sequence i has L_i cached tokens and n_i drafted nodes, whose K/V have been
  * appended at positions L_i .. L_i + n_i - 1 (in any order in which the caller numbers them).  Row j sees the keys 0 .. L_i - 1 and

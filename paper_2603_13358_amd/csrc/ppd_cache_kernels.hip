@@ -19,106 +19,379 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 }  // namespace
 
-// One workgroup chooses for one sequence and KV head.  The weight of the last chosen token is found digit by digit (four
-// histograms of eight bits, the heaviest digit first); every wave then counts the chosen ones of its stretch of positions, and
-// after a sum over the waves in front writes them in order.  Tokens of that last weight are taken from the lowest position on.
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
-__global__ __launch_bounds__(kSelectThreads) void ppd_select_kernel(const SelectParams P) {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t found[2];
-    __shared__ int heavier[kSelectWaves], equal[kSelectWaves];
+// ---- the choice ---------------------------------------------------------------------------------------------
+// The weight of the last chosen token is found digit by digit, the heaviest first (histograms in LDS over 11, 11 and 10 bits): `prefix` holds
+// the digits found so far in the places of `mask`, `left` how many of the tokens with these digits are chosen.  A search ends
+// early where they all are.  Tokens of that last weight are taken from the lowest position on.
+constexpr int kDigits = 3, kBins = kSelectBins;
+__device__ __forceinline__ int digit_shift(int i) { return i == 0 ? 21 : i == 1 ? 10 : 0; }
+__device__ __forceinline__ int digit_bins(int i) { return i == 2 ? 1024 : 2048; }
+
+struct Search {
+    uint32_t prefix = 0, mask = 0;
+    int left = 0;
+    __device__ __forceinline__ bool candidate(uint32_t key) const { return (key & mask) == prefix; }
+    __device__ __forceinline__ bool above(uint32_t key) const { return (key & mask) > prefix; }
+};
+
+template <int NT>
+struct SearchLds {
+    uint32_t hist[kBins];
+    uint32_t wave_sum[NT / 64];
+    uint32_t found[3];  // digit, tokens above it, tokens of it
+};
+
+// Adds the digits of a wave's lanes to the histogram.  Weights that attention leaves crowd in few bins (and many are zero): the
+// first lane's digit is counted for all that share it at once.
+__device__ __forceinline__ void count_digit(uint32_t* hist, bool live, uint32_t digit) {
+    const uint64_t all = __ballot(live);
+    if (!all) return;
+    const int first = __builtin_ctzll(all);
+    const uint32_t common = __builtin_amdgcn_readlane(digit, first);
+    const uint64_t same = __ballot(live && digit == common);
+    if ((int)(threadIdx.x & 63) == first) atomicAdd(&hist[common], (uint32_t)__popcll(same));
+    if (live && digit != common) atomicAdd(&hist[digit], 1u);
+}
+
+// Thread t has the bins kBins - 1 - t * PER .. (heaviest first); the one in which the running count reaches `left` is the digit.  All threads
+// call it, with the histogram complete; the histogram may be cleared after it.  Returns whether all tokens of the digit are chosen.
+template <int NT>
+__device__ __forceinline__ bool take_digit(SearchLds<NT>& lds, Search& s, int i, const uint32_t (&n)[kBins / NT]) {
+    constexpr int PER = kBins / NT;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) mine += n[j];
+    uint32_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(upto, d, 64);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 63) lds.wave_sum[wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - mine;
+    for (int w = 0; w < wave; ++w) before += lds.wave_sum[w];
+    if (before < (uint32_t)s.left && before + mine >= (uint32_t)s.left) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            if (before < (uint32_t)s.left && before + n[j] >= (uint32_t)s.left) {
+                lds.found[0] = kBins - 1 - (tid * PER + j);
+                lds.found[1] = before;
+                lds.found[2] = n[j];
+            }
+            before += n[j];
+        }
+    }
+    __syncthreads();
+    const int shift = digit_shift(i);
+    s.prefix |= lds.found[0] << shift;
+    s.mask |= (uint32_t)(digit_bins(i) - 1) << shift;
+    s.left -= (int)lds.found[1];
+    return (int)lds.found[2] == s.left;
+}
+
+template <int NT>
+__device__ __forceinline__ bool take_digit_from_lds(SearchLds<NT>& lds, Search& s, int i) {
+    constexpr int PER = kBins / NT;
+    uint32_t n[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) n[j] = lds.hist[kBins - 1 - (threadIdx.x * PER + j)];
+    return take_digit<NT>(lds, s, i, n);
+}
+
+template <int NT>
+__device__ __forceinline__ void clear_hist(SearchLds<NT>& lds) {
+    for (int i = threadIdx.x; i < kBins; i += NT) lds.hist[i] = 0;
+    __syncthreads();
+}
+
+// A line is 64 neighbouring positions, a lane each.  Writes the chosen ones of a line in order and moves on.
+struct Writer {
+    int32_t* keep;
+    int at, same_before;
+    __device__ __forceinline__ void line(const Search& s, int pos, bool always, bool candidate) {
+        const int lane = threadIdx.x & 63;
+        const uint64_t below = (1ull << lane) - 1, same = __ballot(candidate);
+        const bool chosen = always || (candidate && same_before + __popcll(same & below) < s.left);
+        same_before += __popcll(same);
+        const uint64_t m = __ballot(chosen);
+        if (chosen) keep[at + __popcll(m & below)] = pos;
+        at += __popcll(m);
+    }
+};
+
+// One workgroup to a sequence and KV head, whose weights it reads once and holds in registers: wave w has the lines w * lines ..
+// (w + 1) * lines - 1, at most VPT of them.
+template <int NT, int VPT>
+__global__ __launch_bounds__(NT) void ppd_select_kernel(const SelectParams P) {
+    constexpr int NW = NT / 64;
+    __shared__ SearchLds<NT> lds;
+    __shared__ int n_above[NW], n_same[NW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int b = blockIdx.y, head = blockIdx.x, len = P.length[b];
     const float* w = P.weights + ((int64_t)b * P.Hkv + head) * P.weight_stride;
     int32_t* keep = P.keep + ((int64_t)b * P.Hkv + head) * P.keep_stride;
     if (len <= P.budget) {
-        for (int t = tid; t < len; t += kSelectThreads) keep[t] = t;
+        for (int t = tid; t < len; t += NT) keep[t] = t;
         return;
     }
     const int lo = P.sinks, hi = len - P.recent;  // the others: positions [lo, hi)
-    const int want = P.budget - P.sinks - P.recent;
-    uint32_t prefix = 0, mask = 0;
-    int left = want;  // of the tokens whose digits so far are `prefix`
-    if (want > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0;
-            __syncthreads();
-            for (int t = lo + tid; t < hi; t += kSelectThreads) {
-                const uint32_t k = weight_key(w[t]);
-                if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+    const int lines = ((len + 63) / 64 + NW - 1) / NW;
+    const int p0 = wave * lines * 64 + lane;
+    uint32_t key[VPT];
+#pragma unroll
+    for (int r = 0; r < VPT; ++r) {
+        const int pos = p0 + r * 64;
+        key[r] = 0;
+        if (r < lines && pos >= lo && pos < hi) key[r] = __builtin_bit_cast(uint32_t, w[pos]);
+    }
+#pragma unroll
+    for (int r = 0; r < VPT; ++r) key[r] = weight_key(__builtin_bit_cast(float, key[r]));
+    Search s;
+    s.left = P.budget - P.sinks - P.recent;
+    const bool search = s.left > 0;
+    if (search) {
+        for (int i = 0; i < kDigits; ++i) {
+            clear_hist(lds);
+            const int shift = digit_shift(i);
+            const uint32_t bins = digit_bins(i) - 1;
+#pragma unroll
+            for (int r = 0; r < VPT; ++r) {
+                const int pos = p0 + r * 64;
+                if (r < lines) count_digit(lds.hist, pos >= lo && pos < hi && s.candidate(key[r]), (key[r] >> shift) & bins);
             }
             __syncthreads();
-            if (wave == 0) {
-                // lane l has digits 255 - 4l .. 252 - 4l, heaviest first
-                uint32_t n[4], mine = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mine += n[i] = hist[255 - 4 * lane - i];
-                uint32_t upto = mine;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const uint32_t o = __shfl_up(upto, d, 64);
-                    if (lane >= d) upto += o;
-                }
-                uint32_t before = upto - mine;
-                if (before < (uint32_t)left && upto >= (uint32_t)left) {
-                    int i = 0;
-                    while (before + n[i] < (uint32_t)left) before += n[i++];
-                    found[0] = 255u - 4 * lane - i;
-                    found[1] = before;
-                }
-            }
-            __syncthreads();
-            prefix |= found[0] << shift;
-            mask |= 255u << shift;
-            left -= (int)found[1];
+            if (take_digit_from_lds<NT>(lds, s, i)) break;
         }
     }
-    // chosen: the first and the last ones, keys above `prefix`, and the first `left` ones equal to it
-    auto classify = [&](int t, bool* above, bool* same) {
-        *above = *same = false;
-        if (t >= len) return;
-        if (t < lo || t >= hi) {
-            *above = true;
-        } else if (want > 0) {
-            const uint32_t k = weight_key(w[t]);
-            *above = k > prefix;
-            *same = k == prefix;
+    int above = 0, same = 0;
+#pragma unroll
+    for (int r = 0; r < VPT; ++r) {
+        const int pos = p0 + r * 64;
+        if (r < lines) {
+            const bool other = pos >= lo && pos < hi;
+            above += __popcll(__ballot(pos < len && (!other || (search && s.above(key[r])))));
+            same += __popcll(__ballot(other && search && s.candidate(key[r])));
         }
-    };
-    const int stretch = (len + kSelectThreads - 1) / kSelectThreads * 64;
-    const int begin = wave * stretch, end = begin + stretch;
-    int n_above = 0, n_same = 0;
-    for (int t = begin; t < end; t += 64) {
-        bool above, same;
-        classify(t + lane, &above, &same);
-        n_above += __popcll(__ballot(above));
-        n_same += __popcll(__ballot(same));
     }
     if (lane == 0) {
-        heavier[wave] = n_above;
-        equal[wave] = n_same;
+        n_above[wave] = above;
+        n_same[wave] = same;
     }
     __syncthreads();
-    int at = 0, same_before = 0;
+    Writer out{keep, 0, 0};
     for (int i = 0; i < wave; ++i) {
-        at += heavier[i];
-        same_before += equal[i];
+        out.at += n_above[i];
+        out.same_before += n_same[i];
     }
-    at += same_before < left ? same_before : left;
-    for (int t = begin; t < end; t += 64) {
-        bool above, same;
-        classify(t + lane, &above, &same);
-        const uint64_t m_same = __ballot(same), below = (1ull << lane) - 1;
-        const bool chosen = above || (same && same_before + __popcll(m_same & below) < left);
-        same_before += __popcll(m_same);
-        const uint64_t m = __ballot(chosen);
-        if (chosen) keep[at + __popcll(m & below)] = t + lane;
-        at += __popcll(m);
+    out.at += out.same_before < s.left ? out.same_before : s.left;
+#pragma unroll
+    for (int r = 0; r < VPT; ++r) {
+        const int pos = p0 + r * 64;
+        if (r < lines) {
+            const bool other = pos >= lo && pos < hi;
+            out.line(s, pos, pos < len && (!other || (search && s.above(key[r]))), other && search && s.candidate(key[r]));
+        }
     }
 }
 
-int launch_select(const SelectParams& p, void* stream) {
-    hipLaunchKernelGGL(ppd_select_kernel, dim3((unsigned)p.Hkv, (unsigned)p.B), dim3(kSelectThreads), 0, static_cast<hipStream_t>(stream), p);
+// Longer rows are cut into chunks of kSelectChunk positions, a workgroup each, in three launches: the first leaves every chunk's
+// histogram of the first digit; the second finds that digit from all of the row's, and leaves every chunk's candidates (the
+// tokens that have it) and how many are above them; the third finds the rest from the candidates of all chunks, which every
+// chunk's workgroup reads for itself, and writes its chunk.
+constexpr int kChunkThreads = 1024, kChunkLines = kSelectChunk / kChunkThreads;
+static_assert(kChunkLines * kChunkThreads == kSelectChunk, "whole lines");
+
+struct ChunkRow {  // what a chunk's workgroup knows of its row
+    int row, chunk, len, lo, hi, chunks;
+    const float* w;
+};
+__device__ __forceinline__ ChunkRow chunk_row(const SelectParams& P) {
+    ChunkRow c;
+    c.row = blockIdx.x / P.max_chunks;
+    c.chunk = blockIdx.x % P.max_chunks;
+    c.len = P.length[c.row / P.Hkv];
+    c.lo = P.sinks;
+    c.hi = c.len - P.recent;
+    c.chunks = (c.len + kSelectChunk - 1) / kSelectChunk;
+    c.w = P.weights + (int64_t)c.row * P.weight_stride;
+    return c;
+}
+// Keys of this thread's lines of the chunk, and which of them are others (neither first nor last ones).
+__device__ __forceinline__ void chunk_keys(const ChunkRow& c, uint32_t (&key)[kChunkLines], bool (&other)[kChunkLines], int (&pos)[kChunkLines]) {
+    const int p0 = c.chunk * kSelectChunk + (int)(threadIdx.x >> 6) * (kChunkLines * 64) + (int)(threadIdx.x & 63);
+#pragma unroll
+    for (int r = 0; r < kChunkLines; ++r) {
+        pos[r] = p0 + r * 64;
+        other[r] = pos[r] >= c.lo && pos[r] < c.hi;
+        key[r] = other[r] ? __builtin_bit_cast(uint32_t, c.w[pos[r]]) : 0;
+    }
+#pragma unroll
+    for (int r = 0; r < kChunkLines; ++r) key[r] = weight_key(__builtin_bit_cast(float, key[r]));
+}
+// The first digit, from the histograms of the row's chunks.
+__device__ __forceinline__ bool first_digit(const SelectParams& P, const ChunkRow& c, SearchLds<kChunkThreads>& lds, Search& s) {
+    constexpr int PER = kBins / kChunkThreads;
+    uint32_t n[PER] = {};
+    const uint32_t* h = P.hist + (int64_t)c.row * P.max_chunks * kBins + kBins - 1 - threadIdx.x * PER;
+    for (int k = 0; k < c.chunks; ++k)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) n[j] += h[(int64_t)k * kBins - j];
+    return take_digit<kChunkThreads>(lds, s, 0, n);
+}
+
+__global__ __launch_bounds__(kChunkThreads) void ppd_select_digits_kernel(const SelectParams P) {
+    __shared__ SearchLds<kChunkThreads> lds;
+    const ChunkRow c = chunk_row(P);
+    if (c.chunk >= c.chunks || c.len <= P.budget || P.budget == P.sinks + P.recent) return;
+    uint32_t key[kChunkLines];
+    bool other[kChunkLines];
+    int pos[kChunkLines];
+    chunk_keys(c, key, other, pos);
+    clear_hist(lds);
+#pragma unroll
+    for (int r = 0; r < kChunkLines; ++r) count_digit(lds.hist, other[r], key[r] >> digit_shift(0));
+    __syncthreads();
+    uint32_t* h = P.hist + ((int64_t)c.row * P.max_chunks + c.chunk) * kBins;
+    for (int i = threadIdx.x; i < kBins; i += kChunkThreads) h[i] = lds.hist[i];
+}
+
+__global__ __launch_bounds__(kChunkThreads) void ppd_select_candidates_kernel(const SelectParams P) {
+    constexpr int NW = kChunkThreads / 64;
+    __shared__ SearchLds<kChunkThreads> lds;
+    __shared__ int n_above[NW], n_same[NW];
+    const ChunkRow c = chunk_row(P);
+    if (c.chunk >= c.chunks || c.len <= P.budget) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Search s;
+    s.left = P.budget - P.sinks - P.recent;
+    const bool search = s.left > 0;
+    uint32_t key[kChunkLines];
+    bool other[kChunkLines];
+    int pos[kChunkLines];
+    chunk_keys(c, key, other, pos);
+    if (search) first_digit(P, c, lds, s);
+    int above = 0, same = 0;
+#pragma unroll
+    for (int r = 0; r < kChunkLines; ++r) {
+        above += __popcll(__ballot(pos[r] < c.len && (!other[r] || (search && s.above(key[r])))));
+        same += __popcll(__ballot(other[r] && search && s.candidate(key[r])));
+    }
+    if (lane == 0) {
+        n_above[wave] = above;
+        n_same[wave] = same;
+    }
+    __syncthreads();
+    int at = 0;
+    for (int i = 0; i < wave; ++i) at += n_same[i];
+    const int64_t mine = (int64_t)c.row * P.max_chunks + c.chunk;
+    uint32_t* list = P.candidates + mine * kSelectChunk;
+#pragma unroll
+    for (int r = 0; r < kChunkLines; ++r) {
+        const bool cand = other[r] && search && s.candidate(key[r]);
+        const uint64_t m = __ballot(cand);
+        if (cand) list[at + __popcll(m & ((1ull << lane) - 1))] = key[r];
+        at += __popcll(m);
+    }
+    if (threadIdx.x == 0) {
+        int total_above = 0, total_same = 0;
+        for (int i = 0; i < NW; ++i) {
+            total_above += n_above[i];
+            total_same += n_same[i];
+        }
+        P.counts[mine * 2] = total_above;
+        P.counts[mine * 2 + 1] = total_same;
+    }
+}
+
+__global__ __launch_bounds__(kChunkThreads) void ppd_select_finish_kernel(const SelectParams P) {
+    constexpr int NW = kChunkThreads / 64;
+    __shared__ SearchLds<kChunkThreads> lds;
+    __shared__ int n_above[NW], n_same[NW], before[2];
+    const ChunkRow c = chunk_row(P);
+    if (c.chunk >= c.chunks) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int32_t* keep = P.keep + (int64_t)c.row * P.keep_stride;
+    if (c.len <= P.budget) {
+        for (int t = c.chunk * kSelectChunk + tid; t < c.len && t < (c.chunk + 1) * kSelectChunk; t += kChunkThreads) keep[t] = t;
+        return;
+    }
+    Search s;
+    s.left = P.budget - P.sinks - P.recent;
+    const bool search = s.left > 0;
+    uint32_t key[kChunkLines];
+    bool other[kChunkLines];
+    int pos[kChunkLines];
+    chunk_keys(c, key, other, pos);
+    const int64_t first = (int64_t)c.row * P.max_chunks;
+    bool all = !search || first_digit(P, c, lds, s);
+    auto each_candidate = [&](int chunks, auto f) {  // f(live, key) for the candidates of the first `chunks` chunks, by whole waves
+        for (int k = 0; k < chunks; ++k) {
+            const int n = P.counts[(first + k) * 2 + 1];
+            const uint32_t* list = P.candidates + (first + k) * kSelectChunk;
+            for (int i = wave * 64; i < n; i += kChunkThreads) f(i + lane < n, i + lane < n ? list[i + lane] : 0u);
+        }
+    };
+    for (int i = 1; i < kDigits && !all; ++i) {
+        clear_hist(lds);
+        const int shift = digit_shift(i);
+        const uint32_t bins = digit_bins(i) - 1;
+        each_candidate(c.chunks, [&](bool live, uint32_t k) { count_digit(lds.hist, live && s.candidate(k), (k >> shift) & bins); });
+        __syncthreads();
+        all = take_digit_from_lds<kChunkThreads>(lds, s, i);
+    }
+    // how many are chosen for certain, and how many have the last weight, in the chunks in front: counted above the first digit there, the
+    // rest among their candidates
+    if (tid < 2) before[tid] = 0;
+    __syncthreads();
+    {
+        int above = 0, same = 0;
+        if (search)
+            each_candidate(c.chunk, [&](bool live, uint32_t k) {
+                above += __popcll(__ballot(live && s.above(k)));
+                same += __popcll(__ballot(live && s.candidate(k)));
+            });
+        if (tid < c.chunk) atomicAdd(&before[0], P.counts[(first + tid) * 2]);
+        for (int k = tid + kChunkThreads; k < c.chunk; k += kChunkThreads) atomicAdd(&before[0], P.counts[(first + k) * 2]);
+        if (lane == 0 && above) atomicAdd(&before[0], above);
+        if (lane == 0 && same) atomicAdd(&before[1], same);
+    }
+    int above = 0, same = 0;
+#pragma unroll
+    for (int r = 0; r < kChunkLines; ++r) {
+        above += __popcll(__ballot(pos[r] < c.len && (!other[r] || (search && s.above(key[r])))));
+        same += __popcll(__ballot(other[r] && search && s.candidate(key[r])));
+    }
+    if (lane == 0) {
+        n_above[wave] = above;
+        n_same[wave] = same;
+    }
+    __syncthreads();
+    Writer out{keep, before[0], before[1]};
+    for (int i = 0; i < wave; ++i) {
+        out.at += n_above[i];
+        out.same_before += n_same[i];
+    }
+    out.at += out.same_before < s.left ? out.same_before : s.left;
+#pragma unroll
+    for (int r = 0; r < kChunkLines; ++r)
+        out.line(s, pos[r], pos[r] < c.len && (!other[r] || (search && s.above(key[r]))), other[r] && search && s.candidate(key[r]));
+}
+
+int launch_select(const SelectParams& p, int longest, void* stream) {
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    if (p.max_chunks > 0) {
+        const dim3 grid((unsigned)(p.B * p.Hkv * p.max_chunks));
+        hipLaunchKernelGGL(ppd_select_digits_kernel, grid, dim3(kChunkThreads), 0, hs, p);
+        hipLaunchKernelGGL(ppd_select_candidates_kernel, grid, dim3(kChunkThreads), 0, hs, p);
+        hipLaunchKernelGGL(ppd_select_finish_kernel, grid, dim3(kChunkThreads), 0, hs, p);
+        return (int)hipGetLastError();
+    }
+    const dim3 grid((unsigned)p.Hkv, (unsigned)p.B);
+    if (longest <= 256 * 8) hipLaunchKernelGGL((ppd_select_kernel<256, 8>), grid, dim3(256), 0, hs, p);
+    else if (longest <= 1024 * 8) hipLaunchKernelGGL((ppd_select_kernel<1024, 8>), grid, dim3(1024), 0, hs, p);
+    else hipLaunchKernelGGL((ppd_select_kernel<1024, kSelectChunk / 1024>), grid, dim3(1024), 0, hs, p);
     return (int)hipGetLastError();
 }
 

@@ -19,6 +19,8 @@ constexpr int kMaxTreeBlockChunk = 16384;  // the same of a row block
 constexpr int kMaxMaskWords = 16;    // 64-bit words of a row's tree mask at most
 constexpr int kWeighKeys = 256;      // keys of a workgroup that adds up attention weights
 constexpr int kSelectBatch = 512;    // sequences per launch of the select kernel (their lengths are kernel arguments)
+constexpr int kSelectChunk = 16384;  // weights that a workgroup of the select kernels holds in registers
+constexpr int kSelectBins = 2048;    // of the chunks' histograms
 constexpr int kCompactBatch = 256;   // the same for the move (two lists)
 
 // A tile of tree attention: all `ncols` query columns of one sequence and KV head (row-major over the G heads of the group), at most
@@ -106,6 +108,11 @@ struct SelectParams {
     int64_t weight_stride, keep_stride;
     int32_t Hkv, budget, sinks, recent;
     int32_t B;
+    // rows longer than kSelectChunk: chunks of the longest (0: none is longer), and per row and chunk the histogram, the candidates and
+    // (tokens above them, candidates)
+    int32_t max_chunks;
+    uint32_t *hist, *candidates;
+    int32_t* counts;
     int32_t length[kSelectBatch];
 };
 
@@ -128,7 +135,7 @@ int launch_tree(const TreeParams& p, int head_dim, bool fp8_pages, void* stream)
 int launch_tree_blocks(const TreeBlockParams& p, int head_dim, bool fp8_pages, void* stream);
 int launch_tree_join(const TreeParams& p, int head_dim, void* stream);
 int launch_weigh(const TreeParams& p, int head_dim, bool fp8_pages, void* stream);
-int launch_select(const SelectParams& p, void* stream);
+int launch_select(const SelectParams& p, int longest, void* stream);
 int launch_compact(const CompactParams& p, int head_dim, bool fp8_pages, int layers, void* stream);
 
 }  // namespace ppd

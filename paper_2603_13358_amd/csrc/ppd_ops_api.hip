@@ -27,6 +27,8 @@ struct TreeState {
     size_t d_stats_bytes = 0;
     void* d_scores = nullptr;
     size_t d_scores_bytes = 0;
+    void* d_select = nullptr;
+    size_t d_select_bytes = 0;
     std::vector<int32_t> L, n;
     bool weighted = false, fp8_pages = false, on_device = false;
     ppd::TreePlan plan;
@@ -42,6 +44,7 @@ void free_tree_state(void* p) {
     if (t->d_partials) (void)hipFree(t->d_partials);
     if (t->d_stats) (void)hipFree(t->d_stats);
     if (t->d_scores) (void)hipFree(t->d_scores);
+    if (t->d_select) (void)hipFree(t->d_select);
     delete t;
 }
 
@@ -62,6 +65,14 @@ ppd_status tree_state(ppd_ctx* ctx, TreeState** out) {
         ctx->free_tree = free_tree_state;
     }
     *out = static_cast<TreeState*>(ctx->tree);
+    return PPD_OK;
+}
+
+// A context serves one stream at a time: what the call before enqueued on another one has to finish first.
+ppd_status follow_stream(ppd_ctx* ctx, hipStream_t hs) {
+    if (ctx->have_plan_stream && ctx->plan_stream != hs) PPD_HIP(ctx, hipStreamSynchronize(ctx->plan_stream));
+    ctx->plan_stream = hs;
+    ctx->have_plan_stream = true;
     return PPD_OK;
 }
 
@@ -157,7 +168,8 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
     hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
     PPD_HIP(ctx, hipStreamIsCapturing(hs, &capturing));
     const bool in_capture = capturing != hipStreamCaptureStatusNone;
-    if (!in_capture && ctx->have_plan_stream && ctx->plan_stream != hs) PPD_HIP(ctx, hipStreamSynchronize(ctx->plan_stream));
+    if (!in_capture) st = follow_stream(ctx, hs);
+    if (st != PPD_OK) return st;
     const bool reuse = t->on_device && t->weighted == weighted && t->fp8_pages == ctx->fp8_pages && (int32_t)t->L.size() == B &&
                        std::memcmp(t->L.data(), L, sizeof(int32_t) * B) == 0 && std::memcmp(t->n.data(), n, sizeof(int32_t) * B) == 0;
     if (!reuse) {
@@ -165,10 +177,6 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
             return fail(ctx, PPD_ERR_RANGE, "plan changed under capture: run the step once eagerly with these L, n and options first, then capture it");
         st = upload_tree_plan(ctx, t, L, n, B, weighted, hs);
         if (st != PPD_OK) return st;
-    }
-    if (!in_capture) {
-        ctx->plan_stream = hs;
-        ctx->have_plan_stream = true;
     }
     const ppd::TreePlan& plan = t->plan;
     const char* d_plan = static_cast<const char*>(t->d_plan);
@@ -263,6 +271,30 @@ ppd_status guarded(ppd_ctx* ctx, F f) {
     }
 }
 
+// Rows of more than one chunk leave histograms and candidates in the workspace between their launches.
+ppd_status select_workspace(ppd_ctx* ctx, ppd::SelectParams* p, int32_t longest, hipStream_t hs) {
+    TreeState* t = nullptr;
+    ppd_status st = tree_state(ctx, &t);
+    if (st != PPD_OK) return st;
+    p->max_chunks = (longest + ppd::kSelectChunk - 1) / ppd::kSelectChunk;
+    const size_t chunks = (size_t)p->B * p->Hkv * p->max_chunks, words = (size_t)ppd::kSelectBins + ppd::kSelectChunk + 2;
+    if (chunks > (size_t)INT32_MAX) return fail(ctx, PPD_ERR_RANGE, "more rows of this length than one launch takes");
+    hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+    PPD_HIP(ctx, hipStreamIsCapturing(hs, &capturing));
+    const size_t bytes = chunks * words * sizeof(uint32_t);
+    if (capturing == hipStreamCaptureStatusNone) {
+        st = follow_stream(ctx, hs);
+        if (st == PPD_OK) st = grow_device(ctx, &t->d_select, &t->d_select_bytes, bytes, hs);
+        if (st != PPD_OK) return st;
+    } else if (bytes > t->d_select_bytes) {
+        return fail(ctx, PPD_ERR_RANGE, "rows this long need a workspace, which cannot be allocated under capture: run the call once eagerly first");
+    }
+    p->hist = static_cast<uint32_t*>(t->d_select);
+    p->candidates = p->hist + chunks * ppd::kSelectBins;
+    p->counts = reinterpret_cast<int32_t*>(p->candidates + chunks * ppd::kSelectChunk);
+    return PPD_OK;
+}
+
 ppd_status select_impl(ppd_ctx* ctx, const float* weights, int64_t weight_stride, const int32_t* length, int32_t B, int32_t budget, int32_t sinks,
                        int32_t recent, int32_t* keep, int64_t keep_stride, void* stream) {
     if (!ctx) return PPD_ERR_NULL;
@@ -291,7 +323,13 @@ ppd_status select_impl(ppd_ctx* ctx, const float* weights, int64_t weight_stride
         p.weights = weights + (int64_t)at * p.Hkv * weight_stride;
         p.keep = keep + (int64_t)at * p.Hkv * keep_stride;
         std::copy(length + at, length + at + p.B, p.length);
-        const int rc = ppd::launch_select(p, stream);
+        const int32_t longest = *std::max_element(p.length, p.length + p.B);
+        p.max_chunks = 0;
+        if (longest > ppd::kSelectChunk) {
+            ppd_status st = select_workspace(ctx, &p, longest, static_cast<hipStream_t>(stream));
+            if (st != PPD_OK) return st;
+        }
+        const int rc = ppd::launch_select(p, longest, stream);
         if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch kv_select");
     }
     if (ctx->log_calls) std::fprintf(stderr, "ppd: kv_select B=%d budget=%d\n", (int)B, (int)budget);

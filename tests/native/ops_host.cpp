@@ -42,7 +42,7 @@ int launch_tree(const TreeParams& p, int, bool, void*) { g_tree.push_back(p); re
 int launch_tree_blocks(const TreeBlockParams& p, int, bool, void*) { g_blocks.push_back(p); return 0; }
 int launch_tree_join(const TreeParams&, int, void*) { return 0; }
 int launch_weigh(const TreeParams& p, int, bool, void*) { g_weigh.push_back(p); return 0; }
-int launch_select(const SelectParams& p, void*) { g_select.push_back(p); return 0; }
+int launch_select(const SelectParams& p, int, void*) { g_select.push_back(p); return 0; }
 int launch_compact(const CompactParams& p, int, bool, int, void*) { g_compact.push_back(p); return 0; }
 }  // namespace ppd
 
