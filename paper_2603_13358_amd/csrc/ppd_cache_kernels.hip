@@ -10,19 +10,36 @@ namespace ppd {
 
 namespace {
 
-// Larger for the heavier weight: the bits as an integer of the same order.  Both zeros are equal, NaN is heavier than all else.
+// A weight's bits as an integer of the same order: larger for the heavier one.  Both zeros are equal, NaN is heavier than all else.
+// The lightest, negative infinity, is 0x007fffff; kNoKey is below all and kHeldKey above.
+constexpr uint32_t kNoKey = 0, kHeldKey = ~0u, kNanKey = ~0u - 1;
 __device__ __forceinline__ uint32_t weight_key(float w) {
-    if (w != w) return ~0u;
+    if (w != w) return kNanKey;
     const uint32_t b = w == 0.f ? 0u : __builtin_bit_cast(uint32_t, w);
     return b >> 31 ? ~b : b | 0x80000000u;
 }
 
+// Inclusive sum over the lanes of a wave.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // from the lane 1, 2, 4, 8 to the left within 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 to the next 16 lanes
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
+    return x;
+}
+
+__device__ __forceinline__ int lanes_below(uint64_t m) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0)); }
+
 }  // namespace
 
 // ---- the choice ---------------------------------------------------------------------------------------------
-// The weight of the last chosen token is found digit by digit, the heaviest first (histograms in LDS over 11, 11 and 10 bits): `prefix` holds
-// the digits found so far in the places of `mask`, `left` how many of the tokens with these digits are chosen.  A search ends
-// early where they all are.  Tokens of that last weight are taken from the lowest position on.
+// The first and the last tokens get the heaviest key, so that the choice is the `budget` heaviest of all, the lower position first
+// where keys are equal.  The key of the last chosen token is found from a histogram over its upper 11 bits, in LDS, which leaves few
+// candidates, and from their ranks among one another (or two more histograms, where they are many).  `prefix` holds the bits found
+// so far in the places of `mask`, `left` how many of the tokens with these bits are chosen.
+// Bound by instructions and barriers, not by the weights: a workgroup's steps behind one another take about 4 us.
 constexpr int kDigits = 3, kBins = kSelectBins;
 __device__ __forceinline__ int digit_shift(int i) { return i == 0 ? 21 : i == 1 ? 10 : 0; }
 __device__ __forceinline__ int digit_bins(int i) { return i == 2 ? 1024 : 2048; }
@@ -36,42 +53,35 @@ struct Search {
 
 template <int NT>
 struct SearchLds {
+    static constexpr int kList = 64;  // candidates that are ranked, at most
     uint32_t hist[kBins];
-    uint32_t wave_sum[NT / 64];
+    __attribute__((aligned(16))) uint32_t list[kList];
+    uint32_t wave_sum[NT / 64], wave_sum2[NT / 64];
+    uint32_t listed;
     uint32_t found[3];  // digit, tokens above it, tokens of it
 };
 
-// Adds the digits of a wave's lanes to the histogram.  Weights that attention leaves crowd in few bins (and many are zero): the
-// first lane's digit is counted for all that share it at once.
-__device__ __forceinline__ void count_digit(uint32_t* hist, bool live, uint32_t digit) {
-    const uint64_t all = __ballot(live);
-    if (!all) return;
-    const int first = __builtin_ctzll(all);
-    const uint32_t common = __builtin_amdgcn_readlane(digit, first);
-    const uint64_t same = __ballot(live && digit == common);
-    if ((int)(threadIdx.x & 63) == first) atomicAdd(&hist[common], (uint32_t)__popcll(same));
-    if (live && digit != common) atomicAdd(&hist[digit], 1u);
+template <int NT>
+__device__ __forceinline__ uint32_t sum_before(const uint32_t (&v)[NT / 64], int wave) {  // all reads at once
+    uint32_t s = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) s += w < wave ? v[w] : 0u;
+    return s;
 }
 
 // Thread t has the bins kBins - 1 - t * PER .. (heaviest first); the one in which the running count reaches `left` is the digit.  All threads
-// call it, with the histogram complete; the histogram may be cleared after it.  Returns whether all tokens of the digit are chosen.
+// call it, with the histogram complete.  Returns how many tokens have the digit.
 template <int NT>
-__device__ __forceinline__ bool take_digit(SearchLds<NT>& lds, Search& s, int i, const uint32_t (&n)[kBins / NT]) {
+__device__ __forceinline__ int take_digit(SearchLds<NT>& lds, Search& s, int i, const uint32_t (&n)[kBins / NT]) {
     constexpr int PER = kBins / NT;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     uint32_t mine = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) mine += n[j];
-    uint32_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = __shfl_up(upto, d, 64);
-        if (lane >= d) upto += o;
-    }
+    const uint32_t upto = wave_scan(mine);
     if (lane == 63) lds.wave_sum[wave] = upto;
     __syncthreads();
-    uint32_t before = upto - mine;
-    for (int w = 0; w < wave; ++w) before += lds.wave_sum[w];
+    uint32_t before = upto - mine + sum_before<NT>(lds.wave_sum, wave);
     if (before < (uint32_t)s.left && before + mine >= (uint32_t)s.left) {
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
@@ -88,11 +98,11 @@ __device__ __forceinline__ bool take_digit(SearchLds<NT>& lds, Search& s, int i,
     s.prefix |= lds.found[0] << shift;
     s.mask |= (uint32_t)(digit_bins(i) - 1) << shift;
     s.left -= (int)lds.found[1];
-    return (int)lds.found[2] == s.left;
+    return (int)lds.found[2];
 }
 
 template <int NT>
-__device__ __forceinline__ bool take_digit_from_lds(SearchLds<NT>& lds, Search& s, int i) {
+__device__ __forceinline__ int take_digit_from_lds(SearchLds<NT>& lds, Search& s, int i) {
     constexpr int PER = kBins / NT;
     uint32_t n[PER];
 #pragma unroll
@@ -103,31 +113,140 @@ __device__ __forceinline__ bool take_digit_from_lds(SearchLds<NT>& lds, Search& 
 template <int NT>
 __device__ __forceinline__ void clear_hist(SearchLds<NT>& lds) {
     for (int i = threadIdx.x; i < kBins; i += NT) lds.hist[i] = 0;
+    if (threadIdx.x == 0) lds.listed = 0;
     __syncthreads();
 }
 
-// A line is 64 neighbouring positions, a lane each.  Writes the chosen ones of a line in order and moves on.
-struct Writer {
-    int32_t* keep;
-    int at, same_before;
-    __device__ __forceinline__ void line(const Search& s, int pos, bool always, bool candidate) {
-        const int lane = threadIdx.x & 63;
-        const uint64_t below = (1ull << lane) - 1, same = __ballot(candidate);
-        const bool chosen = always || (candidate && same_before + __popcll(same & below) < s.left);
-        same_before += __popcll(same);
-        const uint64_t m = __ballot(chosen);
-        if (chosen) keep[at + __popcll(m & below)] = pos;
+// Adds the digits of a wave's live lanes to the histogram.  Lanes that share a bin take their turns in LDS, and keys crowd: the held ones
+// are all equal, weights next to nothing are in few bins.  The first live lane counts for all that have its bin (histograms of 24
+// rows of 40K-131K tokens 16.6 us without that, 6.8 with it).
+template <int NT>
+__device__ __forceinline__ void count_digit(SearchLds<NT>& lds, bool live, uint32_t digit) {
+    const uint64_t all = __ballot(live);
+    if (!all) return;
+    const int lane = threadIdx.x & 63, first = __builtin_ctzll(all);
+    const uint32_t common = __builtin_amdgcn_readlane(digit, first);
+    const uint64_t same = __ballot(live && digit == common);
+    if (lane == first || (live && digit != common)) atomicAdd(&lds.hist[digit], lane == first ? (uint32_t)__popcll(same) : 1u);
+}
+
+// The rest of the search, when `count` tokens have the bits found so far, over the keys that each thread holds.
+template <int NT, int VPT>
+__device__ __forceinline__ void finish_search(SearchLds<NT>& lds, Search& s, int count, const uint32_t (&key)[VPT], int lines) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    for (int i = 1; i < kDigits && count != s.left && count > SearchLds<NT>::kList; ++i) {
+        clear_hist(lds);
+        const int shift = digit_shift(i);
+        const uint32_t bins = digit_bins(i) - 1;
+#pragma unroll
+        for (int r = 0; r < VPT; ++r)
+            if (r < lines) count_digit(lds, s.candidate(key[r]), (key[r] >> shift) & bins);
+        __syncthreads();
+        count = take_digit_from_lds<NT>(lds, s, i);
+    }
+    if (count == s.left || s.mask == ~0u) return;  // all of them are chosen, or they are all equal
+    // Few are left: each one's rank among them.  The one with fewer than `left` above it and at least as many not below it is the last
+    // chosen.
+    uint32_t mine = 0;
+#pragma unroll
+    for (int r = 0; r < VPT; ++r)
+        if (r < lines) mine += (uint32_t)__popcll(__ballot(s.candidate(key[r])));
+    uint32_t at = 0;
+    if (lane == 0 && mine) at = atomicAdd(&lds.listed, mine);
+    at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+    for (int r = 0; r < VPT; ++r) {
+        if (r >= lines) continue;
+        const bool c = s.candidate(key[r]);
+        const uint64_t m = __ballot(c);
+        if (c) lds.list[at + lanes_below(m)] = key[r];
+        at += (uint32_t)__popcll(m);
+    }
+    const int padded = (count + 3) & ~3;
+    if (tid < padded - count) lds.list[count + tid] = kNoKey;
+    __syncthreads();
+    if (tid < count) {
+        const uint32_t k = lds.list[tid];
+        int above = 0, same = 0;
+#pragma unroll 4
+        for (int j = 0; j < padded; j += 4) {
+            const u32x4 o = *reinterpret_cast<const u32x4*>(&lds.list[j]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                above += o[e] > k;
+                same += o[e] == k;
+            }
+        }
+        if (above < s.left && above + same >= s.left) {  // every one with this key writes the same
+            lds.found[0] = k;
+            lds.found[1] = (uint32_t)above;
+        }
+    }
+    __syncthreads();
+    s.prefix = lds.found[0];
+    s.mask = ~0u;
+    s.left -= (int)lds.found[1];
+}
+
+// A line is 64 neighbouring positions, a lane each; a wave has `lines` of them from position p0 - lane on.  Writes the wave's chosen tokens in
+// order: `chosen` and `same_before` are how many come in front of them for certain and how many have the last key there.
+template <int NT, int VPT>
+__device__ __forceinline__ void write_chosen(SearchLds<NT>& lds, const Search& s, const uint32_t (&key)[VPT], int lines, int p0, int chosen, int same_before, int32_t* keep) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint64_t above[VPT], same[VPT];
+    uint32_t n_above = 0, n_same = 0;
+#pragma unroll
+    for (int r = 0; r < VPT; ++r) {
+        above[r] = same[r] = 0;
+        if (r < lines) {
+            above[r] = __ballot(s.above(key[r]));
+            same[r] = __ballot(s.candidate(key[r]));
+            n_above += (uint32_t)__popcll(above[r]);
+            n_same += (uint32_t)__popcll(same[r]);
+        }
+    }
+    if (lane == 0) {
+        lds.wave_sum[wave] = n_above;
+        lds.wave_sum2[wave] = n_same;
+    }
+    __syncthreads();
+    same_before += (int)sum_before<NT>(lds.wave_sum2, wave);
+    int at = chosen + (int)sum_before<NT>(lds.wave_sum, wave) + (same_before < s.left ? same_before : s.left);
+#pragma unroll
+    for (int r = 0; r < VPT; ++r) {
+        if (r >= lines) continue;
+        uint64_t m = same[r];
+        const int n = __popcll(m);
+        if (same_before + n > s.left) m = __ballot(__builtin_amdgcn_inverse_ballot_w64(same[r]) && same_before + lanes_below(same[r]) < s.left);
+        same_before += n;
+        m |= above[r];
+        if (__builtin_amdgcn_inverse_ballot_w64(m)) keep[at + lanes_below(m)] = p0 + r * 64;
         at += __popcll(m);
     }
-};
+}
+
+// Keys of a thread's lines, from position p0 on.
+template <int VPT>
+__device__ __forceinline__ void load_keys(const float* w, int len, int sinks, int recent, int p0, int lines, uint32_t (&key)[VPT]) {
+    float v[VPT];
+#pragma unroll
+    for (int r = 0; r < VPT; ++r) {
+        const int pos = p0 + r * 64;
+        v[r] = 0.f;
+        if (r < lines && pos < len) v[r] = w[pos];
+    }
+#pragma unroll
+    for (int r = 0; r < VPT; ++r) {
+        const int pos = p0 + r * 64;
+        key[r] = pos >= len ? kNoKey : pos < sinks || pos >= len - recent ? kHeldKey : weight_key(v[r]);
+    }
+}
 
 // One workgroup to a sequence and KV head, whose weights it reads once and holds in registers: wave w has the lines w * lines ..
 // (w + 1) * lines - 1, at most VPT of them.
 template <int NT, int VPT>
 __global__ __launch_bounds__(NT) void ppd_select_kernel(const SelectParams P) {
-    constexpr int NW = NT / 64;
     __shared__ SearchLds<NT> lds;
-    __shared__ int n_above[NW], n_same[NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int b = blockIdx.y, head = blockIdx.x, len = P.length[b];
     const float* w = P.weights + ((int64_t)b * P.Hkv + head) * P.weight_stride;
@@ -136,247 +255,186 @@ __global__ __launch_bounds__(NT) void ppd_select_kernel(const SelectParams P) {
         for (int t = tid; t < len; t += NT) keep[t] = t;
         return;
     }
-    const int lo = P.sinks, hi = len - P.recent;  // the others: positions [lo, hi)
-    const int lines = ((len + 63) / 64 + NW - 1) / NW;
+    const int lines = ((len + 63) / 64 + NT / 64 - 1) / (NT / 64);
     const int p0 = wave * lines * 64 + lane;
     uint32_t key[VPT];
-#pragma unroll
-    for (int r = 0; r < VPT; ++r) {
-        const int pos = p0 + r * 64;
-        key[r] = 0;
-        if (r < lines && pos >= lo && pos < hi) key[r] = __builtin_bit_cast(uint32_t, w[pos]);
-    }
-#pragma unroll
-    for (int r = 0; r < VPT; ++r) key[r] = weight_key(__builtin_bit_cast(float, key[r]));
+    load_keys(w, len, P.sinks, P.recent, p0, lines, key);
     Search s;
-    s.left = P.budget - P.sinks - P.recent;
-    const bool search = s.left > 0;
-    if (search) {
-        for (int i = 0; i < kDigits; ++i) {
-            clear_hist(lds);
-            const int shift = digit_shift(i);
-            const uint32_t bins = digit_bins(i) - 1;
+    s.left = P.budget;
+    clear_hist(lds);
 #pragma unroll
-            for (int r = 0; r < VPT; ++r) {
-                const int pos = p0 + r * 64;
-                if (r < lines) count_digit(lds.hist, pos >= lo && pos < hi && s.candidate(key[r]), (key[r] >> shift) & bins);
-            }
-            __syncthreads();
-            if (take_digit_from_lds<NT>(lds, s, i)) break;
-        }
-    }
-    int above = 0, same = 0;
-#pragma unroll
-    for (int r = 0; r < VPT; ++r) {
-        const int pos = p0 + r * 64;
-        if (r < lines) {
-            const bool other = pos >= lo && pos < hi;
-            above += __popcll(__ballot(pos < len && (!other || (search && s.above(key[r])))));
-            same += __popcll(__ballot(other && search && s.candidate(key[r])));
-        }
-    }
-    if (lane == 0) {
-        n_above[wave] = above;
-        n_same[wave] = same;
-    }
+    for (int r = 0; r < VPT; ++r)
+        if (r < lines) count_digit(lds, true, key[r] >> digit_shift(0));
     __syncthreads();
-    Writer out{keep, 0, 0};
-    for (int i = 0; i < wave; ++i) {
-        out.at += n_above[i];
-        out.same_before += n_same[i];
-    }
-    out.at += out.same_before < s.left ? out.same_before : s.left;
-#pragma unroll
-    for (int r = 0; r < VPT; ++r) {
-        const int pos = p0 + r * 64;
-        if (r < lines) {
-            const bool other = pos >= lo && pos < hi;
-            out.line(s, pos, pos < len && (!other || (search && s.above(key[r]))), other && search && s.candidate(key[r]));
-        }
-    }
+    const int count = take_digit_from_lds<NT>(lds, s, 0);
+    finish_search(lds, s, count, key, lines);
+    write_chosen(lds, s, key, lines, p0, 0, 0, keep);
 }
 
 // Longer rows are cut into chunks of kSelectChunk positions, a workgroup each, in three launches: the first leaves every chunk's
-// histogram of the first digit; the second finds that digit from all of the row's, and leaves every chunk's candidates (the
-// tokens that have it) and how many are above them; the third finds the rest from the candidates of all chunks, which every
-// chunk's workgroup reads for itself, and writes its chunk.
+// histogram of the upper bits; the second finds the bits from all of the row's, and leaves the row's candidates (the tokens that
+// have them) and how many are above them in every chunk; the third finds the rest from the candidates, which every chunk's
+// workgroup reads for itself, and writes its chunk.
 constexpr int kChunkThreads = 1024, kChunkLines = kSelectChunk / kChunkThreads;
 static_assert(kChunkLines * kChunkThreads == kSelectChunk, "whole lines");
 
 struct ChunkRow {  // what a chunk's workgroup knows of its row
-    int row, chunk, len, lo, hi, chunks;
+    int row, chunk, len, chunks, p0;
     const float* w;
+    int32_t* counts;  // the row's: candidates, the bits found, how many are chosen of them; then per chunk how many are above
 };
 __device__ __forceinline__ ChunkRow chunk_row(const SelectParams& P) {
     ChunkRow c;
     c.row = blockIdx.x / P.max_chunks;
     c.chunk = blockIdx.x % P.max_chunks;
     c.len = P.length[c.row / P.Hkv];
-    c.lo = P.sinks;
-    c.hi = c.len - P.recent;
     c.chunks = (c.len + kSelectChunk - 1) / kSelectChunk;
+    c.p0 = c.chunk * kSelectChunk + (int)(threadIdx.x >> 6) * (kChunkLines * 64) + (int)(threadIdx.x & 63);
     c.w = P.weights + (int64_t)c.row * P.weight_stride;
+    c.counts = P.counts + (int64_t)c.row * (P.max_chunks + kSelectRowWords);
     return c;
-}
-// Keys of this thread's lines of the chunk, and which of them are others (neither first nor last ones).
-__device__ __forceinline__ void chunk_keys(const ChunkRow& c, uint32_t (&key)[kChunkLines], bool (&other)[kChunkLines], int (&pos)[kChunkLines]) {
-    const int p0 = c.chunk * kSelectChunk + (int)(threadIdx.x >> 6) * (kChunkLines * 64) + (int)(threadIdx.x & 63);
-#pragma unroll
-    for (int r = 0; r < kChunkLines; ++r) {
-        pos[r] = p0 + r * 64;
-        other[r] = pos[r] >= c.lo && pos[r] < c.hi;
-        key[r] = other[r] ? __builtin_bit_cast(uint32_t, c.w[pos[r]]) : 0;
-    }
-#pragma unroll
-    for (int r = 0; r < kChunkLines; ++r) key[r] = weight_key(__builtin_bit_cast(float, key[r]));
-}
-// The first digit, from the histograms of the row's chunks.
-__device__ __forceinline__ bool first_digit(const SelectParams& P, const ChunkRow& c, SearchLds<kChunkThreads>& lds, Search& s) {
-    constexpr int PER = kBins / kChunkThreads;
-    uint32_t n[PER] = {};
-    const uint32_t* h = P.hist + (int64_t)c.row * P.max_chunks * kBins + kBins - 1 - threadIdx.x * PER;
-    for (int k = 0; k < c.chunks; ++k)
-#pragma unroll
-        for (int j = 0; j < PER; ++j) n[j] += h[(int64_t)k * kBins - j];
-    return take_digit<kChunkThreads>(lds, s, 0, n);
 }
 
 __global__ __launch_bounds__(kChunkThreads) void ppd_select_digits_kernel(const SelectParams P) {
     __shared__ SearchLds<kChunkThreads> lds;
     const ChunkRow c = chunk_row(P);
-    if (c.chunk >= c.chunks || c.len <= P.budget || P.budget == P.sinks + P.recent) return;
+    if (c.chunk >= c.chunks || c.len <= P.budget) return;
     uint32_t key[kChunkLines];
-    bool other[kChunkLines];
-    int pos[kChunkLines];
-    chunk_keys(c, key, other, pos);
+    load_keys(c.w, c.len, P.sinks, P.recent, c.p0, kChunkLines, key);
     clear_hist(lds);
 #pragma unroll
-    for (int r = 0; r < kChunkLines; ++r) count_digit(lds.hist, other[r], key[r] >> digit_shift(0));
+    for (int r = 0; r < kChunkLines; ++r) count_digit(lds, true, key[r] >> digit_shift(0));
+    if (c.chunk == 0 && threadIdx.x == 0) c.counts[0] = 0;
     __syncthreads();
     uint32_t* h = P.hist + ((int64_t)c.row * P.max_chunks + c.chunk) * kBins;
     for (int i = threadIdx.x; i < kBins; i += kChunkThreads) h[i] = lds.hist[i];
 }
 
 __global__ __launch_bounds__(kChunkThreads) void ppd_select_candidates_kernel(const SelectParams P) {
-    constexpr int NW = kChunkThreads / 64;
+    constexpr int PER = kBins / kChunkThreads;
     __shared__ SearchLds<kChunkThreads> lds;
-    __shared__ int n_above[NW], n_same[NW];
+    __shared__ int above, same, list_at;
     const ChunkRow c = chunk_row(P);
     if (c.chunk >= c.chunks || c.len <= P.budget) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Search s;
-    s.left = P.budget - P.sinks - P.recent;
-    const bool search = s.left > 0;
+    const int lane = threadIdx.x & 63;
     uint32_t key[kChunkLines];
-    bool other[kChunkLines];
-    int pos[kChunkLines];
-    chunk_keys(c, key, other, pos);
-    if (search) first_digit(P, c, lds, s);
-    int above = 0, same = 0;
+    load_keys(c.w, c.len, P.sinks, P.recent, c.p0, kChunkLines, key);
+    Search s;
+    s.left = P.budget;
+    uint32_t n[PER] = {};
+    const uint32_t* h = P.hist + (int64_t)c.row * P.max_chunks * kBins + kBins - 1 - threadIdx.x * PER;
+#pragma unroll 4
+    for (int k = 0; k < c.chunks; ++k)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) n[j] += h[(int64_t)k * kBins - j];
+    if (threadIdx.x == 0) above = same = 0;
+    const int count = take_digit<kChunkThreads>(lds, s, 0, n);
+    int n_above = 0, n_same = 0;
 #pragma unroll
     for (int r = 0; r < kChunkLines; ++r) {
-        above += __popcll(__ballot(pos[r] < c.len && (!other[r] || (search && s.above(key[r])))));
-        same += __popcll(__ballot(other[r] && search && s.candidate(key[r])));
+        n_above += __popcll(__ballot(s.above(key[r])));
+        n_same += __popcll(__ballot(s.candidate(key[r])));
     }
+    int at = 0;
     if (lane == 0) {
-        n_above[wave] = above;
-        n_same[wave] = same;
+        atomicAdd(&above, n_above);
+        at = atomicAdd(&same, n_same);
     }
     __syncthreads();
-    int at = 0;
-    for (int i = 0; i < wave; ++i) at += n_same[i];
-    const int64_t mine = (int64_t)c.row * P.max_chunks + c.chunk;
-    uint32_t* list = P.candidates + mine * kSelectChunk;
+    if (threadIdx.x == 0) {
+        list_at = atomicAdd(&c.counts[0], same);  // the candidates' order does not matter
+        c.counts[kSelectRowWords + c.chunk] = above;
+        if (c.chunk == 0) {
+            c.counts[1] = (int)s.prefix;
+            c.counts[2] = s.left;
+            c.counts[3] = count;
+        }
+    }
+    __syncthreads();
+    at = __builtin_amdgcn_readfirstlane(at) + list_at;
+    u32x2* list = reinterpret_cast<u32x2*>(P.candidates) + (int64_t)c.row * P.max_chunks * kSelectChunk;
 #pragma unroll
     for (int r = 0; r < kChunkLines; ++r) {
-        const bool cand = other[r] && search && s.candidate(key[r]);
+        const bool cand = s.candidate(key[r]);
         const uint64_t m = __ballot(cand);
-        if (cand) list[at + __popcll(m & ((1ull << lane) - 1))] = key[r];
+        if (cand) list[at + lanes_below(m)] = u32x2{key[r], (uint32_t)c.chunk};
         at += __popcll(m);
-    }
-    if (threadIdx.x == 0) {
-        int total_above = 0, total_same = 0;
-        for (int i = 0; i < NW; ++i) {
-            total_above += n_above[i];
-            total_same += n_same[i];
-        }
-        P.counts[mine * 2] = total_above;
-        P.counts[mine * 2 + 1] = total_same;
     }
 }
 
 __global__ __launch_bounds__(kChunkThreads) void ppd_select_finish_kernel(const SelectParams P) {
-    constexpr int NW = kChunkThreads / 64;
     __shared__ SearchLds<kChunkThreads> lds;
-    __shared__ int n_above[NW], n_same[NW], before[2];
+    __shared__ int before[2];
     const ChunkRow c = chunk_row(P);
     if (c.chunk >= c.chunks) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
     int32_t* keep = P.keep + (int64_t)c.row * P.keep_stride;
     if (c.len <= P.budget) {
         for (int t = c.chunk * kSelectChunk + tid; t < c.len && t < (c.chunk + 1) * kSelectChunk; t += kChunkThreads) keep[t] = t;
         return;
     }
     Search s;
-    s.left = P.budget - P.sinks - P.recent;
-    const bool search = s.left > 0;
+    s.prefix = (uint32_t)c.counts[1];
+    s.mask = (uint32_t)(digit_bins(0) - 1) << digit_shift(0);
+    s.left = c.counts[2];
+    int count = c.counts[3];
     uint32_t key[kChunkLines];
-    bool other[kChunkLines];
-    int pos[kChunkLines];
-    chunk_keys(c, key, other, pos);
-    const int64_t first = (int64_t)c.row * P.max_chunks;
-    bool all = !search || first_digit(P, c, lds, s);
-    auto each_candidate = [&](int chunks, auto f) {  // f(live, key) for the candidates of the first `chunks` chunks, by whole waves
-        for (int k = 0; k < chunks; ++k) {
-            const int n = P.counts[(first + k) * 2 + 1];
-            const uint32_t* list = P.candidates + (first + k) * kSelectChunk;
-            for (int i = wave * 64; i < n; i += kChunkThreads) f(i + lane < n, i + lane < n ? list[i + lane] : 0u);
-        }
-    };
-    for (int i = 1; i < kDigits && !all; ++i) {
-        clear_hist(lds);
-        const int shift = digit_shift(i);
-        const uint32_t bins = digit_bins(i) - 1;
-        each_candidate(c.chunks, [&](bool live, uint32_t k) { count_digit(lds.hist, live && s.candidate(k), (k >> shift) & bins); });
-        __syncthreads();
-        all = take_digit_from_lds<kChunkThreads>(lds, s, i);
-    }
-    // how many are chosen for certain, and how many have the last weight, in the chunks in front: counted above the first digit there, the
-    // rest among their candidates
-    if (tid < 2) before[tid] = 0;
-    __syncthreads();
-    {
-        int above = 0, same = 0;
-        if (search)
-            each_candidate(c.chunk, [&](bool live, uint32_t k) {
-                above += __popcll(__ballot(live && s.above(k)));
-                same += __popcll(__ballot(live && s.candidate(k)));
-            });
-        if (tid < c.chunk) atomicAdd(&before[0], P.counts[(first + tid) * 2]);
-        for (int k = tid + kChunkThreads; k < c.chunk; k += kChunkThreads) atomicAdd(&before[0], P.counts[(first + k) * 2]);
-        if (lane == 0 && above) atomicAdd(&before[0], above);
-        if (lane == 0 && same) atomicAdd(&before[1], same);
-    }
-    int above = 0, same = 0;
+    load_keys(c.w, c.len, P.sinks, P.recent, c.p0, kChunkLines, key);
+    const u32x2* list = reinterpret_cast<const u32x2*>(P.candidates) + (int64_t)c.row * P.max_chunks * kSelectChunk;
+    const int total = count;
+    // the candidates, kChunkLines to a thread where they fit, or again and again from the list
+    uint32_t cand[kChunkLines];
+    uint64_t front[kChunkLines];  // which of them are in chunks in front of this one
+    const bool held = total <= kSelectChunk;
+    const int lines = held ? (total + kChunkThreads - 1) / kChunkThreads : 0;
 #pragma unroll
     for (int r = 0; r < kChunkLines; ++r) {
-        above += __popcll(__ballot(pos[r] < c.len && (!other[r] || (search && s.above(key[r])))));
-        same += __popcll(__ballot(other[r] && search && s.candidate(key[r])));
+        const int i = r * kChunkThreads + tid;
+        u32x2 v = {kNoKey, ~0u};
+        if (r < lines && i < total) v = list[i];
+        cand[r] = v[0];
+        front[r] = __ballot(v[1] < (uint32_t)c.chunk);
     }
-    if (lane == 0) {
-        n_above[wave] = above;
-        n_same[wave] = same;
+    if (tid < 2) before[tid] = 0;
+    if (tid == 0) lds.listed = 0;
+    __syncthreads();
+    if (held) {
+        finish_search(lds, s, count, cand, lines);
+    } else {
+        for (int i = 1; i < kDigits && count != s.left; ++i) {
+            clear_hist(lds);
+            for (int t0 = tid - lane; t0 < total; t0 += kChunkThreads) {
+                const uint32_t k = t0 + lane < total ? list[t0 + lane][0] : kNoKey;
+                count_digit(lds, s.candidate(k), (k >> digit_shift(i)) & (digit_bins(i) - 1));
+            }
+            __syncthreads();
+            count = take_digit_from_lds<kChunkThreads>(lds, s, i);
+        }
     }
     __syncthreads();
-    Writer out{keep, before[0], before[1]};
-    for (int i = 0; i < wave; ++i) {
-        out.at += n_above[i];
-        out.same_before += n_same[i];
-    }
-    out.at += out.same_before < s.left ? out.same_before : s.left;
+    // how many are chosen for certain, and how many have the last key, in the chunks in front: those above the upper bits were counted there,
+    // the rest is among the candidates
+    int above = 0, same = 0;
+    if (held) {
 #pragma unroll
-    for (int r = 0; r < kChunkLines; ++r)
-        out.line(s, pos[r], pos[r] < c.len && (!other[r] || (search && s.above(key[r]))), other[r] && search && s.candidate(key[r]));
+        for (int r = 0; r < kChunkLines; ++r) {
+            if (r >= lines) continue;
+            above += __popcll(__ballot(s.above(cand[r])) & front[r]);
+            same += __popcll(__ballot(s.candidate(cand[r])) & front[r]);
+        }
+    } else {
+        for (int t0 = tid - lane; t0 < total; t0 += kChunkThreads) {
+            const u32x2 v = t0 + lane < total ? list[t0 + lane] : u32x2{kNoKey, ~0u};
+            above += __popcll(__ballot(v[1] < (uint32_t)c.chunk && s.above(v[0])));
+            same += __popcll(__ballot(v[1] < (uint32_t)c.chunk && s.candidate(v[0])));
+        }
+    }
+    if (lane == 0 && above) atomicAdd(&before[0], above);
+    if (lane == 0 && same) atomicAdd(&before[1], same);
+    for (int k = tid; k < c.chunk; k += kChunkThreads) atomicAdd(&before[0], c.counts[kSelectRowWords + k]);
+    __syncthreads();
+    const int chosen = before[0], same_before = before[1];
+    write_chosen(lds, s, key, kChunkLines, c.p0, chosen, same_before, keep);
 }
 
 int launch_select(const SelectParams& p, int longest, void* stream) {

@@ -21,6 +21,7 @@ constexpr int kWeighKeys = 256;      // keys of a workgroup that adds up attenti
 constexpr int kSelectBatch = 512;    // sequences per launch of the select kernel (their lengths are kernel arguments)
 constexpr int kSelectChunk = 16384;  // weights that a workgroup of the select kernels holds in registers
 constexpr int kSelectBins = 2048;    // of the chunks' histograms
+constexpr int kSelectRowWords = 4;   // of a row's counts, in front of its chunks'
 constexpr int kCompactBatch = 256;   // the same for the move (two lists)
 
 // A tile of tree attention: all `ncols` query columns of one sequence and KV head (row-major over the G heads of the group), at most
@@ -108,8 +109,8 @@ struct SelectParams {
     int64_t weight_stride, keep_stride;
     int32_t Hkv, budget, sinks, recent;
     int32_t B;
-    // rows longer than kSelectChunk: chunks of the longest (0: none is longer), and per row and chunk the histogram, the candidates and
-    // (tokens above them, candidates)
+    // rows longer than kSelectChunk: chunks of the longest (0: none is longer), every chunk's histogram, every row's candidates (key and
+    // chunk) and counts
     int32_t max_chunks;
     uint32_t *hist, *candidates;
     int32_t* counts;

@@ -277,11 +277,11 @@ ppd_status select_workspace(ppd_ctx* ctx, ppd::SelectParams* p, int32_t longest,
     ppd_status st = tree_state(ctx, &t);
     if (st != PPD_OK) return st;
     p->max_chunks = (longest + ppd::kSelectChunk - 1) / ppd::kSelectChunk;
-    const size_t chunks = (size_t)p->B * p->Hkv * p->max_chunks, words = (size_t)ppd::kSelectBins + ppd::kSelectChunk + 2;
+    const size_t rows = (size_t)p->B * p->Hkv, chunks = rows * p->max_chunks;
     if (chunks > (size_t)INT32_MAX) return fail(ctx, PPD_ERR_RANGE, "more rows of this length than one launch takes");
     hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
     PPD_HIP(ctx, hipStreamIsCapturing(hs, &capturing));
-    const size_t bytes = chunks * words * sizeof(uint32_t);
+    const size_t bytes = (chunks * (ppd::kSelectBins + 2 * ppd::kSelectChunk) + rows * (p->max_chunks + ppd::kSelectRowWords)) * sizeof(uint32_t);
     if (capturing == hipStreamCaptureStatusNone) {
         st = follow_stream(ctx, hs);
         if (st == PPD_OK) st = grow_device(ctx, &t->d_select, &t->d_select_bytes, bytes, hs);
@@ -291,7 +291,7 @@ ppd_status select_workspace(ppd_ctx* ctx, ppd::SelectParams* p, int32_t longest,
     }
     p->hist = static_cast<uint32_t*>(t->d_select);
     p->candidates = p->hist + chunks * ppd::kSelectBins;
-    p->counts = reinterpret_cast<int32_t*>(p->candidates + chunks * ppd::kSelectChunk);
+    p->counts = reinterpret_cast<int32_t*>(p->candidates + chunks * 2 * ppd::kSelectChunk);
     return PPD_OK;
 }
 
