@@ -56,17 +56,22 @@ struct SearchLds {
     static constexpr int kList = 64;  // candidates that are ranked, at most
     uint32_t hist[kBins];
     __attribute__((aligned(16))) uint32_t list[kList];
-    uint32_t wave_sum[NT / 64], wave_sum2[NT / 64];
+    uint32_t wave_sum[NT / 64];
     uint32_t listed;
     uint32_t found[3];  // digit, tokens above it, tokens of it
 };
 
+// Sum of the values of the waves in front.
 template <int NT>
-__device__ __forceinline__ uint32_t sum_before(const uint32_t (&v)[NT / 64], int wave) {  // all reads at once
-    uint32_t s = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) s += w < wave ? v[w] : 0u;
-    return s;
+__device__ __forceinline__ uint32_t sum_before(const uint32_t (&v)[NT / 64], int wave) {
+    static_assert(NT <= 1024, "the waves' values fit a row of 16 lanes");
+    const int lane = threadIdx.x & 63;
+    uint32_t x = lane < NT / 64 && lane < wave ? v[lane & (NT / 64 - 1)] : 0u;
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    return __builtin_amdgcn_readlane(x, 15);
 }
 
 // Thread t has the bins kBins - 1 - t * PER .. (heaviest first); the one in which the running count reaches `left` is the digit.  All threads
@@ -149,14 +154,12 @@ __device__ __forceinline__ void finish_search(SearchLds<NT>& lds, Search& s, int
     // chosen.
     uint32_t mine = 0;
 #pragma unroll
-    for (int r = 0; r < VPT; ++r)
-        if (r < lines) mine += (uint32_t)__popcll(__ballot(s.candidate(key[r])));
+    for (int r = 0; r < VPT; ++r) mine += (uint32_t)__popcll(__ballot(s.candidate(key[r])));
     uint32_t at = 0;
     if (lane == 0 && mine) at = atomicAdd(&lds.listed, mine);
     at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
     for (int r = 0; r < VPT; ++r) {
-        if (r >= lines) continue;
         const bool c = s.candidate(key[r]);
         const uint64_t m = __ballot(c);
         if (c) lds.list[at + lanes_below(m)] = key[r];
@@ -188,33 +191,28 @@ __device__ __forceinline__ void finish_search(SearchLds<NT>& lds, Search& s, int
     s.left -= (int)lds.found[1];
 }
 
-// A line is 64 neighbouring positions, a lane each; a wave has `lines` of them from position p0 - lane on.  Writes the wave's chosen tokens in
+// A line is 64 neighbouring positions, a lane each; a wave has VPT of them from position p0 - lane on.  Writes the wave's chosen tokens in
 // order: `chosen` and `same_before` are how many come in front of them for certain and how many have the last key there.
 template <int NT, int VPT>
-__device__ __forceinline__ void write_chosen(SearchLds<NT>& lds, const Search& s, const uint32_t (&key)[VPT], int lines, int p0, int chosen, int same_before, int32_t* keep) {
+__device__ __forceinline__ void write_chosen(SearchLds<NT>& lds, const Search& s, const uint32_t (&key)[VPT], int p0, int chosen, int same_before, int32_t* keep) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint64_t above[VPT], same[VPT];
     uint32_t n_above = 0, n_same = 0;
 #pragma unroll
     for (int r = 0; r < VPT; ++r) {
-        above[r] = same[r] = 0;
-        if (r < lines) {
-            above[r] = __ballot(s.above(key[r]));
-            same[r] = __ballot(s.candidate(key[r]));
-            n_above += (uint32_t)__popcll(above[r]);
-            n_same += (uint32_t)__popcll(same[r]);
-        }
+        above[r] = __ballot(s.above(key[r]));
+        same[r] = __ballot(s.candidate(key[r]));
+        n_above += (uint32_t)__popcll(above[r]);
+        n_same += (uint32_t)__popcll(same[r]);
     }
-    if (lane == 0) {
-        lds.wave_sum[wave] = n_above;
-        lds.wave_sum2[wave] = n_same;
-    }
+    static_assert(NT * VPT <= 65535, "both counts fit a word");
+    if (lane == 0) lds.wave_sum[wave] = n_above | n_same << 16;
     __syncthreads();
-    same_before += (int)sum_before<NT>(lds.wave_sum2, wave);
-    int at = chosen + (int)sum_before<NT>(lds.wave_sum, wave) + (same_before < s.left ? same_before : s.left);
+    const uint32_t front = sum_before<NT>(lds.wave_sum, wave);
+    same_before += (int)(front >> 16);
+    int at = chosen + (int)(front & 0xFFFFu) + (same_before < s.left ? same_before : s.left);
 #pragma unroll
     for (int r = 0; r < VPT; ++r) {
-        if (r >= lines) continue;
         uint64_t m = same[r];
         const int n = __popcll(m);
         if (same_before + n > s.left) m = __ballot(__builtin_amdgcn_inverse_ballot_w64(same[r]) && same_before + lanes_below(same[r]) < s.left);
@@ -238,7 +236,7 @@ __device__ __forceinline__ void load_keys(const float* w, int len, int sinks, in
 #pragma unroll
     for (int r = 0; r < VPT; ++r) {
         const int pos = p0 + r * 64;
-        key[r] = pos >= len ? kNoKey : pos < sinks || pos >= len - recent ? kHeldKey : weight_key(v[r]);
+        key[r] = r >= lines || pos >= len ? kNoKey : pos < sinks || pos >= len - recent ? kHeldKey : weight_key(v[r]);
     }
 }
 
@@ -268,7 +266,7 @@ __global__ __launch_bounds__(NT) void ppd_select_kernel(const SelectParams P) {
     __syncthreads();
     const int count = take_digit_from_lds<NT>(lds, s, 0);
     finish_search(lds, s, count, key, lines);
-    write_chosen(lds, s, key, lines, p0, 0, 0, keep);
+    write_chosen(lds, s, key, p0, 0, 0, keep);
 }
 
 // Longer rows are cut into chunks of kSelectChunk positions, a workgroup each, in three launches: the first leaves every chunk's
@@ -434,7 +432,7 @@ __global__ __launch_bounds__(kChunkThreads) void ppd_select_finish_kernel(const 
     for (int k = tid; k < c.chunk; k += kChunkThreads) atomicAdd(&before[0], c.counts[kSelectRowWords + k]);
     __syncthreads();
     const int chosen = before[0], same_before = before[1];
-    write_chosen(lds, s, key, kChunkLines, c.p0, chosen, same_before, keep);
+    write_chosen(lds, s, key, c.p0, chosen, same_before, keep);
 }
 
 int launch_select(const SelectParams& p, int longest, void* stream) {
