@@ -451,122 +451,127 @@ int launch_select(const SelectParams& p, int longest, void* stream) {
     return (int)hipGetLastError();
 }
 
-// Moves token keep[i] of one sequence, KV head and layer to position first + i, in place.  The lists ascend and keep[i] >= first + i, so
-// a destination is never read by a later token: a workgroup takes 128 destinations at a time, reads all of them, waits, and
-// writes.  The d axis of K and of V is independent, so K, V and slices of d are workgroups of their own; the weights are another.
-// Entries that do not ascend or lie outside the sequence's pages raise the sticky flag, and their tokens stay where they are.
-constexpr int kCompactThreads = 256, kCompactStep = 128;
+// ---- the move -----------------------------------------------------------------------------------------------
+// Token keep[i] of a sequence, KV head and layer goes to position first + i, in place.  The lists ascend and keep[i] >= first + i, so a
+// destination is never read by a later token: a workgroup takes kMoves destinations at a time -- `P.step` positions of as many heads as
+// that leaves room for -- reads all of them, waits, and writes.  Every d is independent, so K, V and slices of d are workgroups of their
+// own; the weights are another.  Entries that do not ascend or lie outside the sequence's pages raise the sticky flag, and their
+// tokens stay where they are.
+// Bound by memory where lists are long: a K token is 16-byte granules, but V's granules hold 8 tokens of one d, which come from up to
+// eight places, so all of V is read where every eighth token is kept.  Short lists (the accepted path of a tree) are a chain of
+// reads, list, page, token; there one workgroup takes all heads.
+constexpr int kCompactThreads = 256, kMoves = 128, kUnits = 4;  // units (granules) a thread moves at a time
+constexpr int kCompactWidth = kUnits * kCompactThreads * 8 / kMoves;  // d of a slice
 
 template <int HD, bool FP8>
 __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const CompactParams P) {
     typedef std::conditional_t<FP8, uint8_t, uint16_t> Elem;
     typedef std::conditional_t<FP8, u32x2, u32x4> Raw;  // eight elements
-    __shared__ int64_t from[kCompactStep], to[kCompactStep];  // element offset of the page block of a token, -1: it stays
-    __shared__ int from_tok[kCompactStep];
+    constexpr int WIDTH = HD < kCompactWidth ? HD : kCompactWidth, SLICES = HD / WIDTH;
+    __shared__ int64_t from[kMoves], to[kMoves];  // element offset of a move's page block, -1: it stays
+    __shared__ int from_tok[kMoves], to_tok[kMoves];
     const int tid = threadIdx.x;
-    const int b = blockIdx.x / P.Hkv, head = blockIdx.x % P.Hkv, layer = blockIdx.z;
-    const int first = P.first[b], count = P.count[b];
-    const int32_t* keep = P.keep + layer * P.keep_layer + b * P.keep_seq + head * P.keep_head;
+    const int heads = kMoves / P.step, groups = (P.Hkv + heads - 1) / heads;
+    const int b = blockIdx.x / groups, head0 = blockIdx.x % groups * heads, layer = blockIdx.z;
+    const int first = P.first[b], end = first + P.count[b];
+    const int part = blockIdx.y;  // K slices, V slices, weights
+    const bool is_weights = part == 2 * SLICES, is_v = part >= SLICES;
+    const int d0 = part % SLICES * WIDTH;
     const int32_t* pages = P.page_tables + (int64_t)b * P.max_pages;
     int64_t capacity = (int64_t)P.max_pages * kPage;
     if (P.weights && P.weight_stride < capacity) capacity = P.weight_stride;
-    const int part = blockIdx.y;  // K slices, V slices, weights
-    const int start = first & ~7, end = first + count;  // steps begin on a granule of V
-    Elem* const pool = static_cast<Elem*>(P.pool) + layer * P.pool_layer + (int64_t)head * (kPage * HD);
-    float* const weights = P.weights ? P.weights + layer * P.weight_layer + ((int64_t)b * P.Hkv + head) * P.weight_stride : nullptr;
-    const bool is_weights = part == 2 * P.slices, is_v = part >= P.slices;
-    const int width = HD / P.slices, d0 = (part % P.slices) * width;
+    // thread t < kMoves looks up move t: position p0 + t % step of head head0 + t / step
+    const int head = head0 + tid / P.step;
+    const bool looks = tid < kMoves && head < P.Hkv;
+    const int32_t* keep = P.keep + layer * P.keep_layer + b * P.keep_seq + (looks ? head : head0) * P.keep_head;
+    float* const weights = P.weights ? P.weights + layer * P.weight_layer + ((int64_t)b * P.Hkv + (looks ? head : head0)) * P.weight_stride : nullptr;
+    Elem* const pool = static_cast<Elem*>(P.pool) + layer * P.pool_layer + (is_v ? (int64_t)P.Hkv * (kPage * HD) : 0);
 
-    auto source = [&](int pos) {  // of destination `pos`, -1 where there is none
-        const int i = pos - first;
-        if (i < 0 || pos >= end) return -1;
-        const int src = keep[i];
-        if (src < pos || src >= capacity || (i > 0 && keep[i - 1] >= src)) {
-            atomicOr(P.err_flags, 8u);
-            return -1;
-        }
-        return src;
-    };
     auto page_base = [&](int pos) {
         int id = pages[pos >> 4];
         if (id < 0 || id >= P.num_pages) {
             atomicOr(P.err_flags, 2u);
             return (int64_t)-1;
         }
-        return id * P.page_stride;
+        return id * P.page_stride + head * (kPage * HD);
     };
 
-    for (int p0 = start; p0 < end; p0 += kCompactStep) {
+    for (int p0 = first & ~7; p0 < end; p0 += P.step) {  // steps begin on a granule of V
+        const int pos = p0 + tid % P.step, i = pos - first;
+        int src = -1;
+        if (looks && i >= 0 && pos < end) {
+            src = keep[i];
+            const int previous = i > 0 ? keep[i - 1] : -1;
+            if (src < pos || src >= capacity || previous >= src) {
+                atomicOr(P.err_flags, 8u);
+                src = -1;
+            }
+        }
         if (is_weights) {
-            const int src = tid < kCompactStep ? source(p0 + tid) : -1;
             float v = 0.f;
             if (src >= 0) v = weights[src];
             asm volatile("s_waitcnt vmcnt(0)" : "+v"(v) : : "memory");
             __syncthreads();
-            if (src >= 0) weights[p0 + tid] = v;
+            if (src >= 0) weights[pos] = v;
             continue;
         }
+        int64_t f = -1, t = -1;
+        if (src >= 0) {
+            f = page_base(src);
+            t = page_base(pos);
+        }
+        const bool moves = f >= 0 && t >= 0;
         __syncthreads();  // the lists of the step before are read
-        if (tid < kCompactStep) {
-            const int src = source(p0 + tid);
-            int64_t f = -1, t = -1;
-            if (src >= 0) {
-                f = page_base(src);
-                t = page_base(p0 + tid);
-            }
-            from[tid] = t < 0 ? -1 : f;
-            to[tid] = f < 0 ? -1 : t;
+        if (tid < kMoves) {
+            from[tid] = moves ? f : -1;
+            to[tid] = moves ? t : -1;
             from_tok[tid] = src & 15;
+            to_tok[tid] = pos & 15;
         }
         __syncthreads();
         if (!is_v) {
-            constexpr int PER = kCompactStep * (HD / 8) / kCompactThreads;
-            const int units = kCompactStep * (width / 8);
-            Raw v[PER];
+            Raw v[kUnits];
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const int u = tid + j * kCompactThreads, t = u % kCompactStep, g = d0 / 8 + u / kCompactStep;
+            for (int j = 0; j < kUnits; ++j) {
+                const int u = tid + j * kCompactThreads, m = u % kMoves, g = d0 / 8 + u / kMoves;
                 v[j] = Raw{};
-                if (u < units && from[t] >= 0) v[j] = *reinterpret_cast<const Raw*>(pool + from[t] + (g * kPage + from_tok[t]) * 8);
+                if (u < kMoves * (WIDTH / 8) && from[m] >= 0) v[j] = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(pool + from[m] + (g * kPage + from_tok[m]) * 8));
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const int u = tid + j * kCompactThreads, t = u % kCompactStep, g = d0 / 8 + u / kCompactStep;
-                if (u < units && to[t] >= 0) *reinterpret_cast<Raw*>(pool + to[t] + (g * kPage + ((p0 + t) & 15)) * 8) = v[j];
+            for (int j = 0; j < kUnits; ++j) {
+                const int u = tid + j * kCompactThreads, m = u % kMoves, g = d0 / 8 + u / kMoves;
+                if (u < kMoves * (WIDTH / 8) && to[m] >= 0) *reinterpret_cast<Raw*>(pool + to[m] + (g * kPage + to_tok[m]) * 8) = v[j];
             }
         } else {
-            constexpr int PER = kCompactStep / 8 * HD / kCompactThreads;
-            const int units = kCompactStep / 8 * width;
-            Elem* const vpool = pool + (int64_t)P.Hkv * (kPage * HD);
-            Elem v[PER][8];
+            Elem v[kUnits][8];
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const int u = tid + j * kCompactThreads, d = d0 + u % width, g = u / width;
+            for (int j = 0; j < kUnits; ++j) {
+                const int u = tid + j * kCompactThreads, d = d0 + u % WIDTH, g = u / WIDTH;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int t = g * 8 + e;
+                    const int m = g * 8 + e;
                     v[j][e] = 0;
-                    if (u < units && from[t] >= 0) v[j][e] = vpool[from[t] + (from_tok[t] >> 3) * (HD * 8) + d * 8 + (from_tok[t] & 7)];
+                    if (u < kMoves / 8 * WIDTH && from[m] >= 0) v[j][e] = pool[from[m] + (from_tok[m] >> 3) * (HD * 8) + d * 8 + (from_tok[m] & 7)];
                 }
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const int u = tid + j * kCompactThreads, d = d0 + u % width, g = u / width;
-                if (u >= units) continue;
+            for (int j = 0; j < kUnits; ++j) {
+                const int u = tid + j * kCompactThreads, d = d0 + u % WIDTH, g = u / WIDTH;
+                if (u >= kMoves / 8 * WIDTH) continue;
                 bool whole = true;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) whole &= to[g * 8 + e] >= 0;
-                const int at = (((p0 + g * 8) & 15) >> 3) * (HD * 8) + d * 8;
+                const int at = (to_tok[g * 8] >> 3) * (HD * 8) + d * 8;
                 if (whole) {
-                    *reinterpret_cast<Raw*>(vpool + to[g * 8] + at) = __builtin_bit_cast(Raw, v[j]);
+                    *reinterpret_cast<Raw*>(pool + to[g * 8] + at) = __builtin_bit_cast(Raw, v[j]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (to[g * 8 + e] >= 0) vpool[to[g * 8 + e] + at + e] = v[j][e];
+                        if (to[g * 8 + e] >= 0) pool[to[g * 8 + e] + at + e] = v[j][e];
                 }
             }
         }
@@ -575,7 +580,8 @@ __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const Comp
 
 int launch_compact(const CompactParams& p, int head_dim, bool fp8_pages, int layers, void* stream) {
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)(p.B * p.Hkv), (unsigned)(2 * p.slices + (p.weights ? 1 : 0)), (unsigned)layers);
+    const int heads = kMoves / p.step, groups = (p.Hkv + heads - 1) / heads, slices = head_dim / (head_dim < kCompactWidth ? head_dim : kCompactWidth);
+    const dim3 grid((unsigned)(p.B * groups), (unsigned)(2 * slices + (p.weights ? 1 : 0)), (unsigned)layers);
     if (head_dim == 128 && fp8_pages) hipLaunchKernelGGL((ppd_compact_kernel<128, true>), grid, dim3(kCompactThreads), 0, hs, p);
     else if (head_dim == 128) hipLaunchKernelGGL((ppd_compact_kernel<128, false>), grid, dim3(kCompactThreads), 0, hs, p);
     else if (fp8_pages) hipLaunchKernelGGL((ppd_compact_kernel<64, true>), grid, dim3(kCompactThreads), 0, hs, p);

@@ -127,7 +127,8 @@ struct CompactParams {
     int64_t weight_layer, weight_stride;
     int64_t pool_layer;        // elements
     int64_t num_pages, page_stride;
-    int32_t max_pages, Hkv, B, slices;
+    int32_t max_pages, Hkv, B;
+    int32_t step;              // positions of a head that a workgroup takes at a time: 16, 32, 64 or 128
     int32_t first[kCompactBatch], count[kCompactBatch];
 };
 

@@ -384,9 +384,13 @@ ppd_status compact_impl(ppd_ctx* ctx, void* kv_pages, int64_t layer_stride_elems
         p.page_tables = page_tables + (int64_t)at * max_pages;
         p.keep = keep + (int64_t)at * keep_seq_stride;
         p.weights = weights ? weights + (int64_t)at * Hkv * weight_stride : nullptr;
-        p.slices = (int64_t)p.B * Hkv * num_layers * 2 >= 4 * ctx->num_cus ? 1 : D / 32;
         std::copy(first + at, first + at + p.B, p.first);
         std::copy(count + at, count + at + p.B, p.count);
+        // the fewest positions at a time that take the longest list in one step, or 128
+        int64_t span = 0;
+        for (int i = 0; i < p.B; ++i) span = std::max<int64_t>(span, p.first[i] % 8 + (int64_t)p.count[i]);
+        p.step = 16;
+        while (p.step < 128 && p.step < span) p.step *= 2;
         const int rc = ppd::launch_compact(p, D, ctx->fp8_pages, num_layers, stream);
         if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch kv_compact");
     }
