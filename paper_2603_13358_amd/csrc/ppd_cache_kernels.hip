@@ -467,10 +467,11 @@ template <int HD, bool FP8>
 __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const CompactParams P) {
     typedef std::conditional_t<FP8, uint8_t, uint16_t> Elem;
     typedef std::conditional_t<FP8, u32x2, u32x4> Raw;  // eight elements
-    constexpr int WIDTH = HD < kCompactWidth ? HD : kCompactWidth, SLICES = HD / WIDTH;
+    constexpr int WIDTH = kCompactWidth, SLICES = HD / WIDTH;
+    static_assert(WIDTH == 64 && kMoves / 8 == kUnits * kCompactThreads / 64, "a wave moves a granule of V of 64 d at a time");
     __shared__ int64_t from[kMoves], to[kMoves];  // element offset of a move's page block, -1: it stays
     __shared__ int from_tok[kMoves], to_tok[kMoves];
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int heads = kMoves / P.step, groups = (P.Hkv + heads - 1) / heads;
     const int b = blockIdx.x / groups, head0 = blockIdx.x % groups * heads, layer = blockIdx.z;
     const int first = P.first[b], end = first + P.count[b];
@@ -535,43 +536,74 @@ __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const Comp
             for (int j = 0; j < kUnits; ++j) {
                 const int u = tid + j * kCompactThreads, m = u % kMoves, g = d0 / 8 + u / kMoves;
                 v[j] = Raw{};
-                if (u < kMoves * (WIDTH / 8) && from[m] >= 0) v[j] = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(pool + from[m] + (g * kPage + from_tok[m]) * 8));
+                if (from[m] >= 0) v[j] = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(pool + from[m] + (g * kPage + from_tok[m]) * 8));
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < kUnits; ++j) {
                 const int u = tid + j * kCompactThreads, m = u % kMoves, g = d0 / 8 + u / kMoves;
-                if (u < kMoves * (WIDTH / 8) && to[m] >= 0) *reinterpret_cast<Raw*>(pool + to[m] + (g * kPage + to_tok[m]) * 8) = v[j];
+                if (to[m] >= 0) *reinterpret_cast<Raw*>(pool + to[m] + (g * kPage + to_tok[m]) * 8) = v[j];
             }
         } else {
-            Elem v[kUnits][8];
+            // A wave takes a granule of destinations and 64 d, so that where its eight tokens come from is the same for all lanes.  A
+            // source granule is read once, whole, for all of the tokens in it (an element at a time the lanes asked for lines that
+            // were still on their way, and 32 evictions from 1K-8K to 1024 tokens took 203 us; this way THIS).
+            Raw v[kUnits];
 #pragma unroll
             for (int j = 0; j < kUnits; ++j) {
-                const int u = tid + j * kCompactThreads, d = d0 + u % WIDTH, g = u / WIDTH;
+                const int g = wave + j * (kCompactThreads / 64);
+                const Elem* at[8];
+                int tok[8];
+                bool there[8], fresh[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int m = g * 8 + e;
-                    v[j][e] = 0;
-                    if (u < kMoves / 8 * WIDTH && from[m] >= 0) v[j][e] = pool[from[m] + (from_tok[m] >> 3) * (HD * 8) + d * 8 + (from_tok[m] & 7)];
+                    const uint64_t f = (uint64_t)from[m];
+                    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)f), hi = __builtin_amdgcn_readfirstlane((uint32_t)(f >> 32));
+                    tok[e] = __builtin_amdgcn_readfirstlane(from_tok[m]);
+                    there[e] = (int32_t)hi >= 0;
+                    at[e] = pool + (int64_t)(((uint64_t)hi << 32) | lo) + (tok[e] >> 3) * (HD * 8);
+                    fresh[e] = there[e] && (e == 0 || !there[e - 1] || at[e] != at[e - 1]);
+                }
+                Raw r[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    r[e] = Raw{};
+                    if (fresh[e]) r[e] = *reinterpret_cast<const Raw*>(at[e] + (d0 + lane) * 8);
+                }
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int e = 1; e < 8; ++e)
+                    if (there[e] && !fresh[e]) r[e] = r[e - 1];
+                v[j] = Raw{};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    constexpr int PW = 4 / (int)sizeof(Elem);  // elements of a word
+                    uint32_t w = r[e][0];
+#pragma unroll
+                    for (int i = 1; i < (int)(sizeof(Raw) / 4); ++i)
+                        if (((tok[e] & 7) / PW) == i) w = r[e][i];
+                    w = (w >> (tok[e] % PW * (int)sizeof(Elem) * 8)) & (Elem)~(Elem)0;
+                    v[j][e / PW] |= w << (e % PW * (int)sizeof(Elem) * 8);
                 }
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < kUnits; ++j) {
-                const int u = tid + j * kCompactThreads, d = d0 + u % WIDTH, g = u / WIDTH;
-                if (u >= kMoves / 8 * WIDTH) continue;
+                const int g = wave + j * (kCompactThreads / 64);
                 bool whole = true;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) whole &= to[g * 8 + e] >= 0;
-                const int at = (to_tok[g * 8] >> 3) * (HD * 8) + d * 8;
+                const int at = (to_tok[g * 8] >> 3) * (HD * 8) + (d0 + lane) * 8;
                 if (whole) {
-                    *reinterpret_cast<Raw*>(pool + to[g * 8] + at) = __builtin_bit_cast(Raw, v[j]);
+                    *reinterpret_cast<Raw*>(pool + to[g * 8] + at) = v[j];
                 } else {
+                    constexpr int PW = 4 / (int)sizeof(Elem);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (to[g * 8 + e] >= 0) pool[to[g * 8 + e] + at + e] = v[j][e];
+                        if (to[g * 8 + e] >= 0) pool[to[g * 8 + e] + at + e] = (Elem)(v[j][e / PW] >> (e % PW * (int)sizeof(Elem) * 8));
                 }
             }
         }
@@ -580,7 +612,7 @@ __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const Comp
 
 int launch_compact(const CompactParams& p, int head_dim, bool fp8_pages, int layers, void* stream) {
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    const int heads = kMoves / p.step, groups = (p.Hkv + heads - 1) / heads, slices = head_dim / (head_dim < kCompactWidth ? head_dim : kCompactWidth);
+    const int heads = kMoves / p.step, groups = (p.Hkv + heads - 1) / heads, slices = head_dim / kCompactWidth;
     const dim3 grid((unsigned)(p.B * groups), (unsigned)(2 * slices + (p.weights ? 1 : 0)), (unsigned)layers);
     if (head_dim == 128 && fp8_pages) hipLaunchKernelGGL((ppd_compact_kernel<128, true>), grid, dim3(kCompactThreads), 0, hs, p);
     else if (head_dim == 128) hipLaunchKernelGGL((ppd_compact_kernel<128, false>), grid, dim3(kCompactThreads), 0, hs, p);
