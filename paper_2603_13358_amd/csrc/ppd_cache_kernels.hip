@@ -461,7 +461,11 @@ int launch_select(const SelectParams& p, int longest, void* stream) {
 // eight places, so all of V is read where every eighth token is kept.  Short lists (the accepted path of a tree) are a chain of
 // reads, list, page, token; there one workgroup takes all heads.
 constexpr int kCompactThreads = 256, kMoves = 128, kUnits = 4;  // units (granules) a thread moves at a time
+constexpr int kTogether = 2;  // granules of V whose sources a wave asks for at once
 constexpr int kCompactWidth = kUnits * kCompactThreads * 8 / kMoves;  // d of a slice
+
+// Workgroup barrier that leaves reads of the next step's lists on their way; what has to be there is waited for before it.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 template <int HD, bool FP8>
 __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const CompactParams P) {
@@ -488,122 +492,143 @@ __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const Comp
     float* const weights = P.weights ? P.weights + layer * P.weight_layer + ((int64_t)b * P.Hkv + (looks ? head : head0)) * P.weight_stride : nullptr;
     Elem* const pool = static_cast<Elem*>(P.pool) + layer * P.pool_layer + (is_v ? (int64_t)P.Hkv * (kPage * HD) : 0);
 
-    auto page_base = [&](int pos) {
-        int id = pages[pos >> 4];
-        if (id < 0 || id >= P.num_pages) {
-            atomicOr(P.err_flags, 2u);
-            return (int64_t)-1;
+    // Looking a move up is a chain of two reads, the list and the page table, which run ahead of the data by a step: `want` holds the
+    // list's entries of the next step, `pages_of` their pages.
+    struct Move { int pos, src, previous, from_id, to_id; };
+    auto ask_list = [&](int p0, Move& m) {
+        m.pos = p0 + tid % P.step;
+        const int i = m.pos - first;
+        m.src = -1;
+        m.previous = -1;
+        if (looks && i >= 0 && m.pos < end) {
+            m.src = keep[i];
+            if (i > 0) m.previous = keep[i - 1];
         }
-        return id * P.page_stride + head * (kPage * HD);
+    };
+    auto ask_pages = [&](Move& m) {
+        const int i = m.pos - first;
+        const bool listed = looks && i >= 0 && m.pos < end;
+        if (listed && (m.src < m.pos || m.src >= capacity || m.previous >= m.src)) {
+            atomicOr(P.err_flags, 8u);
+            m.src = -1;
+        }
+        m.from_id = m.to_id = 0;
+        if (m.src >= 0 && !is_weights) {
+            m.from_id = pages[m.src >> 4];
+            m.to_id = pages[m.pos >> 4];
+        }
     };
 
-    for (int p0 = first & ~7; p0 < end; p0 += P.step) {  // steps begin on a granule of V
-        const int pos = p0 + tid % P.step, i = pos - first;
-        int src = -1;
-        if (looks && i >= 0 && pos < end) {
-            src = keep[i];
-            const int previous = i > 0 ? keep[i - 1] : -1;
-            if (src < pos || src >= capacity || previous >= src) {
-                atomicOr(P.err_flags, 8u);
-                src = -1;
-            }
-        }
+    const int start = first & ~7;  // steps begin on a granule of V
+    Move m;
+    ask_list(start, m);
+    ask_pages(m);
+    for (int p0 = start; p0 < end; p0 += P.step) {
         if (is_weights) {
             float v = 0.f;
-            if (src >= 0) v = weights[src];
+            if (m.src >= 0) v = weights[m.src];
             asm volatile("s_waitcnt vmcnt(0)" : "+v"(v) : : "memory");
             __syncthreads();
-            if (src >= 0) weights[pos] = v;
+            if (m.src >= 0) weights[m.pos] = v;
+            ask_list(p0 + P.step, m);
+            ask_pages(m);
             continue;
         }
-        int64_t f = -1, t = -1;
-        if (src >= 0) {
-            f = page_base(src);
-            t = page_base(pos);
+        if (m.src >= 0 && ((uint32_t)m.from_id >= (uint64_t)P.num_pages || (uint32_t)m.to_id >= (uint64_t)P.num_pages)) {
+            atomicOr(P.err_flags, 2u);
+            m.src = -1;
         }
-        const bool moves = f >= 0 && t >= 0;
         __syncthreads();  // the lists of the step before are read
         if (tid < kMoves) {
-            from[tid] = moves ? f : -1;
-            to[tid] = moves ? t : -1;
-            from_tok[tid] = src & 15;
-            to_tok[tid] = pos & 15;
+            from[tid] = m.src < 0 ? -1 : m.from_id * P.page_stride + head * (kPage * HD);
+            to[tid] = m.src < 0 ? -1 : m.to_id * P.page_stride + head * (kPage * HD);
+            from_tok[tid] = m.src & 15;
+            to_tok[tid] = m.pos & 15;
         }
         __syncthreads();
+        ask_list(p0 + P.step, m);
         if (!is_v) {
             Raw v[kUnits];
 #pragma unroll
             for (int j = 0; j < kUnits; ++j) {
-                const int u = tid + j * kCompactThreads, m = u % kMoves, g = d0 / 8 + u / kMoves;
+                const int u = tid + j * kCompactThreads, k = u % kMoves, g = d0 / 8 + u / kMoves;
                 v[j] = Raw{};
-                if (from[m] >= 0) v[j] = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(pool + from[m] + (g * kPage + from_tok[m]) * 8));
+                if (from[k] >= 0) v[j] = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(pool + from[k] + (g * kPage + from_tok[k]) * 8));
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
+            ask_pages(m);
+            lds_barrier();
 #pragma unroll
             for (int j = 0; j < kUnits; ++j) {
-                const int u = tid + j * kCompactThreads, m = u % kMoves, g = d0 / 8 + u / kMoves;
-                if (to[m] >= 0) *reinterpret_cast<Raw*>(pool + to[m] + (g * kPage + to_tok[m]) * 8) = v[j];
+                const int u = tid + j * kCompactThreads, k = u % kMoves, g = d0 / 8 + u / kMoves;
+                if (to[k] >= 0) *reinterpret_cast<Raw*>(pool + to[k] + (g * kPage + to_tok[k]) * 8) = v[j];
             }
         } else {
             // A wave takes a granule of destinations and 64 d, so that where its eight tokens come from is the same for all lanes.  A
             // source granule is read once, whole, for all of the tokens in it (an element at a time the lanes asked for lines that
             // were still on their way, and 32 evictions from 1K-8K to 1024 tokens took 203 us; this way THIS).
             Raw v[kUnits];
+            // lane 8 j + e has the move of element e of the wave's granule j; `fresh`: not out of the granule that the element before is from
+            const int my_move = (wave + (lane >> 3) % kUnits * (kCompactThreads / 64)) * 8 + (lane & 7);
+            const uint64_t my_to = (uint64_t)to[my_move];
+            const int my_from_tok = from_tok[my_move], my_to_tok = to_tok[my_move];
+            const uint64_t my_from = (uint64_t)(from[my_move] + (my_from_tok >> 3) * (HD * 8));
+            const uint64_t moving = __ballot((int64_t)my_to >= 0);
+            const uint32_t before_lo = __shfl_up((uint32_t)my_from, 1, 64), before_hi = __shfl_up((uint32_t)(my_from >> 32), 1, 64);
+            const bool same = (lane & 7) != 0 && (moving >> (lane - 1) & 1) && before_lo == (uint32_t)my_from && before_hi == (uint32_t)(my_from >> 32);
+            const uint64_t fresh = moving & ~__ballot(same);
+            auto of_lane = [&](uint64_t x, int l) {
+                return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, l);
+            };
 #pragma unroll
-            for (int j = 0; j < kUnits; ++j) {
-                const int g = wave + j * (kCompactThreads / 64);
-                const Elem* at[8];
-                int tok[8];
-                bool there[8], fresh[8];
+            for (int j0 = 0; j0 < kUnits; j0 += kTogether) {
+                Raw r[kTogether][8];  // of the fresh ones
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int m = g * 8 + e;
-                    const uint64_t f = (uint64_t)from[m];
-                    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)f), hi = __builtin_amdgcn_readfirstlane((uint32_t)(f >> 32));
-                    tok[e] = __builtin_amdgcn_readfirstlane(from_tok[m]);
-                    there[e] = (int32_t)hi >= 0;
-                    at[e] = pool + (int64_t)(((uint64_t)hi << 32) | lo) + (tok[e] >> 3) * (HD * 8);
-                    fresh[e] = there[e] && (e == 0 || !there[e - 1] || at[e] != at[e - 1]);
-                }
-                Raw r[8];
+                for (int j = 0; j < kTogether; ++j)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    r[e] = Raw{};
-                    if (fresh[e]) r[e] = *reinterpret_cast<const Raw*>(at[e] + (d0 + lane) * 8);
-                }
+                    for (int e = 0; e < 8; ++e) {
+                        const int l = (j0 + j) * 8 + e;
+                        r[j][e] = Raw{};
+                        if (fresh >> l & 1) r[j][e] = *reinterpret_cast<const Raw*>(pool + (int64_t)of_lane(my_from, l) + (d0 + lane) * 8);
+                    }
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                if (j0 == 0) ask_pages(m);
+                uint64_t taken = fresh;
+                asm volatile("" : "+s"(taken));  // not to be merged with the branches above
 #pragma unroll
-                for (int e = 1; e < 8; ++e)
-                    if (there[e] && !fresh[e]) r[e] = r[e - 1];
-                v[j] = Raw{};
+                for (int j = 0; j < kTogether; ++j) {
+                    Raw cur = {};
+                    v[j0 + j] = Raw{};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    constexpr int PW = 4 / (int)sizeof(Elem);  // elements of a word
-                    uint32_t w = r[e][0];
+                    for (int e = 0; e < 8; ++e) {
+                        constexpr int PW = 4 / (int)sizeof(Elem);  // elements of a word
+                        const int l = (j0 + j) * 8 + e, tok = __builtin_amdgcn_readlane(my_from_tok, l) & 7;
+                        const bool takes = taken >> l & 1;
 #pragma unroll
-                    for (int i = 1; i < (int)(sizeof(Raw) / 4); ++i)
-                        if (((tok[e] & 7) / PW) == i) w = r[e][i];
-                    w = (w >> (tok[e] % PW * (int)sizeof(Elem) * 8)) & (Elem)~(Elem)0;
-                    v[j][e / PW] |= w << (e % PW * (int)sizeof(Elem) * 8);
+                        for (int i = 0; i < (int)(sizeof(Raw) / 4); ++i) cur[i] = takes ? r[j][e][i] : cur[i];
+                        uint32_t w = cur[0];
+#pragma unroll
+                        for (int i = 1; i < (int)(sizeof(Raw) / 4); ++i) w = tok / PW == i ? cur[i] : w;
+                        w = (w >> (tok % PW * (int)sizeof(Elem) * 8)) & (Elem)~(Elem)0;
+                        v[j0 + j][e / PW] |= w << (e % PW * (int)sizeof(Elem) * 8);
+                    }
+                    asm volatile("" : "+v"(v[j0 + j]) : : "memory");  // taken apart before the next ones are asked for: registers
                 }
             }
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
+            lds_barrier();
 #pragma unroll
             for (int j = 0; j < kUnits; ++j) {
-                const int g = wave + j * (kCompactThreads / 64);
-                bool whole = true;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) whole &= to[g * 8 + e] >= 0;
-                const int at = (to_tok[g * 8] >> 3) * (HD * 8) + (d0 + lane) * 8;
-                if (whole) {
-                    *reinterpret_cast<Raw*>(pool + to[g * 8] + at) = v[j];
+                const uint32_t places = moving >> (j * 8) & 255u;  // the granule's eight places are neighbours in one page
+                if (places == 0) continue;
+                const int l = j * 8 + __builtin_ctz(places);
+                Elem* const at = pool + (int64_t)of_lane(my_to, l) + (__builtin_amdgcn_readlane(my_to_tok, l) >> 3) * (HD * 8);
+                if (places == 255) {
+                    *reinterpret_cast<Raw*>(at + (d0 + lane) * 8) = v[j];
                 } else {
                     constexpr int PW = 4 / (int)sizeof(Elem);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (to[g * 8 + e] >= 0) pool[to[g * 8 + e] + at + e] = (Elem)(v[j][e / PW] >> (e % PW * (int)sizeof(Elem) * 8));
+                        if (places >> e & 1) at[(d0 + lane) * 8 + e] = (Elem)(v[j][e / PW] >> (e % PW * (int)sizeof(Elem) * 8));
                 }
             }
         }
