@@ -12,7 +12,7 @@ _LIB_PATH = os.path.join(_HERE, "libppd.so")
 _CALL_PATH = os.path.join(_HERE, "ppd_call" + sysconfig.get_config_var("EXT_SUFFIX"))  # built for this interpreter's ABI
 _lib = None
 _call = None       # the call module
-_fn_append = _fn_land = _fn_mixed = _fn_mixed_static = None  # addresses of the entry points it calls
+_fn_append = _fn_land = _fn_mixed = _fn_mixed_static = _fn_tree = _fn_weighted = _fn_select = _fn_compact = None  # addresses of the entry points it calls
 
 STATUS_NAMES = {0: "PPD_OK", -1: "PPD_ERR_NULL", -2: "PPD_ERR_SHAPE", -3: "PPD_ERR_RANGE",
                 -4: "PPD_ERR_PAGETABLE", -5: "PPD_ERR_WORKSPACE", -6: "PPD_ERR_HIP"}
@@ -58,7 +58,7 @@ def lib_path():
 
 def load_library():
     """Loads libppd.so; raises if it has not been built (no fallback of any kind)."""
-    global _lib, _call, _fn_append, _fn_land, _fn_mixed, _fn_mixed_static
+    global _lib, _call, _fn_append, _fn_land, _fn_mixed, _fn_mixed_static, _fn_tree, _fn_weighted, _fn_select, _fn_compact
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH) or not os.path.exists(_CALL_PATH):
@@ -105,6 +105,8 @@ def load_library():
     loader.exec_module(_call)
     _fn_append, _fn_land, _fn_mixed, _fn_mixed_static = (ctypes.cast(f, vp).value for f in (
         lib.ppd_kv_append, lib.ppd_kv_land, lib.ppd_mixed_attention, lib.ppd_mixed_attention_static))
+    _fn_tree, _fn_weighted, _fn_select, _fn_compact = (ctypes.cast(f, vp).value for f in (
+        lib.ppd_tree_attention, lib.ppd_weighted_attention, lib.ppd_kv_select, lib.ppd_kv_compact))
     _lib = lib
     return lib
 
@@ -186,11 +188,6 @@ def ppd_mixed_attention_static(ctx, q, kv_pages, page_tables, L, n, scale, out, 
                         static=True)
 
 
-def _ptr(x):
-    """A tensor's address, or an address or None as it is."""
-    return x.data_ptr() if hasattr(x, "data_ptr") else x
-
-
 def _lengths(*arrays):
     """Host int32 arrays of one length."""
     arrays = [_host_i32(a).reshape(-1) for a in arrays]
@@ -201,35 +198,33 @@ def _lengths(*arrays):
 
 def ppd_tree_attention(ctx, q, kv_pages, page_tables, L, n, tree_mask, scale, out, max_pages=None, mask_words=None, stream=None):
     """tree_mask: int64 or uint64 [rows][words], or an address with mask_words."""
-    lib = load_library()
-    L, n = _lengths(L, n)
-    max_pages = page_tables.shape[1] if max_pages is None else max_pages
-    mask_words = tree_mask.shape[1] if mask_words is None else mask_words
-    status = lib.ppd_tree_attention(ctx, _ptr(q), _ptr(kv_pages), _ptr(page_tables), max_pages, _ptr(tree_mask), mask_words, L.ctypes.data, n.ctypes.data,
-                                    L.shape[0], scale, _ptr(out), stream)
+    if _lib is None:
+        load_library()
+    status = _call.tree_attention(_fn_tree, ctx, q, kv_pages, page_tables, max_pages, tree_mask, mask_words, L, n, scale, out, stream)
+    if status is None:  # lengths in another type, layout or container
+        status = _call.tree_attention(_fn_tree, ctx, q, kv_pages, page_tables, max_pages, tree_mask, mask_words, *_lengths(L, n), scale, out, stream)
     if status != 0:
         _check(status, ctx)
 
 
 def ppd_weighted_attention(ctx, q, kv_pages, page_tables, L, n, scale, out, weights, max_pages=None, weight_stride=None, stream=None):
-    """weights: float32 [sequences][KV heads][stride]."""
-    lib = load_library()
-    L, n = _lengths(L, n)
-    max_pages = page_tables.shape[1] if max_pages is None else max_pages
-    weight_stride = weights.shape[-1] if weight_stride is None else weight_stride
-    status = lib.ppd_weighted_attention(ctx, _ptr(q), _ptr(kv_pages), _ptr(page_tables), max_pages, L.ctypes.data, n.ctypes.data, L.shape[0], scale,
-                                        _ptr(out), _ptr(weights), weight_stride, stream)
+    """weights: float32 [sequences][KV heads][stride], or an address with weight_stride."""
+    if _lib is None:
+        load_library()
+    status = _call.weighted_attention(_fn_weighted, ctx, q, kv_pages, page_tables, max_pages, L, n, scale, out, weights, weight_stride, stream)
+    if status is None:
+        status = _call.weighted_attention(_fn_weighted, ctx, q, kv_pages, page_tables, max_pages, *_lengths(L, n), scale, out, weights, weight_stride, stream)
     if status != 0:
         _check(status, ctx)
 
 
 def ppd_kv_select(ctx, weights, length, budget, sinks, recent, keep, weight_stride=None, keep_stride=None, stream=None):
-    """weights: float32 [sequences][KV heads][stride]; keep: int32 [sequences][KV heads][stride]."""
-    lib = load_library()
-    length, = _lengths(length)
-    weight_stride = weights.shape[-1] if weight_stride is None else weight_stride
-    keep_stride = keep.shape[-1] if keep_stride is None else keep_stride
-    status = lib.ppd_kv_select(ctx, _ptr(weights), weight_stride, length.ctypes.data, length.shape[0], budget, sinks, recent, _ptr(keep), keep_stride, stream)
+    """weights: float32 [sequences][KV heads][stride]; keep: int32 [sequences][KV heads][stride]; or addresses with their strides."""
+    if _lib is None:
+        load_library()
+    status = _call.kv_select(_fn_select, ctx, weights, weight_stride, length, budget, sinks, recent, keep, keep_stride, stream)
+    if status is None:
+        status = _call.kv_select(_fn_select, ctx, weights, weight_stride, *_lengths(length), budget, sinks, recent, keep, keep_stride, stream)
     if status != 0:
         _check(status, ctx)
 
@@ -239,20 +234,20 @@ def ppd_kv_compact(ctx, kv_pages, page_tables, keep, first, count, layer_stride_
     """keep: int32 [sequences][n] (shared by heads and layers), [sequences][KV heads][n] (shared by layers) or [layers][sequences][KV heads][n],
     or an address with keep_strides = (layer, sequence, head).  weights: float32 [sequences][KV heads][stride], with a layer axis in front
     if there are several, or None."""
-    lib = load_library()
-    first, count = _lengths(first, count)
-    max_pages = page_tables.shape[1] if max_pages is None else max_pages
+    if _lib is None:
+        load_library()
     if keep_strides is None:
-        strides = tuple(keep.stride())
+        strides = keep.stride()
         if len(strides) not in (2, 3, 4) or strides[-1] != 1 and keep.shape[-1] > 1:
             raise PPDError(-3, "keep has two, three or four axes, the last contiguous")
-        if keep.shape[-1] < (count.max() if count.size else 0):
+        first, count = _lengths(first, count)
+        if keep.shape[-1] < count.max(initial=0):
             raise PPDError(-3, "keep has fewer entries than count")
-        keep_strides = (0, strides[0], 0) if len(strides) == 2 else (0,) + strides[:2] if len(strides) == 3 else strides[:3]
-    if weight_stride is None:
-        weight_stride = 0 if weights is None else weights.shape[-1]
-    status = lib.ppd_kv_compact(ctx, _ptr(kv_pages), layer_stride_elems, num_layers, _ptr(page_tables), max_pages, _ptr(keep), *keep_strides,
-                                first.ctypes.data, count.ctypes.data, first.shape[0], _ptr(weights), weight_stride, stream)
+        keep_strides = (0, strides[0], 0) if len(strides) == 2 else (0, strides[0], strides[1]) if len(strides) == 3 else strides[:3]
+    args = (_fn_compact, ctx, kv_pages, layer_stride_elems, num_layers, page_tables, max_pages, keep, *keep_strides)
+    status = _call.kv_compact(*args, first, count, weights, weight_stride, stream)
+    if status is None:
+        status = _call.kv_compact(*args, *_lengths(first, count), weights, weight_stride, stream)
     if status != 0:
         _check(status, ctx)
 

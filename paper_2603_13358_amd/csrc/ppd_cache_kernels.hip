@@ -457,9 +457,11 @@ int launch_select(const SelectParams& p, int longest, void* stream) {
 // that leaves room for -- reads all of them, waits, and writes.  Every d is independent, so K, V and slices of d are workgroups of their
 // own; the weights are another.  Entries that do not ascend or lie outside the sequence's pages raise the sticky flag, and their
 // tokens stay where they are.
-// Bound by memory where lists are long: a K token is 16-byte granules, but V's granules hold 8 tokens of one d, which come from up to
-// eight places, so all of V is read where every eighth token is kept.  Short lists (the accepted path of a tree) are a chain of
-// reads, list, page, token; there one workgroup takes all heads.
+// Bound by memory, in whole lines of 128 bytes: a line of K is 8 tokens' 8 d, a line of V 8 d of 8 tokens, and both are read for one token as
+// for eight.  32 evictions from 1K-8K to 1024 tokens, every head its own: 271 MB of kept tokens' bytes, in and out, are 610 MB of
+// lines, 126 us at 4.9 TB/s (a large copy's rate: 4.9); K alone takes 54 us, V alone 66.  The accepted paths of 16 trees over 32
+// layers: 22 MB, about 100 MB of lines, 22 us.  Nothing moves less in this layout.  Short lists are a chain of reads -- list, page,
+// token -- so there one workgroup takes all heads.
 constexpr int kCompactThreads = 256, kMoves = 128, kUnits = 4;  // units (granules) a thread moves at a time
 constexpr int kTogether = 2;  // granules of V whose sources a wave asks for at once
 constexpr int kCompactWidth = kUnits * kCompactThreads * 8 / kMoves;  // d of a slice
@@ -479,9 +481,10 @@ __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const Comp
     const int heads = kMoves / P.step, groups = (P.Hkv + heads - 1) / heads;
     const int b = blockIdx.x / groups, head0 = blockIdx.x % groups * heads, layer = blockIdx.z;
     const int first = P.first[b], end = first + P.count[b];
-    const int part = blockIdx.y;  // K slices, V slices, weights
-    const bool is_weights = part == 2 * SLICES, is_v = part >= SLICES;
-    const int d0 = part % SLICES * WIDTH;
+    // Weights first (a step of theirs is as long a chain as the others', and they are few: started last they would end last), K slices, V slices.
+    const int part = (int)blockIdx.y - (P.weights ? 1 : 0);
+    const bool is_weights = part < 0, is_v = part >= SLICES;
+    const int d0 = (is_weights ? 0 : part % SLICES) * WIDTH;
     const int32_t* pages = P.page_tables + (int64_t)b * P.max_pages;
     int64_t capacity = (int64_t)P.max_pages * kPage;
     if (P.weights && P.weight_stride < capacity) capacity = P.weight_stride;
@@ -561,12 +564,12 @@ __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const Comp
 #pragma unroll
             for (int j = 0; j < kUnits; ++j) {
                 const int u = tid + j * kCompactThreads, k = u % kMoves, g = d0 / 8 + u / kMoves;
-                if (to[k] >= 0) *reinterpret_cast<Raw*>(pool + to[k] + (g * kPage + to_tok[k]) * 8) = v[j];
+                if (to[k] >= 0) __builtin_nontemporal_store(v[j], reinterpret_cast<Raw*>(pool + to[k] + (g * kPage + to_tok[k]) * 8));
             }
         } else {
             // A wave takes a granule of destinations and 64 d, so that where its eight tokens come from is the same for all lanes.  A
             // source granule is read once, whole, for all of the tokens in it (an element at a time the lanes asked for lines that
-            // were still on their way, and 32 evictions from 1K-8K to 1024 tokens took 203 us; this way THIS).
+            // were still on their way, and 32 evictions from 1K-8K to 1024 tokens took 203 us, this way 151).
             Raw v[kUnits];
             // lane 8 j + e has the move of element e of the wave's granule j; `fresh`: not out of the granule that the element before is from
             const int my_move = (wave + (lane >> 3) % kUnits * (kCompactThreads / 64)) * 8 + (lane & 7);
@@ -623,7 +626,7 @@ __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const Comp
                 const int l = j * 8 + __builtin_ctz(places);
                 Elem* const at = pool + (int64_t)of_lane(my_to, l) + (__builtin_amdgcn_readlane(my_to_tok, l) >> 3) * (HD * 8);
                 if (places == 255) {
-                    *reinterpret_cast<Raw*>(at + (d0 + lane) * 8) = v[j];
+                    __builtin_nontemporal_store(v[j], reinterpret_cast<Raw*>(at + (d0 + lane) * 8));
                 } else {
                     constexpr int PW = 4 / (int)sizeof(Elem);
 #pragma unroll

@@ -142,10 +142,136 @@ static PyObject* call_mixed(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     return result;
 }
 
+// Two int32 arrays of one length: 1 and both buffers filled, else 0 and none is
+static int int32_arrays(PyObject* x, PyObject* y, Py_buffer* a, Py_buffer* b) {
+    if (!int32_array(x, a)) return 0;
+    if (!int32_array(y, b)) {
+        PyBuffer_Release(a);
+        return 0;
+    }
+    if (a->shape[0] == b->shape[0]) return 1;
+    PyBuffer_Release(b);
+    PyBuffer_Release(a);
+    return 0;
+}
+
+typedef int32_t (*tree_fn)(void*, const void*, const void*, const int32_t*, int32_t, const uint64_t*, int32_t, const int32_t*, const int32_t*, int32_t, float, void*, void*);
+typedef int32_t (*weighted_fn)(void*, const void*, const void*, const int32_t*, int32_t, const int32_t*, const int32_t*, int32_t, float, void*, float*, int64_t, void*);
+typedef int32_t (*select_fn)(void*, const float*, int64_t, const int32_t*, int32_t, int32_t, int32_t, int32_t, int32_t*, int64_t, void*);
+typedef int32_t (*compact_fn)(void*, void*, int64_t, int32_t, const int32_t*, int32_t, const int32_t*, int64_t, int64_t, int64_t, const int32_t*, const int32_t*, int32_t,
+                              float*, int64_t, void*);
+
+// tree_attention(fn, ctx, q, kv_pages, page_tables, max_pages, tree_mask, mask_words, L, n, scale, out, stream) -> status, or None if L and n are
+// not plain int32 arrays of one length yet
+static PyObject* call_tree(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *fn, *ctx, *q, *pages, *tables, *mask, *out, *stream;
+    int64_t max_pages, words;
+    Py_buffer L, nn;
+    (void)self;
+    if (!expect(n, 13)) return NULL;
+    if (!int32_arrays(a[8], a[9], &L, &nn)) Py_RETURN_NONE;
+    PyObject* result = NULL;
+    PyObject* scale = NULL;
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int_or_shape(a[5], a[4], 1, &max_pages) && to_int_or_shape(a[7], a[6], 1, &words) &&
+        to_address(a[2], &q) && to_address(a[3], &pages) && to_address(a[4], &tables) && to_address(a[6], &mask) &&
+        (scale = PyNumber_Float(a[10])) && to_address(a[11], &out) && to_handle(a[12], &stream)) {
+        const float s = (float)PyFloat_AS_DOUBLE(scale);
+        int32_t status;
+        Py_BEGIN_ALLOW_THREADS
+        status = ((tree_fn)fn)(ctx, q, pages, (const int32_t*)tables, (int32_t)max_pages, (const uint64_t*)mask, (int32_t)words, (const int32_t*)L.buf,
+                               (const int32_t*)nn.buf, (int32_t)L.shape[0], s, out, stream);
+        Py_END_ALLOW_THREADS
+        result = PyLong_FromLong(status);
+    }
+    Py_XDECREF(scale);
+    PyBuffer_Release(&nn);
+    PyBuffer_Release(&L);
+    return result;
+}
+
+// weighted_attention(fn, ctx, q, kv_pages, page_tables, max_pages, L, n, scale, out, weights, weight_stride, stream) -> the same
+static PyObject* call_weighted(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *fn, *ctx, *q, *pages, *tables, *out, *weights, *stream;
+    int64_t max_pages, stride;
+    Py_buffer L, nn;
+    (void)self;
+    if (!expect(n, 13)) return NULL;
+    if (!int32_arrays(a[6], a[7], &L, &nn)) Py_RETURN_NONE;
+    PyObject* result = NULL;
+    PyObject* scale = NULL;
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int_or_shape(a[5], a[4], 1, &max_pages) && to_int_or_shape(a[11], a[10], -1, &stride) &&
+        to_address(a[2], &q) && to_address(a[3], &pages) && to_address(a[4], &tables) && (scale = PyNumber_Float(a[8])) &&
+        to_address(a[9], &out) && to_address(a[10], &weights) && to_handle(a[12], &stream)) {
+        const float s = (float)PyFloat_AS_DOUBLE(scale);
+        int32_t status;
+        Py_BEGIN_ALLOW_THREADS
+        status = ((weighted_fn)fn)(ctx, q, pages, (const int32_t*)tables, (int32_t)max_pages, (const int32_t*)L.buf, (const int32_t*)nn.buf,
+                                   (int32_t)L.shape[0], s, out, (float*)weights, stride, stream);
+        Py_END_ALLOW_THREADS
+        result = PyLong_FromLong(status);
+    }
+    Py_XDECREF(scale);
+    PyBuffer_Release(&nn);
+    PyBuffer_Release(&L);
+    return result;
+}
+
+// kv_select(fn, ctx, weights, weight_stride, length, budget, sinks, recent, keep, keep_stride, stream) -> status, or None if length is not a plain
+// int32 array yet
+static PyObject* call_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *fn, *ctx, *weights, *keep, *stream;
+    int64_t stride, keep_stride, budget, sinks, recent;
+    Py_buffer len;
+    (void)self;
+    if (!expect(n, 11)) return NULL;
+    if (!int32_array(a[4], &len)) Py_RETURN_NONE;
+    PyObject* result = NULL;
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int_or_shape(a[3], a[2], -1, &stride) && to_int_or_shape(a[9], a[8], -1, &keep_stride) &&
+        to_address(a[2], &weights) && to_int(a[5], &budget) && to_int(a[6], &sinks) && to_int(a[7], &recent) && to_address(a[8], &keep) && to_handle(a[10], &stream)) {
+        int32_t status;
+        Py_BEGIN_ALLOW_THREADS
+        status = ((select_fn)fn)(ctx, (const float*)weights, stride, (const int32_t*)len.buf, (int32_t)len.shape[0], (int32_t)budget, (int32_t)sinks, (int32_t)recent,
+                                 (int32_t*)keep, keep_stride, stream);
+        Py_END_ALLOW_THREADS
+        result = PyLong_FromLong(status);
+    }
+    PyBuffer_Release(&len);
+    return result;
+}
+
+// kv_compact(fn, ctx, kv_pages, layer_stride_elems, num_layers, page_tables, max_pages, keep, keep_layer, keep_seq, keep_head, first, count, weights,
+// weight_stride, stream) -> status, or None if first and count are not plain int32 arrays of one length yet
+static PyObject* call_compact(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *fn, *ctx, *pages, *tables, *keep, *weights, *stream;
+    int64_t layer_stride, layers, max_pages, kl, ks, kh, stride = 0;
+    Py_buffer first, count;
+    (void)self;
+    if (!expect(n, 16)) return NULL;
+    if (!int32_arrays(a[11], a[12], &first, &count)) Py_RETURN_NONE;
+    PyObject* result = NULL;
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_address(a[2], &pages) && to_int(a[3], &layer_stride) && to_int(a[4], &layers) &&
+        to_int_or_shape(a[6], a[5], 1, &max_pages) && to_address(a[5], &tables) && to_address(a[7], &keep) && to_int(a[8], &kl) && to_int(a[9], &ks) &&
+        to_int(a[10], &kh) && (a[13] == Py_None || to_int_or_shape(a[14], a[13], -1, &stride)) && to_address(a[13], &weights) && to_handle(a[15], &stream)) {
+        int32_t status;
+        Py_BEGIN_ALLOW_THREADS
+        status = ((compact_fn)fn)(ctx, pages, layer_stride, (int32_t)layers, (const int32_t*)tables, (int32_t)max_pages, (const int32_t*)keep, kl, ks, kh,
+                                  (const int32_t*)first.buf, (const int32_t*)count.buf, (int32_t)first.shape[0], (float*)weights, stride, stream);
+        Py_END_ALLOW_THREADS
+        result = PyLong_FromLong(status);
+    }
+    PyBuffer_Release(&count);
+    PyBuffer_Release(&first);
+    return result;
+}
+
 static PyMethodDef kMethods[] = {
     {"kv_append", (PyCFunction)(void (*)(void))call_append, METH_FASTCALL, NULL},
     {"kv_land", (PyCFunction)(void (*)(void))call_land, METH_FASTCALL, NULL},
     {"mixed_attention", (PyCFunction)(void (*)(void))call_mixed, METH_FASTCALL, NULL},
+    {"tree_attention", (PyCFunction)(void (*)(void))call_tree, METH_FASTCALL, NULL},
+    {"weighted_attention", (PyCFunction)(void (*)(void))call_weighted, METH_FASTCALL, NULL},
+    {"kv_select", (PyCFunction)(void (*)(void))call_select, METH_FASTCALL, NULL},
+    {"kv_compact", (PyCFunction)(void (*)(void))call_compact, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "ppd_call", "Calls of libppd's per-layer entry points.", -1, kMethods, NULL, NULL, NULL, NULL};
