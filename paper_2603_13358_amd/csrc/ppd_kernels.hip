@@ -489,6 +489,8 @@ __device__ __forceinline__ void mfma_item(const KP& P, const ppd_work_item& it, 
 #pragma unroll
                     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s_cur[tb][i]);
                 mx = max_halves(mx);
+                // TREE: a column whose own sums are in range keeps its reference, so that no other row decides how it is rounded
+                if constexpr (TREE) mx = max_halves(!(psum <= kMaxLazyP) ? 1.f : 0.f) > 0.f ? mx : m_run;
                 const float m_new = fmaxf(m_run, mx);
                 const float m_use = m_new == NEG_INF ? 0.f : m_new;
                 const float alpha = fast_exp2(m_run * c - m_use * c);  // m_run = -inf gives 0

@@ -167,7 +167,9 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
             float mx = sc[0];
 #pragma unroll
             for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+            // a column whose own sums are in range keeps its reference, so that no other row decides how it is rounded
             mx = max_halves(mx);
+            mx = max_halves(!(psum <= kMaxLazyP) ? 1.f : 0.f) > 0.f ? mx : m_run;
             const float m_new = fmaxf(m_run, mx);
             const float m_use = m_new == NEG_INF ? 0.f : m_new;
             const float alpha = fast_exp2(m_run * c - m_use * c);  // m_run = -inf gives 0

@@ -212,6 +212,18 @@ def test_what_a_row_does_not_see_does_not_reach_it(bad, long):
     assert np.isfinite(seeing[..., :3]).all() and np.isfinite(seeing[..., 9:]).all() and np.isfinite(c[blind]).all()
 
 
+@pytest.mark.parametrize("n", [8, 40])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_row_is_rounded_by_what_it_sees_itself(n, fp8):
+    b = Batch([900], [n], 8, 2, 128, fp8, seed=17)
+    mask = random_mask(b, 1, seed=18)
+    before = b.tree(mask)
+    b.q_dev[3] *= 64.0  # far larger scores: its reference is raised again and again
+    after = b.tree(mask)
+    others = [j for j in range(n) if j != 3]
+    assert torch.equal(before[others], after[others]) and not torch.equal(before[3], after[3])
+
+
 def test_tree_scale_zero_and_sharp_scores():
     b = Batch([70], [9], 8, 1, 128, seed=6, q_scale=12.0)
     mask = random_mask(b, 1, seed=7)
