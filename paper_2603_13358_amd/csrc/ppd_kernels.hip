@@ -493,7 +493,8 @@ __device__ __forceinline__ void mfma_item(const KP& P, const ppd_work_item& it, 
                 if constexpr (TREE) mx = max_halves(!(psum <= kMaxLazyP) ? 1.f : 0.f) > 0.f ? mx : m_run;
                 const float m_new = fmaxf(m_run, mx);
                 const float m_use = m_new == NEG_INF ? 0.f : m_new;
-                const float alpha = fast_exp2(m_run * c - m_use * c);  // m_run = -inf gives 0
+                // m_run = -inf gives 0; TREE: the same reference exactly 1
+                const float alpha = fast_exp2(TREE ? (m_run - m_use) * c : m_run * c - m_use * c);
                 l_run *= alpha;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)

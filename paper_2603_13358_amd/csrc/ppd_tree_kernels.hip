@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
             mx = max_halves(!(psum <= kMaxLazyP) ? 1.f : 0.f) > 0.f ? mx : m_run;
             const float m_new = fmaxf(m_run, mx);
             const float m_use = m_new == NEG_INF ? 0.f : m_new;
-            const float alpha = fast_exp2(m_run * c - m_use * c);  // m_run = -inf gives 0
+            const float alpha = fast_exp2((m_run - m_use) * c);  // m_run = -inf gives 0, the same reference exactly 1
             l_run *= alpha;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
