@@ -1,5 +1,6 @@
 // Tile list of tree and weighted attention: which columns of which sequence meet which keys in which workgroup.
 #include <algorithm>
+#include <functional>
 
 #include "ppd_ops.h"
 
@@ -7,38 +8,73 @@ namespace ppd {
 
 namespace {
 
-// What a kind of tile costs: `start_keys` is its start and end in keys' time, `slots` how many are resident.
+// What a kind of tile costs, in keys' time: `start_keys` is its start and end, `join_keys` the launch that joins partials and
+// `column_keys` a column of a partial, written and read again.  `slots` tiles are resident.
 struct TileKind {
     int32_t max_chunk, step;
-    double start_keys, join_keys, slots;
+    double start_keys, join_keys, column_keys;
+    int32_t slots;
 };
 
-// Keys per tile, about: every sequence's range is cut evenly into as many tiles as this needs.  A launch lasts as long as its even
-// share and, where there is more than one round, half of what the longest tile sticks out; with one round as long as that tile.
-// Splitting costs the launch that joins the partials.
-int32_t choose_chunk(const TileKind& kind, const std::vector<std::pair<int32_t, double>>& ranges) {  // keys, and how many tiles have this range
+// A sequence's key range: `tiles` tiles of `cols` query columns each have it, for every KV head.
+struct KeyRange {
+    int32_t keys, tiles, cols;
+};
+
+// How long the tiles take, the longest first and each where there is room next.  One KV head's tiles on its share of the slots: the
+// heads are alike.
+double last_tile_end(std::vector<double>& tiles, int32_t slots) {
+    std::sort(tiles.begin(), tiles.end(), std::greater<double>());
+    std::vector<double> ends;  // heap, the earliest on top
+    for (double t : tiles) {
+        if ((int32_t)ends.size() < slots) {
+            ends.push_back(t);
+            if ((int32_t)ends.size() == slots) std::make_heap(ends.begin(), ends.end(), std::greater<double>());
+            continue;
+        }
+        std::pop_heap(ends.begin(), ends.end(), std::greater<double>());
+        ends.back() += t;
+        std::push_heap(ends.begin(), ends.end(), std::greater<double>());
+    }
+    return *std::max_element(ends.begin(), ends.end());
+}
+
+// Keys per tile, about: every sequence's range is cut evenly into as many tiles as this needs.  Fewer tiles start less often and leave
+// fewer partials, more fill the slots more evenly.  Up to four rounds the tiles are laid out to see how long they take; many short
+// ones last about their even share and half of the longest.
+int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, int32_t heads) {
     int32_t longest = 1;
-    for (const auto& r : ranges) longest = std::max(longest, r.first);
+    for (const auto& r : ranges) longest = std::max(longest, r.keys);
+    const int32_t slots = std::max(1, kind.slots / heads);
     int32_t chunk = kind.max_chunk;
     double best = -1;
+    std::vector<double> tiles;
     for (double c = std::min<double>(kind.max_chunk, longest); c >= kind.step; c *= 0.84) {
-        double tiles = 0, sum = 0, most = 0;
-        bool split = false;
+        double count = 0, sum = 0, most = 0, joined = 0;
         for (const auto& r : ranges) {
-            const double pieces = (double)((r.first + (int64_t)c - 1) / (int64_t)c);
-            const double cost = r.first / pieces + kind.start_keys;
-            tiles += pieces * r.second;
-            sum += pieces * r.second * cost;
+            const double pieces = (double)((r.keys + (int64_t)c - 1) / (int64_t)c);
+            const double cost = r.keys / pieces + kind.start_keys;
+            count += pieces * r.tiles;
+            sum += pieces * r.tiles * cost;
             most = std::max(most, cost);
-            split |= pieces > 1;
+            if (pieces > 1) joined += pieces * r.tiles * r.cols;
         }
-        if (tiles > kMaxTiles) break;
-        const double est = (tiles <= kind.slots ? most : sum / kind.slots + 0.5 * most) + (split ? kind.join_keys : 0);
+        if (count * heads > kMaxTiles) break;
+        double est = count <= slots ? most : sum / slots + 0.5 * most;
+        if (count > slots && count <= 4.0 * slots) {
+            tiles.clear();
+            for (const auto& r : ranges) {
+                const int64_t pieces = (r.keys + (int64_t)c - 1) / (int64_t)c;
+                tiles.insert(tiles.end(), (size_t)(pieces * r.tiles), (double)r.keys / pieces + kind.start_keys);
+            }
+            est = last_tile_end(tiles, slots);
+        }
+        if (joined > 0) est += kind.join_keys + kind.column_keys * joined * heads;
         if (best < 0 || est < best) {
             best = est;
             chunk = (int32_t)c;
         }
-        if (tiles > 16 * kind.slots) break;
+        if (count > 16.0 * slots) break;
     }
     return chunk;
 }
@@ -55,20 +91,22 @@ bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int
     plan->score_floats = 0;
     plan->partial_floats = 0;
     plan->join_cols = 0;
-    const TileKind narrow = {kMaxTreeChunk, kTreeStep, 256, 256, 2.0 * num_cus};
-    const TileKind wide = {kMaxTreeBlockChunk, kTileTokens, 192, 192, 1.0 * num_cus};
+    const TileKind narrow = {kMaxTreeChunk, kTreeStep, 256, 256, 0, 2 * num_cus};
+    // Measured over batches of 4, 6 and 32 sequences cut into 512 to 8192 keys (D = 128): a row block takes 6.6 us and 1.2 us per 64
+    // keys, a split launch 9.5 us more and 0.2 us per 1000 columns of partials.
+    const TileKind wide = {kMaxTreeBlockChunk, kTileTokens, 350, 500, 0.0114, num_cus};
     const int block_rows = kMfmaCols / G;
     double fewest = 0;
-    std::vector<std::pair<int32_t, double>> narrow_ranges, wide_ranges;
+    std::vector<KeyRange> narrow_ranges, wide_ranges;
     for (int i = 0; i < B; ++i) {
         const bool is_wide = (int64_t)n[i] * G > kTreeCols;
-        const double blocks = is_wide ? (double)((n[i] + (int64_t)block_rows - 1) / block_rows) : 1.0;
-        (is_wide ? wide_ranges : narrow_ranges).push_back({L[i] + n[i], blocks * Hkv});
-        fewest += blocks * Hkv * (((double)L[i] + n[i]) / kMaxTreeChunk + 1);
+        const int32_t blocks = is_wide ? (n[i] - 1) / block_rows + 1 : 1;
+        (is_wide ? wide_ranges : narrow_ranges).push_back({L[i] + n[i], blocks, is_wide ? (n[i] + blocks - 1) / blocks * G : n[i] * G});
+        fewest += (double)blocks * Hkv * (((double)L[i] + n[i]) / kMaxTreeChunk + 1);
     }
     if (fewest > kMaxTiles) return false;
-    const int32_t narrow_chunk = narrow_ranges.empty() ? 0 : choose_chunk(narrow, narrow_ranges);
-    const int32_t wide_chunk = wide_ranges.empty() ? 0 : choose_chunk(wide, wide_ranges);
+    const int32_t narrow_chunk = narrow_ranges.empty() ? 0 : choose_chunk(narrow, narrow_ranges, Hkv);
+    const int32_t wide_chunk = wide_ranges.empty() ? 0 : choose_chunk(wide, wide_ranges, Hkv);
     int32_t grow0 = 0;
     for (int i = 0; i < B; ++i) {
         const int32_t total = L[i] + n[i];
