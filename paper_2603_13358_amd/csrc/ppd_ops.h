@@ -17,6 +17,7 @@ constexpr int kTreeStep = kSlab * kTreeWaves;  // split boundaries are multiples
 constexpr int kMaxTreeChunk = 8192;  // keys per tree tile at most (its page ids are staged in LDS)
 constexpr int kMaxTreeBlockChunk = 16384;  // the same of a row block
 constexpr int kMaxMaskWords = 16;    // 64-bit words of a row's tree mask at most
+constexpr int kKeptScores = 19200;  // scores that a tree tile holds in LDS: two workgroups' fill a unit
 constexpr int kWeighKeys = 256;      // keys of a workgroup that adds up attention weights
 constexpr int kSelectBatch = 512;    // sequences per launch of the select kernel (their lengths are kernel arguments)
 constexpr int kSelectChunk = 16384;  // weights that a workgroup of the select kernels holds in registers
@@ -48,15 +49,13 @@ struct TreeGroup {
 // Keys [kv_begin, min(kv_begin + kWeighKeys, kv_total)) of one sequence and KV head, whose weights are added up over all its columns.
 struct WeighItem {
     int32_t seq, kvh, grow0, cols;
-    int32_t L, kv_total, kv_begin, unused;
-    int64_t score_off;         // floats: scores [column][score_stride], or -1: they are computed again
+    int32_t L, kv_total, kv_begin;
+    int32_t group;             // of kept scores, where the range was split; or -1
+    int64_t score_off;         // floats: scores [slab][column][32 keys], or -1: they are computed again
 };
 
-// Keys of a row of kept scores: whole slabs, whose every key is written.
-#ifdef __HIPCC__
-__host__ __device__
-#endif
-constexpr int32_t score_stride(int32_t kv_total) { return (kv_total + kSlab - 1) / kSlab * kSlab; }
+// Keys of kept scores: whole slabs, whose every key is written.
+constexpr int32_t score_keys(int32_t kv_total) { return (kv_total + kSlab - 1) / kSlab * kSlab; }
 
 struct TreePlan {
     std::vector<TreeItem> items;           // tiles of sequences with at most kTreeCols query columns

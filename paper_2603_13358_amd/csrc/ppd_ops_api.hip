@@ -245,11 +245,11 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
         rc = ppd::launch_tree(p, D, ctx->fp8_pages, stream);
         if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch tree attention");
     }
-    if (p.n_groups > 0) {
+    if (p.n_groups > 0 || p.n_score_weighs > 0) {
         rc = ppd::launch_tree_join(p, D, stream);
         if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch join of tree tiles");
     }
-    if (weighted) {
+    if (p.n_weighs > 0) {
         rc = ppd::launch_weigh(p, D, ctx->fp8_pages, stream);
         if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch weights");
     }

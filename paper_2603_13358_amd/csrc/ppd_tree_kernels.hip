@@ -42,14 +42,17 @@ __device__ __forceinline__ void stage_pages(const TreeParams& P, int seq, int kv
 // A tree tile: up to 32 query columns against a range of keys.  Four waves, each with every fourth slab of 32 keys, which it
 // takes from the pool straight into registers in the layouts of the matrix instructions' operands: no LDS, no barrier.  The
 // waves' results meet in LDS at the end.
-template <int HD, bool FP8>
-__global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreeParams P) {
+template <int HD, bool FP8, bool SCORES>
+__device__ __forceinline__ void tree_tile(const TreeParams& P) {
     typedef typename Granule<FP8>::type Raw;
     constexpr int EB = FP8 ? 1 : 2, KS = HD / 16, DB = HD / 32;
     constexpr int CB = 16;          // columns that meet in LDS at a time
     constexpr int ROW = HD + 4;     // floats of a staged column: the padding spreads the columns over the banks
     __shared__ int ids[kMaxTreeChunk / kPage];
-    __shared__ __attribute__((aligned(16))) float stage[kTreeWaves][CB * ROW];
+    // one after the other: the tile's scores (SCORES), the waves' results
+    constexpr int AREA = kTreeWaves * CB * ROW;
+    __shared__ __attribute__((aligned(16))) float area[SCORES && kKeptScores > AREA ? kKeptScores : AREA];
+    float (&stage)[kTreeWaves][CB * ROW] = *reinterpret_cast<float (*)[kTreeWaves][CB * ROW]>(area);
     __shared__ float stage_ml[kTreeWaves][CB][2];
 
     const TreeItem it = P.items[blockIdx.x];
@@ -60,8 +63,9 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
     const float c = P.scale_log2e;
     const uint64_t* const words = P.mask ? P.mask + (int64_t)(it.grow0 + jrow) * P.mask_words : nullptr;
 
-    float* const scores = it.score_off >= 0 ? P.scores + it.score_off + (int64_t)col * score_stride(it.kv_total) + h * 8 : nullptr;
-
+    // SCORES: every slab leaves a block of [column][32 keys].  The stores are asked for whether a lane has a column or not -- a buffer
+    // store beyond the block's end is dropped -- because behind stores that some path leaves out, the wait for V would be for the next
+    // slab's K as well (64 decodes of 1K-8K keys 172 -> @@ us).
     const int slabs = (it.kv_end - it.kv_begin + kSlab - 1) / kSlab;
     stage_pages(P, it.seq, it.kv_begin, it.kv_total, slabs * 2, ids);
     bf16x8 qreg[KS];
@@ -144,10 +148,12 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
                         }
             }
         }
-        if (scores && l32 < it.ncols) {
+        if constexpr (SCORES) {
+            if (it.score_off >= 0 && l32 < it.ncols) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<f32x4*>(scores + base + (i >> 1) * 16 + (i & 1) * 4) = f32x4{sc[4 * i], sc[4 * i + 1], sc[4 * i + 2], sc[4 * i + 3]};
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<f32x4*>(&area[(s * it.ncols + l32) * kSlab + h * 8 + (i >> 1) * 16 + (i & 1) * 4]) = f32x4{sc[4 * i], sc[4 * i + 1], sc[4 * i + 2], sc[4 * i + 3]};
+            }
         }
         // The exponentials are taken against the running reference as it is; only where a lane's sum of 16 of them is above
         // 2^kLazyRescale (or not a number: no reference yet) is the maximum looked for and everything rescaled.
@@ -223,6 +229,18 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
         step(s, std::true_type{});
     }
 
+    // The scores leave at the end, all at once: stores of every slab on its own made the wait for V one for their arrival (64 decodes of
+    // 1K-8K keys 173 us, 142 without stores, 159 this way).  Stores of device scope: left in L2 they go to memory when the launch
+    // ends, with nothing to do meanwhile (165).
+    if constexpr (SCORES) {
+        __syncthreads();
+        if (it.score_off >= 0) {
+            const int floats = slabs * it.ncols * kSlab;
+            const auto to = __builtin_amdgcn_make_buffer_rsrc(P.scores + it.score_off + (int64_t)(it.kv_begin / kSlab) * (it.ncols * kSlab), 0, floats * 4, 0x00020000);
+            constexpr int DEVICE_SCOPE = 16;  // sc1
+            for (int i = tid * 4; i < floats; i += kTreeThreads * 4) __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const u32x4*>(&area[i]), to, i * 4, 0, DEVICE_SCOPE);
+        }
+    }
     const float l_tot = sum_halves(l_run);
     for (int c0 = 0; c0 < it.ncols; c0 += CB) {
         __syncthreads();
@@ -271,15 +289,19 @@ __global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreePar
     }
 }
 
+template <int HD, bool FP8>
+__global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_kernel(const TreeParams P) { tree_tile<HD, FP8, false>(P); }
+template <int HD, bool FP8>
+__global__ __launch_bounds__(kTreeThreads, 2) void ppd_tree_scores_kernel(const TreeParams P) { tree_tile<HD, FP8, true>(P); }
+
 // Joins the partials of split key ranges, splits in order.  Bound by latency: the (m, l) pairs of a workgroup's columns go to LDS all at
 // once, and a lane asks for eight splits' values before it adds the first.  One lane after the other over 32 splits took 24 us.
 constexpr int kJoinPairs = 2048;
 template <int HD>
-__global__ __launch_bounds__(256) void ppd_tree_join_kernel(const TreeParams P) {
+__device__ __forceinline__ void join_columns(const TreeParams& P, int group, int part, f32x2* ml) {
     constexpr int LANES = HD / 4, COLS = 256 / LANES, AT_ONCE = 8;
-    __shared__ f32x2 ml[kJoinPairs];
-    const TreeGroup g = P.groups[blockIdx.x];
-    const int c0 = blockIdx.y * COLS, cl = threadIdx.x / LANES, col = c0 + cl, d = (threadIdx.x % LANES) * 4;
+    const TreeGroup g = P.groups[group];
+    const int c0 = part * COLS, cl = threadIdx.x / LANES, col = c0 + cl, d = (threadIdx.x % LANES) * 4;
     if (c0 >= g.ncols) return;
     const float c = P.scale_log2e;
     const float* base = P.partials + g.part_off;
@@ -414,22 +436,75 @@ __global__ __launch_bounds__(256, 2) void ppd_weigh_kernel(const TreeParams P) {
 
 // Adds up the weights of sequences with few query columns, whose scores ppd_tree_kernel has left in the workspace: a thread to a key.
 // The scores of G columns are 8 G bytes a key, written and read, where K again would be 2 D: 64 decodes of 1K-8K keys (32 query
-// heads, D = 128) 106 us that way, 17 this way.
-__global__ __launch_bounds__(kWeighKeys) void ppd_weigh_scores_kernel(const TreeParams P) {
-    const WeighItem it = P.score_weighs[blockIdx.x];
-    const int key = it.kv_begin + (int)threadIdx.x;
-    if (key >= it.kv_total) return;
+// heads, D = 128) 106 us that way, 14 this way.  Where the range was split, the references come from the partials' own pairs, so
+// that nothing waits for the join.
+template <int HD>
+__device__ __forceinline__ void weigh_scores(const TreeParams& P, const WeighItem& it, f32x2* ml) {
+    const int tid = threadIdx.x, cols = it.cols;
     const float c = P.scale_log2e;
-    const float* scores = P.scores + it.score_off + key;
-    const int stride = score_stride(it.kv_total);
-    float sum = 0.f;
-    for (int cc = 0; cc < it.cols; ++cc) {
-        const int row = cc / P.G;
-        const f32x2 w = *reinterpret_cast<const f32x2*>(P.stats + ((int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G)) * 2);
-        sum += fast_exp2(__builtin_fmaf(scores[(int64_t)cc * stride], c, -(w[0] * c))) * w[1];
+    constexpr int PARTS = kWeighKeys / kTreeCols;  // threads that go over a column's splits
+    constexpr int AHEAD = 8;  // scores asked for before the references are known
+    const int key = it.kv_begin + tid, safe = key < it.kv_total ? key : it.kv_total - 1;
+    const float* scores = P.scores + it.score_off + (int64_t)(safe / kSlab) * (cols * kSlab) + safe % kSlab;
+    float* to = P.weights + ((int64_t)it.seq * P.Hkv + it.kvh) * P.weight_stride + safe;
+    float ahead[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ahead[i] = scores[(i < cols ? i : 0) * kSlab];
+    const float old = *to;
+    if (it.group >= 0) {
+        const TreeGroup g = P.groups[it.group];
+        const int cc = tid % kTreeCols, part = tid / kTreeCols;
+        const float* pairs = P.partials + g.part_off + (int64_t)cols * HD + cc * 2;
+        float m = NEG_INF, l = 0.f;
+        if (cc < cols) {
+            for (int j = part; j < g.nsplit; j += PARTS) {
+                const f32x2 w = *reinterpret_cast<const f32x2*>(pairs + g.part_stride * j);
+                const float top = fmaxf(m, w[0]);
+                if (w[0] == NEG_INF) continue;
+                l = l * fast_exp2((m - top) * c) + w[1] * fast_exp2((w[0] - top) * c);
+                m = top;
+            }
+        }
+        ml[tid] = f32x2{m, l};
+        __syncthreads();
+        m = NEG_INF;
+        l = 0.f;
+        if (tid < kTreeCols) {
+#pragma unroll
+            for (int k = 0; k < PARTS; ++k) m = fmaxf(m, ml[k * kTreeCols + tid][0]);
+#pragma unroll
+            for (int k = 0; k < PARTS; ++k) {
+                const f32x2 w = ml[k * kTreeCols + tid];
+                if (w[0] != NEG_INF) l += w[1] * fast_exp2((w[0] - m) * c);
+            }
+        }
+        __syncthreads();
+        if (tid < kTreeCols) ml[tid] = f32x2{m == NEG_INF ? 0.f : m * c, l == 0.f ? 0.f : 1.0f / l};
+    } else if (tid < cols) {
+        const int row = tid / P.G;
+        const f32x2 w = *reinterpret_cast<const f32x2*>(P.stats + ((int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (tid - row * P.G)) * 2);
+        ml[tid] = f32x2{w[0] * c, w[1]};
     }
-    float* to = P.weights + ((int64_t)it.seq * P.Hkv + it.kvh) * P.weight_stride + key;
-    *to = key < it.L ? *to + sum : sum;
+    __syncthreads();
+    if (key >= it.kv_total) return;
+    float sum = 0.f;
+    auto add = [&](float score, int cc) { sum += fast_exp2(__builtin_fmaf(score, c, -ml[cc][0])) * ml[cc][1]; };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (i < cols) add(ahead[i], i);
+    for (int cc = AHEAD; cc < cols; ++cc) add(scores[cc * kSlab], cc);
+    *to = key < it.L ? old + sum : sum;
+}
+
+// Behind the tiles: joins their partials and adds up the weights of kept scores, in one launch (one decode of 4000 keys 17.1 us with
+// a launch each, @@ with one).
+static_assert(kWeighKeys == 256, "both parts work with 256 threads");
+template <int HD>
+__global__ __launch_bounds__(256) void ppd_tree_join_kernel(const TreeParams P, int parts) {
+    __shared__ f32x2 ml[kJoinPairs];
+    const int joins = P.n_groups * parts;
+    if ((int)blockIdx.x < joins) join_columns<HD>(P, blockIdx.x / parts, blockIdx.x % parts, ml);
+    else weigh_scores<HD>(P, P.score_weighs[blockIdx.x - joins], ml);
 }
 
 #define PPD_BY_FORM(KERNEL, GRID, THREADS)                                                                                        \
@@ -442,23 +517,23 @@ __global__ __launch_bounds__(kWeighKeys) void ppd_weigh_scores_kernel(const Tree
 
 int launch_tree(const TreeParams& p, int head_dim, bool fp8_pages, void* stream) {
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    PPD_BY_FORM(ppd_tree_kernel, dim3((unsigned)p.n_items), kTreeThreads);
+    if (p.n_score_weighs > 0) PPD_BY_FORM(ppd_tree_scores_kernel, dim3((unsigned)p.n_items), kTreeThreads);
+    else PPD_BY_FORM(ppd_tree_kernel, dim3((unsigned)p.n_items), kTreeThreads);
     return (int)hipGetLastError();
 }
 
 int launch_tree_join(const TreeParams& p, int head_dim, void* stream) {
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    const int cols = 256 / (head_dim / 4);  // per workgroup
-    const dim3 grid((unsigned)p.n_groups, (unsigned)((p.join_cols + cols - 1) / cols));
-    if (head_dim == 128) hipLaunchKernelGGL(ppd_tree_join_kernel<128>, grid, dim3(256), 0, hs, p);
-    else hipLaunchKernelGGL(ppd_tree_join_kernel<64>, grid, dim3(256), 0, hs, p);
+    const int cols = 256 / (head_dim / 4), parts = (p.join_cols + cols - 1) / cols;  // columns of a workgroup, workgroups of a group
+    const dim3 grid((unsigned)(p.n_groups * parts + p.n_score_weighs));
+    if (head_dim == 128) hipLaunchKernelGGL(ppd_tree_join_kernel<128>, grid, dim3(256), 0, hs, p, parts);
+    else hipLaunchKernelGGL(ppd_tree_join_kernel<64>, grid, dim3(256), 0, hs, p, parts);
     return (int)hipGetLastError();
 }
 
 int launch_weigh(const TreeParams& p, int head_dim, bool fp8_pages, void* stream) {
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    if (p.n_score_weighs > 0) hipLaunchKernelGGL(ppd_weigh_scores_kernel, dim3((unsigned)p.n_score_weighs), dim3(kWeighKeys), 0, hs, p);
-    if (p.n_weighs > 0) PPD_BY_FORM(ppd_weigh_kernel, dim3((unsigned)p.n_weighs), 256);
+    PPD_BY_FORM(ppd_weigh_kernel, dim3((unsigned)p.n_weighs), 256);
     return (int)hipGetLastError();
 }
 

@@ -96,13 +96,19 @@ bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int
     // keys, a split launch 9.5 us more and 0.2 us per 1000 columns of partials.
     const TileKind wide = {kMaxTreeBlockChunk, kTileTokens, 350, 500, 0.0114, num_cus};
     const int block_rows = kMfmaCols / G;
+    // Scores are kept where writing and reading them (8 bytes a column and key) moves less than reading K again.
+    auto keeps_scores = [&](int32_t rows) { return weighted && (int64_t)rows * G <= kTreeCols && (int64_t)rows * G * 8 <= (int64_t)D * kv_elem_bytes; };
+    auto max_piece = [&](int32_t rows) {
+        if ((int64_t)rows * G > kTreeCols) return wide.max_chunk;
+        return keeps_scores(rows) ? std::min(narrow.max_chunk, kKeptScores / (rows * G) / narrow.step * narrow.step) : narrow.max_chunk;
+    };
     double fewest = 0;
     std::vector<KeyRange> narrow_ranges, wide_ranges;
     for (int i = 0; i < B; ++i) {
         const bool is_wide = (int64_t)n[i] * G > kTreeCols;
         const int32_t blocks = is_wide ? (n[i] - 1) / block_rows + 1 : 1;
         (is_wide ? wide_ranges : narrow_ranges).push_back({L[i] + n[i], blocks, is_wide ? (n[i] + blocks - 1) / blocks * G : n[i] * G});
-        fewest += (double)blocks * Hkv * (((double)L[i] + n[i]) / kMaxTreeChunk + 1);
+        fewest += (double)blocks * Hkv * (((double)L[i] + n[i]) / std::min(kMaxTreeChunk, max_piece(n[i])) + 1);
     }
     if (fewest > kMaxTiles) return false;
     const int32_t narrow_chunk = narrow_ranges.empty() ? 0 : choose_chunk(narrow, narrow_ranges, Hkv);
@@ -112,13 +118,13 @@ bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int
         const int32_t total = L[i] + n[i];
         const bool is_wide = (int64_t)n[i] * G > kTreeCols;
         const TileKind& kind = is_wide ? wide : narrow;
-        const int32_t chunk = is_wide ? wide_chunk : narrow_chunk;
+        const bool keep_scores = keeps_scores(n[i]);
+        const int32_t most = max_piece(n[i]);
+        const int32_t chunk = std::min(most, is_wide ? wide_chunk : narrow_chunk);
         const int32_t pieces = (total + chunk - 1) / chunk;
-        const int32_t piece = std::min(kind.max_chunk, ((total + pieces - 1) / pieces + kind.step - 1) / kind.step * kind.step);
+        const int32_t piece = std::min(most, ((total + pieces - 1) / pieces + kind.step - 1) / kind.step * kind.step);
         const int32_t nsplit = (total + piece - 1) / piece;
         const int32_t blocks = is_wide ? (n[i] + block_rows - 1) / block_rows : 1, rows = (n[i] + blocks - 1) / blocks;
-        // Scores are kept where writing and reading them (8 bytes a column and key) moves less than reading K again.
-        const bool keep_scores = weighted && !is_wide && (int64_t)n[i] * G * 8 <= (int64_t)D * kv_elem_bytes;
         for (int h = 0; h < Hkv; ++h) {
             for (int32_t row0 = 0; row0 < n[i]; row0 += rows) {
                 const int32_t nrows = std::min(rows, n[i] - row0), cols = nrows * G;
@@ -153,8 +159,8 @@ bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int
             }
             if (weighted) {
                 std::vector<WeighItem>& list = keep_scores ? plan->score_weighs : plan->weighs;
-                for (int32_t t = 0; t < total; t += kWeighKeys) list.push_back({i, h, grow0, n[i] * G, L[i], total, t, 0, keep_scores ? plan->score_floats : -1});
-                if (keep_scores) plan->score_floats += (int64_t)n[i] * G * score_stride(total);
+                for (int32_t t = 0; t < total; t += kWeighKeys) list.push_back({i, h, grow0, n[i] * G, L[i], total, t, keep_scores && nsplit > 1 ? (int32_t)plan->groups.size() - 1 : -1, keep_scores ? plan->score_floats : -1});
+                if (keep_scores) plan->score_floats += (int64_t)n[i] * G * score_keys(total);
             }
         }
         grow0 += n[i];

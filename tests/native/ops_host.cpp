@@ -265,9 +265,9 @@ static void plans() {
         all.insert(all.end(), p.score_weighs.begin(), p.score_weighs.end());
         std::map<std::pair<int, int>, int64_t> kept;  // where the scores of a sequence and head go
         for (const auto& it : p.items)
-            if (it.score_off >= 0) CHECK(weighted && kept.emplace(std::make_pair(it.seq, it.kvh), it.score_off).first->second == it.score_off);
+            if (it.score_off >= 0) CHECK(weighted && ppd::score_keys(it.kv_end - it.kv_begin) * it.ncols <= ppd::kKeptScores && kept.emplace(std::make_pair(it.seq, it.kvh), it.score_off).first->second == it.score_off);
         std::map<int64_t, int64_t> areas;
-        for (const auto& k : kept) CHECK(areas.emplace(k.second, k.second + (int64_t)n[k.first.first] * G * ppd::score_stride(L[k.first.first] + n[k.first.first])).second);
+        for (const auto& k : kept) CHECK(areas.emplace(k.second, k.second + (int64_t)n[k.first.first] * G * ppd::score_keys(L[k.first.first] + n[k.first.first])).second);
         int64_t area_end = 0;
         for (const auto& a : areas) {
             CHECK(a.first == area_end && a.first % 4 == 0);
@@ -276,6 +276,10 @@ static void plans() {
         CHECK(area_end == p.score_floats);
         for (const auto& w : p.weighs) CHECK(w.score_off < 0);
         for (const auto& w : p.score_weighs) CHECK(kept.at(std::make_pair(w.seq, w.kvh)) == w.score_off);
+        for (const auto& w : p.score_weighs) {
+            if (w.group >= 0) CHECK(p.groups.at(w.group).kvh == w.kvh && p.groups[w.group].grow0 == w.grow0 && p.groups[w.group].ncols == w.cols && p.groups[w.group].col0 == 0);
+            else CHECK(ranges.at(std::make_tuple(w.seq, w.kvh, 0)).size() == 1);
+        }
         with_scores += p.score_weighs.size();
         without += p.weighs.size();
         for (const auto& w : all) {
