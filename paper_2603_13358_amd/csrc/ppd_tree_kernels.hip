@@ -41,7 +41,12 @@ __device__ __forceinline__ void stage_pages(const TreeParams& P, int seq, int kv
 
 // A tree tile: up to 32 query columns against a range of keys.  Four waves, each with every fourth slab of 32 keys, which it
 // takes from the pool straight into registers in the layouts of the matrix instructions' operands: no LDS, no barrier.  The
-// waves' results meet in LDS at the end.
+// waves' results meet in LDS at the end.  Probabilities enter the second product as bf16 numbers, as the matrix instruction takes them
+// (their sum is of the 32-bit ones); everything else is held in 32 bits.
+// Bound by memory where there is much to read: 64 decodes of 1K-8K keys (32 query heads, D = 128) 142 us, 6.6 TB/s; by a chain of
+// dependent loads (tile, page ids, K) of 5 us in small launches.  More than 32 columns as several tiles side by side, their keys read
+// from L2 once more for every 32, were no faster than row blocks from 64 columns on (32 trees of 8-24 nodes, 8 query heads to a KV
+// head: 137-152 us against 137), and two launches where a batch has both kinds.
 template <int HD, bool FP8, bool SCORES>
 __device__ __forceinline__ void tree_tile(const TreeParams& P) {
     typedef typename Granule<FP8>::type Raw;
@@ -63,9 +68,6 @@ __device__ __forceinline__ void tree_tile(const TreeParams& P) {
     const float c = P.scale_log2e;
     const uint64_t* const words = P.mask ? P.mask + (int64_t)(it.grow0 + jrow) * P.mask_words : nullptr;
 
-    // SCORES: every slab leaves a block of [column][32 keys].  The stores are asked for whether a lane has a column or not -- a buffer
-    // store beyond the block's end is dropped -- because behind stores that some path leaves out, the wait for V would be for the next
-    // slab's K as well (64 decodes of 1K-8K keys 172 -> @@ us).
     const int slabs = (it.kv_end - it.kv_begin + kSlab - 1) / kSlab;
     stage_pages(P, it.seq, it.kv_begin, it.kv_total, slabs * 2, ids);
     bf16x8 qreg[KS];
@@ -497,7 +499,7 @@ __device__ __forceinline__ void weigh_scores(const TreeParams& P, const WeighIte
 }
 
 // Behind the tiles: joins their partials and adds up the weights of kept scores, in one launch (one decode of 4000 keys 17.1 us with
-// a launch each, @@ with one).
+// a launch each, 13.8 with one; 64 of 1K-8K 178 and 175).
 static_assert(kWeighKeys == 256, "both parts work with 256 threads");
 template <int HD>
 __global__ __launch_bounds__(256) void ppd_tree_join_kernel(const TreeParams P, int parts) {
