@@ -346,13 +346,18 @@ __device__ __forceinline__ void join_columns(const TreeParams& P, int group, int
 
 // Adds up the weights of sequences with many query columns: S = Q K^T with the keys as columns, so that a lane owns a key and the sum
 // over the queries runs over its own registers.  A wave holds K of 64 keys, read once, and goes over the sequence's query columns, 32 at
-// a time, the next ones' Q on its way meanwhile.  The reference and one over the sum of every row come from the attention before.
+// a time, which the workgroup brings to LDS, the next ones on their way meanwhile (each wave for itself, in pieces of 16 bytes of 32
+// rows, they kept the load unit busy: the last 16-33 rows of 4 prompts of 4K-32K, 40
+// query heads, 55 us, this way 50: 2.9 TB/s of K; a workgroup's start -- tile, page ids, K -- and 5 steps of 32 columns, two workgroups
+// to a unit, three no faster).  The reference and one over the sum of every row come from the attention before.
 constexpr int kWeighCols = 256;  // columns whose references are in LDS at a time
 template <int HD, bool FP8>
 __global__ __launch_bounds__(256, 2) void ppd_weigh_kernel(const TreeParams P) {
     typedef typename Granule<FP8>::type Raw;
     constexpr int EB = FP8 ? 1 : 2, KS = HD / 16, SLABS = kWeighKeys / 4 / kSlab;
+    constexpr int QG = HD / 64, QROW = HD * 2 + 16;  // granules of 32 columns that a thread fetches; bytes of a column in LDS
     __shared__ int ids[kWeighKeys / kPage];
+    __shared__ __attribute__((aligned(16))) char queries[2][32 * QROW];
     __shared__ f32x2 ml[kWeighCols];
     __shared__ int rows[kWeighCols];
     const WeighItem it = P.weighs[blockIdx.x];
@@ -363,11 +368,13 @@ __global__ __launch_bounds__(256, 2) void ppd_weigh_kernel(const TreeParams P) {
         const int row = cc / P.G;
         return ((int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G));
     };
-    u32x4 qnext[KS];
+    u32x4 qnext[QG];
     auto load_q = [&](int c0) {
-        const uint16_t* qp = P.q + q_at(c0 + l32) * HD + h * 8;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) qnext[ks] = *reinterpret_cast<const u32x4*>(qp + ks * 16);
+        for (int j = 0; j < QG; ++j) {
+            const int i = tid + j * 256;
+            qnext[j] = *reinterpret_cast<const u32x4*>(P.q + q_at(c0 + i / (HD / 8)) * HD + i % (HD / 8) * 8);
+        }
     };
     stage_pages(P, it.seq, it.kv_begin, it.kv_total, kWeighKeys / kPage, ids);
     load_q(0);
@@ -390,15 +397,24 @@ __global__ __launch_bounds__(256, 2) void ppd_weigh_kernel(const TreeParams P) {
         const int b1 = b0 + kWeighCols < it.cols ? b0 + kWeighCols : it.cols;
         if (b0 > 0) __syncthreads();
         {
-            const int cc = b0 + tid;  // columns past the end count nothing
-            ml[tid] = cc < it.cols ? *reinterpret_cast<const f32x2*>(P.stats + q_at(cc) * 2) : f32x2{0.f, 0.f};
+            const int cc = b0 + tid;  // columns past the end count nothing: their exponentials are 0, and so is the factor
+            ml[tid] = cc < it.cols ? *reinterpret_cast<const f32x2*>(P.stats + q_at(cc) * 2) : f32x2{1e30f, 0.f};
+            ml[tid][0] *= c;
             rows[tid] = cc < it.cols ? cc / P.G : -1;
         }
         __syncthreads();
         for (int c0 = b0; c0 < b1; c0 += 32) {
+            char* const qcols = queries[c0 / 32 & 1];
+#pragma unroll
+            for (int j = 0; j < QG; ++j) {
+                const int i = tid + j * 256;
+                *reinterpret_cast<u32x4*>(qcols + i / (HD / 8) * QROW + i % (HD / 8) * 16) = qnext[j];
+            }
+            __syncthreads();
+            if (c0 + 32 < it.cols) load_q(c0 + 32);
             bf16x8 qreg[KS];
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) qreg[ks] = as_bf16x8(qnext[ks]);
+            for (int ks = 0; ks < KS; ++ks) qreg[ks] = as_bf16x8(*reinterpret_cast<const u32x4*>(qcols + l32 * QROW + ks * 32 + h * 16));
             f32x16 sc[SLABS];
 #pragma unroll
             for (int s = 0; s < SLABS; ++s)
@@ -408,19 +424,14 @@ __global__ __launch_bounds__(256, 2) void ppd_weigh_kernel(const TreeParams P) {
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
                 for (int s = 0; s < SLABS; ++s) sc[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qreg[ks], as_bf16x8(kreg[s][ks]), sc[s], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-            if (c0 + 32 < it.cols) load_q(c0 + 32);
-            __builtin_amdgcn_sched_barrier(0);
-            const bool whole = !tail && c0 + 32 <= it.cols;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int r = c0 - b0 + (i & 3) + 8 * (i >> 2) + 4 * h;
                 const f32x2 w = ml[r];
-                const float mc = w[0] * c;
 #pragma unroll
                 for (int s = 0; s < SLABS; ++s) {
-                    const float p = fast_exp2(__builtin_fmaf(sc[s][i], c, -mc)) * w[1];
-                    if (whole || (rows[r] >= 0 && base + s * kSlab + l32 <= it.L + rows[r])) sum[s] += p;
+                    const float p = fast_exp2(__builtin_fmaf(sc[s][i], c, -w[0])) * w[1];
+                    if (!tail || (rows[r] >= 0 && base + s * kSlab + l32 <= it.L + rows[r])) sum[s] += p;
                 }
             }
         }
