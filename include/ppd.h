@@ -233,7 +233,9 @@ ppd_status ppd_mixed_attention_static(ppd_ctx *ctx, const void *q, const void *k
  * contexts that outgrow the pool are cut down to the tokens that attention looks at.  Four calls, on pools of either element
  * format, all asynchronous on `stream` and under the conventions above (a plan changed under capture is refused, as by
  * ppd_mixed_attention; ppd_kv_select of rows above 16384 tokens needs a workspace, and is refused under capture until a call as
- * large has run eagerly; ppd_kv_compact can always be captured). */
+ * large has run eagerly; ppd_kv_compact can always be captured).  A captured graph reads the plan and workspace of its capture: it may
+ * be replayed until a call of these on the same context has planned other lengths or needed a larger workspace.  A program
+ * that does both keeps a context of its own for its graphs. */
 
 /* Attention for a tree of drafted tokens over the cache.  Sequence i has L_i cached tokens and n_i drafted nodes, whose K/V have been
  * appended at positions L_i .. L_i + n_i - 1 (in any order in which the caller numbers them).  Row j sees the keys 0 .. L_i - 1 and
@@ -253,7 +255,8 @@ ppd_status ppd_tree_attention(ppd_ctx *ctx, const void *q, const void *kv_pages,
  * for t < L_i + n_i; entries behind are not touched, so appended tokens need no clearing.
  *   weights       device float [B][Hkv][weight_stride], 4-byte aligned, weight_stride >= L_i + n_i
  *   the rest      as for ppd_mixed_attention
- * Sums are binary32 in a fixed order: bitwise the same from run to run. */
+ * Sums are binary32 in a fixed order: bitwise the same from run to run.  Sequences of few query columns (n_i * G * 8 bytes at most one
+ * key's K) leave their scores in the workspace, 4 n_i G bytes a key and KV head, allocated with the plan. */
 ppd_status ppd_weighted_attention(ppd_ctx *ctx, const void *q, const void *kv_pages, const int32_t *page_tables,
                                   int32_t max_pages, const int32_t *L, const int32_t *n, int32_t B, float scale,
                                   void *out, float *weights, int64_t weight_stride, void *stream);
