@@ -324,6 +324,10 @@ WEIGHTED = [  # L, n, query heads, KV heads, head_dim, FP8 pages
     ([1023, 70], [5, 90], 12, 2, 128, True),
     ([333], [1], 8, 2, 64, True),
     ([2050, 31], [32, 1], 5, 1, 128, False),
+    ([3000, 700], [4, 4], 8, 1, 128, False),         # 32 columns, whose scores fill a tile's LDS at 512 keys
+    ([5000], [2], 16, 2, 128, True),
+    ([2600, 40, 1200], [2, 50, 1], 10, 2, 64, False),  # kept scores, scores computed again, and row blocks in one batch
+    ([9000], [3], 4, 2, 64, False),
 ]
 
 
