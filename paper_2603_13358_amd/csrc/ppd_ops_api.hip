@@ -161,20 +161,23 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
     }
     hipStream_t hs = static_cast<hipStream_t>(stream);
     PPD_HIP(ctx, hipSetDevice(ctx->device));
-    TreeState* t = nullptr;
-    ppd_status st = tree_state(ctx, &t);
-    if (st != PPD_OK) return st;
-    // As with mixed attention: a context serves one stream at a time, and under capture nothing can be planned or allocated.
+    // As with mixed attention: a context serves one stream at a time, and under capture nothing can be planned or allocated, the state
+    // of a context's first call among it.
     hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
     PPD_HIP(ctx, hipStreamIsCapturing(hs, &capturing));
     const bool in_capture = capturing != hipStreamCaptureStatusNone;
-    if (!in_capture) st = follow_stream(ctx, hs);
+    const auto refuse_in_capture = [&] {
+        return fail(ctx, PPD_ERR_RANGE, "plan changed under capture: run the step once eagerly with these L, n and options first, then capture it");
+    };
+    if (in_capture && !ctx->tree) return refuse_in_capture();
+    TreeState* t = nullptr;
+    ppd_status st = tree_state(ctx, &t);
+    if (st == PPD_OK && !in_capture) st = follow_stream(ctx, hs);
     if (st != PPD_OK) return st;
     const bool reuse = t->on_device && t->weighted == weighted && t->fp8_pages == ctx->fp8_pages && (int32_t)t->L.size() == B &&
                        std::memcmp(t->L.data(), L, sizeof(int32_t) * B) == 0 && std::memcmp(t->n.data(), n, sizeof(int32_t) * B) == 0;
     if (!reuse) {
-        if (in_capture)
-            return fail(ctx, PPD_ERR_RANGE, "plan changed under capture: run the step once eagerly with these L, n and options first, then capture it");
+        if (in_capture) return refuse_in_capture();
         st = upload_tree_plan(ctx, t, L, n, B, weighted, hs);
         if (st != PPD_OK) return st;
     }
@@ -273,21 +276,21 @@ ppd_status guarded(ppd_ctx* ctx, F f) {
 
 // Rows of more than one chunk leave histograms and candidates in the workspace between their launches.
 ppd_status select_workspace(ppd_ctx* ctx, ppd::SelectParams* p, int32_t longest, hipStream_t hs) {
-    TreeState* t = nullptr;
-    ppd_status st = tree_state(ctx, &t);
-    if (st != PPD_OK) return st;
     p->max_chunks = (longest + ppd::kSelectChunk - 1) / ppd::kSelectChunk;
     const size_t rows = (size_t)p->B * p->Hkv, chunks = rows * p->max_chunks;
     if (chunks > (size_t)INT32_MAX) return fail(ctx, PPD_ERR_RANGE, "more rows of this length than one launch takes");
+    const size_t bytes = (chunks * (ppd::kSelectBins + 2 * ppd::kSelectChunk) + rows * (p->max_chunks + ppd::kSelectRowWords)) * sizeof(uint32_t);
     hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
     PPD_HIP(ctx, hipStreamIsCapturing(hs, &capturing));
-    const size_t bytes = (chunks * (ppd::kSelectBins + 2 * ppd::kSelectChunk) + rows * (p->max_chunks + ppd::kSelectRowWords)) * sizeof(uint32_t);
+    if (capturing != hipStreamCaptureStatusNone && (!ctx->tree || bytes > static_cast<TreeState*>(ctx->tree)->d_select_bytes))
+        return fail(ctx, PPD_ERR_RANGE, "rows this long need a workspace, which cannot be allocated under capture: run the call once eagerly first");
+    TreeState* t = nullptr;
+    ppd_status st = tree_state(ctx, &t);
+    if (st != PPD_OK) return st;
     if (capturing == hipStreamCaptureStatusNone) {
         st = follow_stream(ctx, hs);
         if (st == PPD_OK) st = grow_device(ctx, &t->d_select, &t->d_select_bytes, bytes, hs);
         if (st != PPD_OK) return st;
-    } else if (bytes > t->d_select_bytes) {
-        return fail(ctx, PPD_ERR_RANGE, "rows this long need a workspace, which cannot be allocated under capture: run the call once eagerly first");
     }
     p->hist = static_cast<uint32_t*>(t->d_select);
     p->candidates = p->hist + chunks * ppd::kSelectBins;
