@@ -233,9 +233,10 @@ ppd_status ppd_mixed_attention_static(ppd_ctx *ctx, const void *q, const void *k
  * contexts that outgrow the pool are cut down to the tokens that attention looks at.  Four calls, on pools of either element
  * format, all asynchronous on `stream` and under the conventions above (a plan changed under capture is refused, as by
  * ppd_mixed_attention; ppd_kv_select of rows above 16384 tokens needs a workspace, and is refused under capture until a call as
- * large has run eagerly; ppd_kv_compact can always be captured).  A captured graph reads the plan and workspace of its capture: it may
- * be replayed until a call of these on the same context has planned other lengths or needed a larger workspace.  A program
- * that does both keeps a context of its own for its graphs. */
+ * large has run eagerly; ppd_kv_compact can always be captured).  A captured graph reads the plans and the
+ * workspace of its capture: it may be replayed until a call on the same context has planned other lengths for the same kind of
+ * attention (tree or weighted) and page format, or any of these calls has needed a larger workspace, which all of them share.  A
+ * program that does either keeps a context of its own for its graphs. */
 
 /* Attention for a tree of drafted tokens over the cache.  Sequence i has L_i cached tokens and n_i drafted nodes, whose K/V have been
  * appended at positions L_i .. L_i + n_i - 1 (in any order in which the caller numbers them).  Row j sees the keys 0 .. L_i - 1 and

@@ -13,14 +13,23 @@
 
 namespace {
 
-// Plan and workspace of tree and weighted attention.  As with mixed attention the plan on the device stays valid while the lengths do
-// not change: the layers of one engine step call with the same ones.
+// A plan and where it lives on the device.  As with mixed attention it stays valid while the lengths do not change: the layers of one
+// engine step call with the same ones.
+struct TreeSlot {
+    void* d_plan = nullptr;
+    size_t d_plan_bytes = 0;
+    std::vector<int32_t> L, n;
+    bool on_device = false;
+    ppd::TreePlan plan;
+};
+
+// Plans and workspace of tree and weighted attention.  Both kinds of call and both page formats have a plan of their own: a graph that
+// holds calls of one kind is not touched by the other's, and one graph can hold both.
 struct TreeState {
     Staging staging[kStagingSlots];
     uint32_t* flags = nullptr;  // pinned: the words the slots' `read` point at
     int next_slot = 0;
-    void* d_plan = nullptr;
-    size_t d_plan_bytes = 0;
+    TreeSlot slots[2][2];  // [weighted][FP8 pages]
     void* d_partials = nullptr;
     size_t d_partials_bytes = 0;
     void* d_stats = nullptr;
@@ -29,9 +38,6 @@ struct TreeState {
     size_t d_scores_bytes = 0;
     void* d_select = nullptr;
     size_t d_select_bytes = 0;
-    std::vector<int32_t> L, n;
-    bool weighted = false, fp8_pages = false, on_device = false;
-    ppd::TreePlan plan;
 };
 
 void free_tree_state(void* p) {
@@ -40,7 +46,9 @@ void free_tree_state(void* p) {
     for (auto& s : t->staging)
         if (s.host) (void)hipHostFree(s.host);
     if (t->flags) (void)hipHostFree(t->flags);
-    if (t->d_plan) (void)hipFree(t->d_plan);
+    for (auto& kind : t->slots)
+        for (auto& s : kind)
+            if (s.d_plan) (void)hipFree(s.d_plan);
     if (t->d_partials) (void)hipFree(t->d_partials);
     if (t->d_stats) (void)hipFree(t->d_stats);
     if (t->d_scores) (void)hipFree(t->d_scores);
@@ -80,11 +88,11 @@ template <class T>
 size_t bytes_of(const std::vector<T>& v) { return v.size() * sizeof(T); }
 
 // Builds the plan, grows the workspace and enqueues the upload.
-ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, const int32_t* L, const int32_t* n, int32_t B, bool weighted, hipStream_t hs) {
-    t->on_device = false;
-    if (!ppd::build_tree_plan(ctx->shape, L, n, B, weighted, ctx->fp8_pages ? 1 : 2, ctx->num_cus, &t->plan))
+ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, TreeSlot* slot, const int32_t* L, const int32_t* n, int32_t B, bool weighted, hipStream_t hs) {
+    slot->on_device = false;
+    if (!ppd::build_tree_plan(ctx->shape, L, n, B, weighted, ctx->fp8_pages ? 1 : 2, ctx->num_cus, &slot->plan))
         return fail(ctx, PPD_ERR_RANGE, "the batch has more tiles than one launch takes");
-    const ppd::TreePlan& plan = t->plan;
+    const ppd::TreePlan& plan = slot->plan;
     const size_t items = bytes_of(plan.items), blocks = bytes_of(plan.blocks), groups = bytes_of(plan.groups);
     const size_t weighs = bytes_of(plan.weighs), score_weighs = bytes_of(plan.score_weighs);
     const size_t total = items + blocks + groups + weighs + score_weighs, upload = (total + 15) / 16 * 16;
@@ -103,11 +111,15 @@ ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, const int32_t* L, const 
         }
         sg.bytes = want;
     }
-    ppd_status st = grow_device(ctx, &t->d_plan, &t->d_plan_bytes, upload, hs);
+    ppd_status st = grow_device(ctx, &slot->d_plan, &slot->d_plan_bytes, upload, hs);
     if (st == PPD_OK) st = grow_device(ctx, &t->d_partials, &t->d_partials_bytes, (size_t)plan.partial_floats * sizeof(float), hs);
     if (st == PPD_OK && weighted) st = grow_device(ctx, &t->d_stats, &t->d_stats_bytes, (size_t)plan.rows * ctx->shape.num_q_heads * 2 * sizeof(float), hs);
     if (st == PPD_OK) st = grow_device(ctx, &t->d_scores, &t->d_scores_bytes, (size_t)plan.score_floats * sizeof(float), hs);
-    if (st != PPD_OK) return st;
+    if (st != PPD_OK) {  // the workspace may be gone: every plan has to ask for its own again
+        for (auto& kind : t->slots)
+            for (auto& s : kind) s.on_device = false;
+        return st;
+    }
     char* host = static_cast<char*>(sg.host);
     if (items) std::memcpy(host, plan.items.data(), items);
     if (blocks) std::memcpy(host + items, plan.blocks.data(), blocks);
@@ -116,7 +128,7 @@ ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, const int32_t* L, const 
     if (score_weighs) std::memcpy(host + items + blocks + groups + weighs, plan.score_weighs.data(), score_weighs);
     std::memset(host + total, 0, upload - total);
     const uint4* src = reinterpret_cast<const uint4*>(host);
-    uint4* dst = static_cast<uint4*>(t->d_plan);
+    uint4* dst = static_cast<uint4*>(slot->d_plan);
     int64_t granules = (int64_t)(upload / 16);
     uint32_t serial = ++sg.serial;
     void* args[] = {&src, &dst, &granules, &ctx->d_counters, &sg.read, &serial};
@@ -126,11 +138,9 @@ ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, const int32_t* L, const 
         sg.serial -= 1;  // nothing was enqueued: the buffer is free
         return hip_fail(ctx, e, "launch plan upload");
     }
-    t->L.assign(L, L + B);
-    t->n.assign(n, n + B);
-    t->weighted = weighted;
-    t->fp8_pages = ctx->fp8_pages;
-    t->on_device = true;
+    slot->L.assign(L, L + B);
+    slot->n.assign(n, n + B);
+    slot->on_device = true;
     return PPD_OK;
 }
 
@@ -174,15 +184,16 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
     ppd_status st = tree_state(ctx, &t);
     if (st == PPD_OK && !in_capture) st = follow_stream(ctx, hs);
     if (st != PPD_OK) return st;
-    const bool reuse = t->on_device && t->weighted == weighted && t->fp8_pages == ctx->fp8_pages && (int32_t)t->L.size() == B &&
-                       std::memcmp(t->L.data(), L, sizeof(int32_t) * B) == 0 && std::memcmp(t->n.data(), n, sizeof(int32_t) * B) == 0;
+    TreeSlot& slot = t->slots[weighted][ctx->fp8_pages];
+    const bool reuse = slot.on_device && (int32_t)slot.L.size() == B && std::memcmp(slot.L.data(), L, sizeof(int32_t) * B) == 0 &&
+                       std::memcmp(slot.n.data(), n, sizeof(int32_t) * B) == 0;
     if (!reuse) {
         if (in_capture) return refuse_in_capture();
-        st = upload_tree_plan(ctx, t, L, n, B, weighted, hs);
+        st = upload_tree_plan(ctx, t, &slot, L, n, B, weighted, hs);
         if (st != PPD_OK) return st;
     }
-    const ppd::TreePlan& plan = t->plan;
-    const char* d_plan = static_cast<const char*>(t->d_plan);
+    const ppd::TreePlan& plan = slot.plan;
+    const char* d_plan = static_cast<const char*>(slot.d_plan);
     ppd::TreeParams p;
     std::memset(&p, 0, sizeof p);
     p.q = static_cast<const uint16_t*>(q);

@@ -4,12 +4,14 @@
 #include <hip/hip_runtime.h>
 
 static int g_captured_allocations = 0;
+static size_t g_largest = SIZE_MAX;  // of an allocation; larger ones fail
 template <class T>
 static hipError_t allocate_unless_captured(T** p, size_t n) {
     if (sim.capturing) {
         ++g_captured_allocations;
         return sim.pending = hipErrorInvalidValue;
     }
+    if (n > g_largest) return sim.pending = hipErrorInvalidValue;
     *p = static_cast<T*>(std::malloc(n));
     return hipSuccess;
 }
@@ -53,9 +55,68 @@ static void first_call_under_capture() {
     ppd_destroy(ctx);
 }
 
+// Tree and weighted attention, on pages of either format, keep a plan each: calls of one leave the others' plans as they are, also with
+// the same lengths, so that a graph of one can be replayed after calls of the other and one graph can hold both.
+static void kinds() {
+    ppd_ctx* ctx = make(32, 8, 128);
+    const int32_t L[3] = {3000, 40, 9000}, n[3] = {5, 9, 1}, other[3] = {3000, 41, 9000};
+    hipStream_t s;
+    hipStreamCreateWithFlags(&s, 0);
+    auto tree = [&](const int32_t* l) { return ppd_tree_attention(ctx, device, device, tables, 600, masks, 1, l, n, 3, 1.f, device, s); };
+    auto weighted = [&](const int32_t* l) { return ppd_weighted_attention(ctx, device, device, tables, 600, l, n, 3, 1.f, device, floats, 9001, s); };
+    struct Plan {  // what a graph reads, and what was there when it was captured
+        ppd::TreeParams p;
+        std::vector<ppd::TreeItem> items;
+        std::vector<ppd::TreeGroup> groups;
+        std::vector<ppd::WeighItem> weighs;
+        bool intact() const {
+            return std::memcmp(items.data(), p.items, items.size() * sizeof items[0]) == 0 && std::memcmp(groups.data(), p.groups, groups.size() * sizeof groups[0]) == 0 &&
+                   std::memcmp(weighs.data(), p.score_weighs, weighs.size() * sizeof weighs[0]) == 0;
+        }
+    };
+    auto last = [&] {
+        const ppd::TreeParams p = g_tree.back();
+        return Plan{p, {p.items, p.items + p.n_items}, {p.groups, p.groups + p.n_groups}, {p.score_weighs, p.score_weighs + p.n_score_weighs}};
+    };
+    auto captured = [&](auto call) {
+        sim.capturing = true;
+        const ppd_status st = call(L);
+        sim.capturing = false;
+        return st == PPD_OK && s->waiting() == 0;
+    };
+    CHECK(weighted(L) == PPD_OK && s->waiting() == 1);
+    s->run();
+    const Plan w = last();
+    CHECK(w.items.size() > 0 && w.groups.size() > 0 && w.weighs.size() > 0);
+    CHECK(tree(L) == PPD_OK && s->waiting() == 1);
+    s->run();
+    const Plan t = last();
+    CHECK(t.p.items != w.p.items && w.intact());
+    CHECK(captured(weighted) && captured(tree) && captured(weighted));
+    CHECK(tree(other) == PPD_OK && s->waiting() == 1);
+    s->run();
+    CHECK(w.intact() && captured(weighted));
+    CHECK(ppd_set_kv_format(ctx, PPD_KV_FP8_E4M3, 1.f, 1.f) == PPD_OK);
+    CHECK(weighted(L) == PPD_OK && s->waiting() == 1);
+    s->run();
+    CHECK(w.intact() && captured(weighted));
+    CHECK(ppd_set_kv_format(ctx, PPD_KV_BF16, 1.f, 1.f) == PPD_OK);
+    CHECK(captured(weighted) && g_tree.back().items == w.p.items);
+    // a workspace that could not grow is gone for all of them
+    const int32_t far[3] = {300000, 40, 300000};
+    g_largest = 1 << 20;
+    CHECK(ppd_tree_attention(ctx, device, device, tables, 20000, masks, 1, far, n, 3, 1.f, device, s) == PPD_ERR_WORKSPACE);
+    g_largest = SIZE_MAX;
+    CHECK(weighted(L) == PPD_OK && s->waiting() == 1 && g_tree.back().partials != nullptr);
+    s->run();
+    ppd_destroy(ctx);
+    delete s;
+}
+
 int main(int, char** argv) {
     const std::string what = argv[1];
     if (what == "first_call_under_capture") first_call_under_capture();
+    else if (what == "kinds") kinds();
     else return 2;
     std::printf("ok\n");
     return 0;

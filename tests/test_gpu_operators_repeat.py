@@ -48,3 +48,42 @@ def test_first_call_under_capture_is_refused_and_the_capture_stays_valid(kind):
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip((out, w, keep), ref))
     assert b.flags() == 0
+
+
+def test_graphs_of_one_kind_outlive_calls_of_the_other():
+    """Tree and weighted attention of the same lengths, together in one graph and eagerly between its replays."""
+    b = Batch([900, 30, 4000], [12, 5, 2], 32, 8, 128, seed=52)
+    mask = dev(random_mask(b, 1, seed=53).view(np.int64))
+    w0 = torch.rand((3, 8, 4100), device="cuda")
+
+    def tree(out, stream=None):
+        b.ctx.tree_attention(b.q_dev, b.pool, b.table_dev, b.L, b.n, mask, b.scale, out, stream=stream)
+
+    t_ref, w_ref = torch.empty((19, 32, 128), dtype=torch.bfloat16, device="cuda"), w0.clone()
+    o_ref = b.weighted(w_ref)
+    tree(t_ref)
+    t_out, o_out, w = torch.zeros_like(t_ref), torch.zeros_like(o_ref), w0.clone()
+    graph, alone = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s = torch.cuda.current_stream().cuda_stream
+        tree(t_out, s)
+        b.weighted(w, out=o_out, stream=s)
+    with torch.cuda.graph(alone):
+        b.weighted(w, out=o_out, stream=torch.cuda.current_stream().cuda_stream)
+    for replayed, between in [(graph, None), (graph, "tree"), (alone, "tree"), (alone, "weighted"), (graph, "weighted"), (alone, None)]:
+        if between == "tree":
+            tree(t_out)
+            assert torch.equal(t_out, t_ref)
+        elif between == "weighted":
+            w.copy_(w0)
+            b.weighted(w, out=o_out)
+            assert torch.equal(w, w_ref) and torch.equal(o_out, o_ref)
+        w.copy_(w0)
+        for x in (o_out, t_out):
+            x.zero_()
+        torch.cuda.synchronize()
+        replayed.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o_out, o_ref) and torch.equal(w, w_ref)
+        assert replayed is alone or torch.equal(t_out, t_ref)
+    assert b.flags() == 0
