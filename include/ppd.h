@@ -282,7 +282,7 @@ ppd_status ppd_kv_select(ppd_ctx *ctx, const float *weights, int64_t weight_stri
  *   keep          device int32; the list of (layer l, sequence b, head h) starts at keep + l * keep_layer_stride + b * keep_seq_stride
  *                 + h * keep_head_stride (a stride of 0: shared).  A list ascends strictly and has keep[i] >= first_b + i; an
  *                 entry that does not, or lies outside the page table (or the weights), is left where it is and raises device error
- *                 flag bit 3
+ *                 flag bit 3; one whose page, or whose new place's, is outside the pool raises bit 1.  Its weights stay where they are too
  *   first, count  HOST int32 [B]
  *   weights       device float [num_layers][B][Hkv][weight_stride] moved along with the tokens, or NULL */
 ppd_status ppd_kv_compact(ppd_ctx *ctx, void *kv_pages, int64_t layer_stride_elems, int32_t num_layers,

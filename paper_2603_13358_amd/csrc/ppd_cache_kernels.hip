@@ -516,7 +516,7 @@ __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const Comp
             m.src = -1;
         }
         m.from_id = m.to_id = 0;
-        if (m.src >= 0 && !is_weights) {
+        if (m.src >= 0) {
             m.from_id = pages[m.src >> 4];
             m.to_id = pages[m.pos >> 4];
         }
@@ -527,19 +527,20 @@ __global__ __launch_bounds__(kCompactThreads) void ppd_compact_kernel(const Comp
     ask_list(start, m);
     ask_pages(m);
     for (int p0 = start; p0 < end; p0 += P.step) {
-        if (is_weights) {
-            float v = 0.f;
-            if (m.src >= 0) v = weights[m.src];
-            asm volatile("s_waitcnt vmcnt(0)" : "+v"(v) : : "memory");
-            __syncthreads();
-            if (m.src >= 0) weights[m.pos] = v;
-            ask_list(p0 + P.step, m);
-            ask_pages(m);
-            continue;
-        }
         if (m.src >= 0 && ((uint32_t)m.from_id >= (uint64_t)P.num_pages || (uint32_t)m.to_id >= (uint64_t)P.num_pages)) {
             atomicOr(P.err_flags, 2u);
             m.src = -1;
+        }
+        if (is_weights) {  // a weight stays where its token stays
+            const int src = m.src, pos = m.pos;
+            float v = 0.f;
+            if (src >= 0) v = weights[src];
+            ask_list(p0 + P.step, m);
+            asm volatile("s_waitcnt vmcnt(0)" : "+v"(v) : : "memory");
+            ask_pages(m);
+            lds_barrier();
+            if (src >= 0) weights[pos] = v;
+            continue;
         }
         __syncthreads();  // the lists of the step before are read
         if (tid < kMoves) {
