@@ -253,7 +253,8 @@ ppd_status ppd_tree_attention(ppd_ctx *ctx, const void *q, const void *kv_pages,
 /* Causal attention (row j of a sequence sees keys 0 .. L_i + j: decode rows, or the last rows of a prompt) that also adds up how much
  * every key of the sequence was looked at, for each KV head over the rows and the G query heads of its group:
  *   weights[i][h][t] = (t < L_i ? weights[i][h][t] : 0) + sum over rows j and heads of the group of the probability of key t
- * for t < L_i + n_i; entries behind are not touched, so appended tokens need no clearing.
+ * for t < L_i + n_i; entries behind are not touched, so appended tokens need no clearing.  A row whose scores are all minus infinity
+ * gives zeros and adds nothing.
  *   weights       device float [B][Hkv][weight_stride], 4-byte aligned, weight_stride >= L_i + n_i
  *   the rest      as for ppd_mixed_attention
  * Sums are binary32 in a fixed order: bitwise the same from run to run.  Sequences of few query columns (n_i * G * 8 bytes at most one

@@ -705,7 +705,7 @@ __device__ __forceinline__ void mfma_item(const KP& P, const ppd_work_item& it, 
         const float inv = TREE && l_tot == 0.f ? 0.f : P.v_scale / l_tot;
         if constexpr (TREE)
             if (P.stats && h == 0 && col < ncols)
-                *reinterpret_cast<f32x2*>(P.stats + ((int64_t)(it.grow0 + jrow) * P.Hq + head) * 2) = f32x2{m_run, 1.0f / l_tot};
+                *reinterpret_cast<f32x2*>(P.stats + ((int64_t)(it.grow0 + jrow) * P.Hq + head) * 2) = l_tot == 0.f ? f32x2{0.f, 0.f} : f32x2{m_run, 1.0f / l_tot};
         if (wave_active) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {

@@ -6,7 +6,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 import paper_2603_13358_amd as ppd  # noqa: E402
-from test_gpu_operators import dev, moved  # noqa: E402
+from test_gpu_operators import Batch, dev, moved, within  # noqa: E402
 
 
 @pytest.mark.parametrize("layers", [1, 2])
@@ -42,3 +42,24 @@ def test_weights_of_tokens_that_stay_stay_as_well(layers):
     table[0, 1::2] = 1 << 30
     keep = list(range(30, 110))
     compact(table, keep, 3, [i for i, t in enumerate(keep) if t // 16 % 2 == 0 and (3 + i) // 16 % 2 == 0], 2)
+
+
+@pytest.mark.parametrize("n,hq,dim", [(1, 8, 64), (8, 8, 128), (40, 8, 128), (70, 2, 64), (300, 2, 128)])
+def test_a_row_whose_every_score_is_minus_infinity_gives_zeros_and_no_weight(n, hq, dim):
+    def fill(b):
+        b.q[..., 5] = 1.0
+        b.k[0][0, :, 5] = -np.inf
+    b = Batch([0], [n], hq, 2, dim, seed=61, kv=fill)  # row 0 sees token 0 alone
+    w = torch.full((1, 2, n), float("nan"), device="cuda")
+    out = b.weighted(w)
+    b.k[0][0] = 0.0
+
+    def sees(i):
+        seen = np.tril(np.ones((n, n), bool))
+        seen[:, 0] = False
+        return seen
+    b.sees = lambda i, mask=None: sees(i)
+    ref, bound, weights = b.reference()
+    assert not ref[0].any() and not out[0].any()
+    within(out, ref, bound)
+    within(w[0], *weights[0])
