@@ -16,6 +16,7 @@ constexpr int kSlab = 32;            // keys a wave works at a time: two pages
 constexpr int kTreeStep = kSlab * kTreeWaves;  // split boundaries are multiples of it
 constexpr int kMaxTreeChunk = 8192;  // keys per tree tile at most (its page ids are staged in LDS)
 constexpr int kMaxTreeBlockChunk = 16384;  // the same of a row block
+constexpr int32_t kMaxTreeTokens = INT32_MAX - kMaxTreeBlockChunk;  // of a sequence: rounded up to whole tiles its keys are numbered in 32 bits
 constexpr int kMaxMaskWords = 16;    // 64-bit words of a row's tree mask at most
 constexpr int kKeptScores = 19200;  // scores that a tree tile holds in LDS: two workgroups' fill a unit
 constexpr int kWeighKeys = 256;      // keys of a workgroup that adds up attention weights

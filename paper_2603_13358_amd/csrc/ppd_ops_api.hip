@@ -160,7 +160,7 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
     for (int i = 0; i < B; ++i) {
         if (n[i] < 1 || L[i] < 0) return fail(ctx, PPD_ERR_RANGE, "n_i must be >= 1 and L_i >= 0");
         const int64_t total = (int64_t)L[i] + n[i];
-        if (total > INT32_MAX - ppd::kMaxTreeChunk) return fail(ctx, PPD_ERR_RANGE, "L_i + n_i is too large");
+        if (total > ppd::kMaxTreeTokens) return fail(ctx, PPD_ERR_RANGE, "L_i + n_i is too large");
         if (!weighted && n[i] > 64 * mask_words)
             return fail(ctx, PPD_ERR_RANGE, "sequence " + std::to_string(i) + " has " + std::to_string(n[i]) + " nodes, a mask of " + std::to_string(mask_words) + " words has fewer bits");
         if (weighted && total > weight_stride)

@@ -21,6 +21,9 @@ struct KeyRange {
     int32_t keys, tiles, cols;
 };
 
+// Rounded up; the sum may pass 32 bits.
+int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
+
 // How long the tiles take, the longest first and each where there is room next.  One KV head's tiles on its share of the slots: the
 // heads are alike.
 double last_tile_end(std::vector<double>& tiles, int32_t slots) {
@@ -52,7 +55,7 @@ int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, 
     for (double c = std::min<double>(kind.max_chunk, longest); c >= kind.step; c *= 0.84) {
         double count = 0, sum = 0, most = 0, joined = 0;
         for (const auto& r : ranges) {
-            const double pieces = (double)((r.keys + (int64_t)c - 1) / (int64_t)c);
+            const double pieces = (double)ceil_div(r.keys, (int64_t)c);
             const double cost = r.keys / pieces + kind.start_keys;
             count += pieces * r.tiles;
             sum += pieces * r.tiles * cost;
@@ -64,7 +67,7 @@ int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, 
         if (count > slots && count <= 4.0 * slots) {
             tiles.clear();
             for (const auto& r : ranges) {
-                const int64_t pieces = (r.keys + (int64_t)c - 1) / (int64_t)c;
+                const int64_t pieces = ceil_div(r.keys, (int64_t)c);
                 tiles.insert(tiles.end(), (size_t)(pieces * r.tiles), (double)r.keys / pieces + kind.start_keys);
             }
             est = last_tile_end(tiles, slots);
@@ -106,8 +109,8 @@ bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int
     std::vector<KeyRange> narrow_ranges, wide_ranges;
     for (int i = 0; i < B; ++i) {
         const bool is_wide = (int64_t)n[i] * G > kTreeCols;
-        const int32_t blocks = is_wide ? (n[i] - 1) / block_rows + 1 : 1;
-        (is_wide ? wide_ranges : narrow_ranges).push_back({L[i] + n[i], blocks, is_wide ? (n[i] + blocks - 1) / blocks * G : n[i] * G});
+        const int32_t blocks = is_wide ? ceil_div(n[i], block_rows) : 1;
+        (is_wide ? wide_ranges : narrow_ranges).push_back({L[i] + n[i], blocks, is_wide ? ceil_div(n[i], blocks) * G : n[i] * G});
         fewest += (double)blocks * Hkv * (((double)L[i] + n[i]) / std::min(kMaxTreeChunk, max_piece(n[i])) + 1);
     }
     if (fewest > kMaxTiles) return false;
@@ -121,10 +124,10 @@ bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int
         const bool keep_scores = keeps_scores(n[i]);
         const int32_t most = max_piece(n[i]);
         const int32_t chunk = std::min(most, is_wide ? wide_chunk : narrow_chunk);
-        const int32_t pieces = (total + chunk - 1) / chunk;
-        const int32_t piece = std::min(most, ((total + pieces - 1) / pieces + kind.step - 1) / kind.step * kind.step);
-        const int32_t nsplit = (total + piece - 1) / piece;
-        const int32_t blocks = is_wide ? (n[i] + block_rows - 1) / block_rows : 1, rows = (n[i] + blocks - 1) / blocks;
+        const int32_t pieces = ceil_div(total, chunk);
+        const int32_t piece = std::min(most, ceil_div(ceil_div(total, pieces), kind.step) * kind.step);
+        const int32_t nsplit = ceil_div(total, piece);
+        const int32_t blocks = is_wide ? ceil_div(n[i], block_rows) : 1, rows = ceil_div(n[i], blocks);
         for (int h = 0; h < Hkv; ++h) {
             for (int32_t row0 = 0; row0 < n[i]; row0 += rows) {
                 const int32_t nrows = std::min(rows, n[i] - row0), cols = nrows * G;

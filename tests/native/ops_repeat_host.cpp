@@ -113,10 +113,43 @@ static void kinds() {
     delete s;
 }
 
+// The longest sequences whose key numbers, rounded up to whole tiles, still fit 32 bits are planned whole; longer ones are refused.
+static void longest() {
+    const ppd_shape s = {8, 1, 64, 16, 1 << 20};
+    for (const int32_t rows : {1, 4, 5, 32}) {
+        const int32_t total = ppd::kMaxTreeTokens, L = total - rows;
+        ppd::TreePlan p;
+        CHECK(ppd::build_tree_plan(s, &L, &rows, 1, false, 1, 256, &p));
+        CHECK(p.items.empty() == (rows > 4) && p.blocks.empty() == (rows <= 4));
+        std::map<int32_t, int32_t> range;  // begin -> end
+        for (const auto& it : p.items) CHECK(range.emplace(it.kv_begin, it.kv_end).second);
+        for (const auto& it : p.blocks) CHECK(range.emplace(it.kv_begin, it.kv_end).second);
+        int32_t at = 0;
+        for (const auto& [b, e] : range) {
+            CHECK(b == at && e > b);
+            at = e;
+        }
+        CHECK(at == total && p.groups.size() == 1 && p.groups[0].nsplit == (int)range.size());
+    }
+    ppd_ctx* ctx = nullptr;
+    CHECK(ppd_create(&s, 0, &ctx) == PPD_OK);
+    for (const int32_t rows : {1, 4, 5, 32}) {
+        for (const int32_t more : {1, 4096, 8192, 12000, 16384 - 8}) {
+            if (more > INT32_MAX - ppd::kMaxTreeTokens) continue;
+            const int32_t L = ppd::kMaxTreeTokens - rows + more;
+            CHECK(ppd_tree_attention(ctx, device, device, tables, INT32_MAX, masks, 1, &L, &rows, 1, 1.f, device, nullptr) == PPD_ERR_RANGE);
+            CHECK(ppd_weighted_attention(ctx, device, device, tables, INT32_MAX, &L, &rows, 1, 1.f, device, floats, INT32_MAX, nullptr) == PPD_ERR_RANGE);
+        }
+    }
+    CHECK(g_tree.empty() && g_blocks.empty());
+    ppd_destroy(ctx);
+}
+
 int main(int, char** argv) {
     const std::string what = argv[1];
     if (what == "first_call_under_capture") first_call_under_capture();
     else if (what == "kinds") kinds();
+    else if (what == "longest") longest();
     else return 2;
     std::printf("ok\n");
     return 0;
