@@ -188,6 +188,13 @@ def ppd_mixed_attention_static(ctx, q, kv_pages, page_tables, L, n, scale, out, 
                         static=True)
 
 
+def _check_call(status, ctx):
+    """Of a call whose arguments the call module looks at: a message where it could not pass them on."""
+    if isinstance(status, str):
+        raise PPDError(-3, status)
+    _check(status, ctx)
+
+
 def _lengths(*arrays):
     """Host int32 arrays of one length."""
     arrays = [_host_i32(a).reshape(-1) for a in arrays]
@@ -204,7 +211,7 @@ def ppd_tree_attention(ctx, q, kv_pages, page_tables, L, n, tree_mask, scale, ou
     if status is None:  # lengths in another type, layout or container
         status = _call.tree_attention(_fn_tree, ctx, q, kv_pages, page_tables, max_pages, tree_mask, mask_words, *_lengths(L, n), scale, out, stream)
     if status != 0:
-        _check(status, ctx)
+        _check_call(status, ctx)
 
 
 def ppd_weighted_attention(ctx, q, kv_pages, page_tables, L, n, scale, out, weights, max_pages=None, weight_stride=None, stream=None):
@@ -215,7 +222,7 @@ def ppd_weighted_attention(ctx, q, kv_pages, page_tables, L, n, scale, out, weig
     if status is None:
         status = _call.weighted_attention(_fn_weighted, ctx, q, kv_pages, page_tables, max_pages, *_lengths(L, n), scale, out, weights, weight_stride, stream)
     if status != 0:
-        _check(status, ctx)
+        _check_call(status, ctx)
 
 
 def ppd_kv_select(ctx, weights, length, budget, sinks, recent, keep, weight_stride=None, keep_stride=None, stream=None):
@@ -226,7 +233,7 @@ def ppd_kv_select(ctx, weights, length, budget, sinks, recent, keep, weight_stri
     if status is None:
         status = _call.kv_select(_fn_select, ctx, weights, weight_stride, *_lengths(length), budget, sinks, recent, keep, keep_stride, stream)
     if status != 0:
-        _check(status, ctx)
+        _check_call(status, ctx)
 
 
 def ppd_kv_compact(ctx, kv_pages, page_tables, keep, first, count, layer_stride_elems=0, num_layers=1, weights=None, keep_strides=None, max_pages=None,
@@ -249,7 +256,7 @@ def ppd_kv_compact(ctx, kv_pages, page_tables, keep, first, count, layer_stride_
     if status is None:
         status = _call.kv_compact(*args, *_lengths(first, count), weights, weight_stride, stream)
     if status != 0:
-        _check(status, ctx)
+        _check_call(status, ctx)
 
 
 def ppd_get_plan_stats(ctx):

@@ -56,6 +56,28 @@ static int to_int_or_shape(PyObject* o, PyObject* x, Py_ssize_t dim, int64_t* ou
     Py_DECREF(v);
     return ok;
 }
+// `o` as an int of 32 bits, or x.shape[dim] if it is None and x is given.  0 with *why set (and no error) if it does not fit: the call is refused
+// with that message.
+static int to_int32(PyObject* o, PyObject* x, Py_ssize_t dim, const char* name, int32_t* out, PyObject** why) {
+    if (o == Py_None && x) {
+        int64_t wide;
+        if (!to_int_or_shape(o, x, dim, &wide)) return 0;
+        *out = (int32_t)wide;
+        return 1;
+    }
+    PyObject* v = PyNumber_Long(o);
+    if (!v) return 0;
+    int over;
+    const long long wide = PyLong_AsLongLongAndOverflow(v, &over);
+    Py_DECREF(v);
+    if (wide == -1 && PyErr_Occurred()) return 0;
+    if (over || wide != (int32_t)wide) {
+        *why = PyUnicode_FromFormat("%s does not fit 32 bits", name);
+        return 0;
+    }
+    *out = (int32_t)wide;
+    return 1;
+}
 static int expect(Py_ssize_t have, Py_ssize_t want) {
     if (have == want) return 1;
     PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
@@ -162,23 +184,24 @@ typedef int32_t (*compact_fn)(void*, void*, int64_t, int32_t, const int32_t*, in
                               float*, int64_t, void*);
 
 // tree_attention(fn, ctx, q, kv_pages, page_tables, max_pages, tree_mask, mask_words, L, n, scale, out, stream) -> status, or None if L and n are
-// not plain int32 arrays of one length yet
+// not plain int32 arrays of one length yet, or, for arguments that cannot be passed on, a message
 static PyObject* call_tree(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     void *fn, *ctx, *q, *pages, *tables, *mask, *out, *stream;
-    int64_t max_pages, words;
+    int32_t max_pages, words;
+    PyObject* why = NULL;
     Py_buffer L, nn;
     (void)self;
     if (!expect(n, 13)) return NULL;
     if (!int32_arrays(a[8], a[9], &L, &nn)) Py_RETURN_NONE;
     PyObject* result = NULL;
     PyObject* scale = NULL;
-    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int_or_shape(a[5], a[4], 1, &max_pages) && to_int_or_shape(a[7], a[6], 1, &words) &&
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int32(a[5], a[4], 1, "max_pages", &max_pages, &why) && to_int32(a[7], a[6], 1, "mask_words", &words, &why) &&
         to_address(a[2], &q) && to_address(a[3], &pages) && to_address(a[4], &tables) && to_address(a[6], &mask) &&
         (scale = PyNumber_Float(a[10])) && to_address(a[11], &out) && to_handle(a[12], &stream)) {
         const float s = (float)PyFloat_AS_DOUBLE(scale);
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
-        status = ((tree_fn)fn)(ctx, q, pages, (const int32_t*)tables, (int32_t)max_pages, (const uint64_t*)mask, (int32_t)words, (const int32_t*)L.buf,
+        status = ((tree_fn)fn)(ctx, q, pages, (const int32_t*)tables, max_pages, (const uint64_t*)mask, words, (const int32_t*)L.buf,
                                (const int32_t*)nn.buf, (int32_t)L.shape[0], s, out, stream);
         Py_END_ALLOW_THREADS
         result = PyLong_FromLong(status);
@@ -186,26 +209,28 @@ static PyObject* call_tree(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     Py_XDECREF(scale);
     PyBuffer_Release(&nn);
     PyBuffer_Release(&L);
-    return result;
+    return why ? why : result;
 }
 
 // weighted_attention(fn, ctx, q, kv_pages, page_tables, max_pages, L, n, scale, out, weights, weight_stride, stream) -> the same
 static PyObject* call_weighted(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     void *fn, *ctx, *q, *pages, *tables, *out, *weights, *stream;
-    int64_t max_pages, stride;
+    int32_t max_pages;
+    int64_t stride;
+    PyObject* why = NULL;
     Py_buffer L, nn;
     (void)self;
     if (!expect(n, 13)) return NULL;
     if (!int32_arrays(a[6], a[7], &L, &nn)) Py_RETURN_NONE;
     PyObject* result = NULL;
     PyObject* scale = NULL;
-    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int_or_shape(a[5], a[4], 1, &max_pages) && to_int_or_shape(a[11], a[10], -1, &stride) &&
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int32(a[5], a[4], 1, "max_pages", &max_pages, &why) && to_int_or_shape(a[11], a[10], -1, &stride) &&
         to_address(a[2], &q) && to_address(a[3], &pages) && to_address(a[4], &tables) && (scale = PyNumber_Float(a[8])) &&
         to_address(a[9], &out) && to_address(a[10], &weights) && to_handle(a[12], &stream)) {
         const float s = (float)PyFloat_AS_DOUBLE(scale);
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
-        status = ((weighted_fn)fn)(ctx, q, pages, (const int32_t*)tables, (int32_t)max_pages, (const int32_t*)L.buf, (const int32_t*)nn.buf,
+        status = ((weighted_fn)fn)(ctx, q, pages, (const int32_t*)tables, max_pages, (const int32_t*)L.buf, (const int32_t*)nn.buf,
                                    (int32_t)L.shape[0], s, out, (float*)weights, stride, stream);
         Py_END_ALLOW_THREADS
         result = PyLong_FromLong(status);
@@ -213,55 +238,60 @@ static PyObject* call_weighted(PyObject* self, PyObject* const* a, Py_ssize_t n)
     Py_XDECREF(scale);
     PyBuffer_Release(&nn);
     PyBuffer_Release(&L);
-    return result;
+    return why ? why : result;
 }
 
 // kv_select(fn, ctx, weights, weight_stride, length, budget, sinks, recent, keep, keep_stride, stream) -> status, or None if length is not a plain
 // int32 array yet
 static PyObject* call_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     void *fn, *ctx, *weights, *keep, *stream;
-    int64_t stride, keep_stride, budget, sinks, recent;
+    int64_t stride, keep_stride;
+    int32_t budget, sinks, recent;
+    PyObject* why = NULL;
     Py_buffer len;
     (void)self;
     if (!expect(n, 11)) return NULL;
     if (!int32_array(a[4], &len)) Py_RETURN_NONE;
     PyObject* result = NULL;
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int_or_shape(a[3], a[2], -1, &stride) && to_int_or_shape(a[9], a[8], -1, &keep_stride) &&
-        to_address(a[2], &weights) && to_int(a[5], &budget) && to_int(a[6], &sinks) && to_int(a[7], &recent) && to_address(a[8], &keep) && to_handle(a[10], &stream)) {
+        to_address(a[2], &weights) && to_int32(a[5], NULL, 0, "budget", &budget, &why) && to_int32(a[6], NULL, 0, "sinks", &sinks, &why) &&
+        to_int32(a[7], NULL, 0, "recent", &recent, &why) && to_address(a[8], &keep) && to_handle(a[10], &stream)) {
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
-        status = ((select_fn)fn)(ctx, (const float*)weights, stride, (const int32_t*)len.buf, (int32_t)len.shape[0], (int32_t)budget, (int32_t)sinks, (int32_t)recent,
+        status = ((select_fn)fn)(ctx, (const float*)weights, stride, (const int32_t*)len.buf, (int32_t)len.shape[0], budget, sinks, recent,
                                  (int32_t*)keep, keep_stride, stream);
         Py_END_ALLOW_THREADS
         result = PyLong_FromLong(status);
     }
     PyBuffer_Release(&len);
-    return result;
+    return why ? why : result;
 }
 
 // kv_compact(fn, ctx, kv_pages, layer_stride_elems, num_layers, page_tables, max_pages, keep, keep_layer, keep_seq, keep_head, first, count, weights,
 // weight_stride, stream) -> status, or None if first and count are not plain int32 arrays of one length yet
 static PyObject* call_compact(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     void *fn, *ctx, *pages, *tables, *keep, *weights, *stream;
-    int64_t layer_stride, layers, max_pages, kl, ks, kh, stride = 0;
+    int64_t layer_stride, kl, ks, kh, stride = 0;
+    int32_t layers, max_pages;
+    PyObject* why = NULL;
     Py_buffer first, count;
     (void)self;
     if (!expect(n, 16)) return NULL;
     if (!int32_arrays(a[11], a[12], &first, &count)) Py_RETURN_NONE;
     PyObject* result = NULL;
-    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_address(a[2], &pages) && to_int(a[3], &layer_stride) && to_int(a[4], &layers) &&
-        to_int_or_shape(a[6], a[5], 1, &max_pages) && to_address(a[5], &tables) && to_address(a[7], &keep) && to_int(a[8], &kl) && to_int(a[9], &ks) &&
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_address(a[2], &pages) && to_int(a[3], &layer_stride) &&
+        to_int32(a[4], NULL, 0, "num_layers", &layers, &why) && to_int32(a[6], a[5], 1, "max_pages", &max_pages, &why) && to_address(a[5], &tables) && to_address(a[7], &keep) && to_int(a[8], &kl) && to_int(a[9], &ks) &&
         to_int(a[10], &kh) && (a[13] == Py_None || to_int_or_shape(a[14], a[13], -1, &stride)) && to_address(a[13], &weights) && to_handle(a[15], &stream)) {
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
-        status = ((compact_fn)fn)(ctx, pages, layer_stride, (int32_t)layers, (const int32_t*)tables, (int32_t)max_pages, (const int32_t*)keep, kl, ks, kh,
+        status = ((compact_fn)fn)(ctx, pages, layer_stride, layers, (const int32_t*)tables, max_pages, (const int32_t*)keep, kl, ks, kh,
                                   (const int32_t*)first.buf, (const int32_t*)count.buf, (int32_t)first.shape[0], (float*)weights, stride, stream);
         Py_END_ALLOW_THREADS
         result = PyLong_FromLong(status);
     }
     PyBuffer_Release(&count);
     PyBuffer_Release(&first);
-    return result;
+    return why ? why : result;
 }
 
 static PyMethodDef kMethods[] = {

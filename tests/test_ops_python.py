@@ -1,0 +1,66 @@
+"""Arguments that the drafting and eviction calls refuse in Python, before the library is called (no GPU: tensors are the CPU's and the
+context is NULL, which the library itself refuses with PPD_ERR_NULL once everything has been passed on)."""
+import ctypes
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2603_13358_amd as ppd  # noqa: E402
+
+L, n = np.array([30, 5], np.int32), np.array([2, 3], np.int32)
+
+
+def tree(ctx=None, **kw):
+    a = dict(q=torch.zeros(5, 8, 64), kv_pages=torch.zeros(64), page_tables=torch.zeros(2, 3, dtype=torch.int32), L=L, n=n,
+             tree_mask=torch.zeros(5, 1, dtype=torch.int64), scale=1.0, out=torch.zeros(5, 8, 64))
+    ppd.ppd_tree_attention(ctx, **dict(a, **kw))
+
+
+def weighted(ctx=None, **kw):
+    a = dict(q=torch.zeros(5, 8, 64), kv_pages=torch.zeros(64), page_tables=torch.zeros(2, 3, dtype=torch.int32), L=L, n=n, scale=1.0,
+             out=torch.zeros(5, 8, 64), weights=torch.zeros(2, 4, 40))
+    ppd.ppd_weighted_attention(ctx, **dict(a, **kw))
+
+
+def select(ctx=None, **kw):
+    a = dict(weights=torch.zeros(2, 4, 40), length=L, budget=20, sinks=1, recent=2, keep=torch.zeros(2, 4, 20, dtype=torch.int32))
+    ppd.ppd_kv_select(ctx, **dict(a, **kw))
+
+
+def compact(ctx=None, **kw):
+    a = dict(kv_pages=torch.zeros(64), page_tables=torch.zeros(2, 3, dtype=torch.int32), keep=torch.zeros(2, 4, 20, dtype=torch.int32),
+             first=np.zeros(2, np.int32), count=np.array([20, 5], np.int32))
+    ppd.ppd_kv_compact(ctx, **dict(a, **kw))
+
+
+def status(call, *args, **kw):
+    with pytest.raises(ppd.PPDError) as e:
+        call(*args, **kw)
+    return e.value.status
+
+
+def refused(call, what, *args, **kw):
+    """Refused in Python, with a message that names the argument."""
+    with pytest.raises(ppd.PPDError) as e:
+        call(*args, **kw)
+    return e.value.status == -3 and what in str(e.value)
+
+
+def test_good_arguments_are_passed_on():
+    for call in (tree, weighted, select, compact):
+        assert status(call) == -1
+    assert status(compact, weights=torch.zeros(2, 4, 40)) == -1
+
+
+@pytest.mark.parametrize("far", [1 << 31, (1 << 32) + 5, -(1 << 31) - 1, 1 << 64, (1 << 64) + 5])
+def test_integers_are_not_cut_to_32_bits(far):
+    assert refused(select, "budget", budget=far)
+    assert refused(select, "sinks", sinks=far)
+    assert refused(select, "recent", recent=far)
+    assert refused(compact, "num_layers", num_layers=far)
+    for call in (tree, weighted, compact):
+        assert refused(call, "max_pages", max_pages=far)
+    assert refused(tree, "mask_words", mask_words=far)
+    assert status(select, budget=(1 << 31) - 1) == -1
