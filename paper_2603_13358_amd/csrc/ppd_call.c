@@ -7,7 +7,7 @@
 #include <Python.h>
 #include <stdint.h>
 
-static PyObject *s_data_ptr, *s_value, *s_shape;
+static PyObject *s_data_ptr, *s_value, *s_shape, *s_element_size, *s_is_floating_point;
 static PyObject *t_void_p, *f_cast;  // ctypes.c_void_p and ctypes.cast
 
 // What a ctypes parameter of type c_void_p takes: None, an int and a c_void_p (a context's handle) here, anything else --
@@ -77,6 +77,22 @@ static int to_int32(PyObject* o, PyObject* x, Py_ssize_t dim, const char* name, 
     }
     *out = (int32_t)wide;
     return 1;
+}
+// Whether a tensor's elements are what the call takes (an address or None is taken on trust): 0 with *why set if not.
+static int call_int(PyObject* o, PyObject* method, int64_t* out) {
+    PyObject* v = PyObject_CallMethodNoArgs(o, method);
+    if (!v) return 0;
+    const int ok = to_int(v, out);
+    Py_DECREF(v);
+    return ok;
+}
+static int has_elements(PyObject* o, const char* name, int64_t bytes, int floating, const char* type, PyObject** why) {
+    int64_t size, is_floating;
+    if (o == Py_None || PyLong_Check(o)) return 1;
+    if (!call_int(o, s_element_size, &size) || !call_int(o, s_is_floating_point, &is_floating)) return 0;
+    if (size == bytes && (is_floating != 0) == floating) return 1;
+    *why = PyUnicode_FromFormat("%s has to be of %s", name, type);
+    return 0;
 }
 static int expect(Py_ssize_t have, Py_ssize_t want) {
     if (have == want) return 1;
@@ -196,7 +212,8 @@ static PyObject* call_tree(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     PyObject* result = NULL;
     PyObject* scale = NULL;
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int32(a[5], a[4], 1, "max_pages", &max_pages, &why) && to_int32(a[7], a[6], 1, "mask_words", &words, &why) &&
-        to_address(a[2], &q) && to_address(a[3], &pages) && to_address(a[4], &tables) && to_address(a[6], &mask) &&
+        to_address(a[2], &q) && to_address(a[3], &pages) && has_elements(a[4], "page_tables", 4, 0, "int32", &why) && to_address(a[4], &tables) &&
+        has_elements(a[6], "tree_mask", 8, 0, "int64 or uint64", &why) && to_address(a[6], &mask) &&
         (scale = PyNumber_Float(a[10])) && to_address(a[11], &out) && to_handle(a[12], &stream)) {
         const float s = (float)PyFloat_AS_DOUBLE(scale);
         int32_t status;
@@ -225,8 +242,9 @@ static PyObject* call_weighted(PyObject* self, PyObject* const* a, Py_ssize_t n)
     PyObject* result = NULL;
     PyObject* scale = NULL;
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int32(a[5], a[4], 1, "max_pages", &max_pages, &why) && to_int_or_shape(a[11], a[10], -1, &stride) &&
-        to_address(a[2], &q) && to_address(a[3], &pages) && to_address(a[4], &tables) && (scale = PyNumber_Float(a[8])) &&
-        to_address(a[9], &out) && to_address(a[10], &weights) && to_handle(a[12], &stream)) {
+        to_address(a[2], &q) && to_address(a[3], &pages) && has_elements(a[4], "page_tables", 4, 0, "int32", &why) && to_address(a[4], &tables) &&
+        (scale = PyNumber_Float(a[8])) &&
+        to_address(a[9], &out) && has_elements(a[10], "weights", 4, 1, "float32", &why) && to_address(a[10], &weights) && to_handle(a[12], &stream)) {
         const float s = (float)PyFloat_AS_DOUBLE(scale);
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
@@ -254,6 +272,7 @@ static PyObject* call_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     if (!int32_array(a[4], &len)) Py_RETURN_NONE;
     PyObject* result = NULL;
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int_or_shape(a[3], a[2], -1, &stride) && to_int_or_shape(a[9], a[8], -1, &keep_stride) &&
+        has_elements(a[2], "weights", 4, 1, "float32", &why) && has_elements(a[8], "keep", 4, 0, "int32", &why) &&
         to_address(a[2], &weights) && to_int32(a[5], NULL, 0, "budget", &budget, &why) && to_int32(a[6], NULL, 0, "sinks", &sinks, &why) &&
         to_int32(a[7], NULL, 0, "recent", &recent, &why) && to_address(a[8], &keep) && to_handle(a[10], &stream)) {
         int32_t status;
@@ -280,7 +299,9 @@ static PyObject* call_compact(PyObject* self, PyObject* const* a, Py_ssize_t n) 
     if (!int32_arrays(a[11], a[12], &first, &count)) Py_RETURN_NONE;
     PyObject* result = NULL;
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_address(a[2], &pages) && to_int(a[3], &layer_stride) &&
-        to_int32(a[4], NULL, 0, "num_layers", &layers, &why) && to_int32(a[6], a[5], 1, "max_pages", &max_pages, &why) && to_address(a[5], &tables) && to_address(a[7], &keep) && to_int(a[8], &kl) && to_int(a[9], &ks) &&
+        to_int32(a[4], NULL, 0, "num_layers", &layers, &why) && to_int32(a[6], a[5], 1, "max_pages", &max_pages, &why) && has_elements(a[5], "page_tables", 4, 0, "int32", &why) &&
+        to_address(a[5], &tables) && has_elements(a[7], "keep", 4, 0, "int32", &why) &&
+        has_elements(a[13], "weights", 4, 1, "float32", &why) && to_address(a[7], &keep) && to_int(a[8], &kl) && to_int(a[9], &ks) &&
         to_int(a[10], &kh) && (a[13] == Py_None || to_int_or_shape(a[14], a[13], -1, &stride)) && to_address(a[13], &weights) && to_handle(a[15], &stream)) {
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
@@ -310,11 +331,13 @@ PyMODINIT_FUNC PyInit_ppd_call(void) {
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_value = PyUnicode_InternFromString("value");
     s_shape = PyUnicode_InternFromString("shape");
+    s_element_size = PyUnicode_InternFromString("element_size");
+    s_is_floating_point = PyUnicode_InternFromString("is_floating_point");
     PyObject* ctypes = PyImport_ImportModule("ctypes");
     if (!ctypes) return NULL;
     t_void_p = PyObject_GetAttrString(ctypes, "c_void_p");
     f_cast = PyObject_GetAttrString(ctypes, "cast");
     Py_DECREF(ctypes);
-    if (!s_data_ptr || !s_value || !s_shape || !t_void_p || !f_cast) return NULL;
+    if (!s_data_ptr || !s_value || !s_shape || !s_element_size || !s_is_floating_point || !t_void_p || !f_cast) return NULL;
     return PyModule_Create(&kModule);
 }

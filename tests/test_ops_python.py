@@ -64,3 +64,25 @@ def test_integers_are_not_cut_to_32_bits(far):
         assert refused(call, "max_pages", max_pages=far)
     assert refused(tree, "mask_words", mask_words=far)
     assert status(select, budget=(1 << 31) - 1) == -1
+
+
+def test_tensors_of_other_types_are_refused():
+    """torch's own defaults among them: indexes (topk, sort, nonzero) are int64."""
+    for call in (tree, weighted, compact):
+        assert refused(call, "page_tables", page_tables=torch.zeros(2, 3, dtype=torch.int64))
+    for dtype in (torch.int32, torch.float64, torch.float32):
+        assert refused(tree, "tree_mask", tree_mask=torch.zeros(5, 1, dtype=dtype))
+    assert status(tree, tree_mask=torch.zeros(5, 1, dtype=torch.uint64)) == -1
+    for dtype in (torch.float64, torch.bfloat16, torch.int32):
+        for call in (weighted, select, compact):
+            assert refused(call, "weights", weights=torch.zeros(2, 4, 40, dtype=dtype))
+    for dtype in (torch.int64, torch.int16, torch.float32):
+        for call in (select, compact):
+            assert refused(call, "keep", keep=torch.zeros(2, 4, 20, dtype=dtype))
+
+
+def test_addresses_are_taken_as_they_are():
+    assert status(select, weights=1 << 20, weight_stride=40, keep=1 << 21, keep_stride=20) == -1
+    assert status(weighted, weights=1 << 20, weight_stride=40) == -1
+    assert status(tree, tree_mask=1 << 20, mask_words=1) == -1
+    assert status(compact, keep=1 << 20, keep_strides=(0, 20, 0), weights=1 << 21, weight_stride=40, page_tables=1 << 22, max_pages=3) == -1
