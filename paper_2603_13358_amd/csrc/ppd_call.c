@@ -7,7 +7,7 @@
 #include <Python.h>
 #include <stdint.h>
 
-static PyObject *s_data_ptr, *s_value, *s_shape, *s_element_size, *s_is_floating_point;
+static PyObject *s_data_ptr, *s_value, *s_shape, *s_element_size, *s_is_floating_point, *s_is_contiguous;
 static PyObject *t_void_p, *f_cast;  // ctypes.c_void_p and ctypes.cast
 
 // What a ctypes parameter of type c_void_p takes: None, an int and a c_void_p (a context's handle) here, anything else --
@@ -92,6 +92,15 @@ static int has_elements(PyObject* o, const char* name, int64_t bytes, int floati
     if (!call_int(o, s_element_size, &size) || !call_int(o, s_is_floating_point, &is_floating)) return 0;
     if (size == bytes && (is_floating != 0) == floating) return 1;
     *why = PyUnicode_FromFormat("%s has to be of %s", name, type);
+    return 0;
+}
+// Whether a tensor whose strides are taken from its shape (`stride` is None) has these strides.
+static int is_dense(PyObject* o, PyObject* stride, const char* name, PyObject** why) {
+    int64_t dense;
+    if (stride != Py_None || o == Py_None || PyLong_Check(o)) return 1;
+    if (!call_int(o, s_is_contiguous, &dense)) return 0;
+    if (dense) return 1;
+    *why = PyUnicode_FromFormat("%s has to be contiguous, or its stride given", name);
     return 0;
 }
 static int expect(Py_ssize_t have, Py_ssize_t want) {
@@ -212,8 +221,9 @@ static PyObject* call_tree(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     PyObject* result = NULL;
     PyObject* scale = NULL;
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int32(a[5], a[4], 1, "max_pages", &max_pages, &why) && to_int32(a[7], a[6], 1, "mask_words", &words, &why) &&
-        to_address(a[2], &q) && to_address(a[3], &pages) && has_elements(a[4], "page_tables", 4, 0, "int32", &why) && to_address(a[4], &tables) &&
-        has_elements(a[6], "tree_mask", 8, 0, "int64 or uint64", &why) && to_address(a[6], &mask) &&
+        to_address(a[2], &q) && to_address(a[3], &pages) && has_elements(a[4], "page_tables", 4, 0, "int32", &why) &&
+        is_dense(a[4], a[5], "page_tables", &why) && to_address(a[4], &tables) &&
+        has_elements(a[6], "tree_mask", 8, 0, "int64 or uint64", &why) && is_dense(a[6], a[7], "tree_mask", &why) && to_address(a[6], &mask) &&
         (scale = PyNumber_Float(a[10])) && to_address(a[11], &out) && to_handle(a[12], &stream)) {
         const float s = (float)PyFloat_AS_DOUBLE(scale);
         int32_t status;
@@ -242,9 +252,11 @@ static PyObject* call_weighted(PyObject* self, PyObject* const* a, Py_ssize_t n)
     PyObject* result = NULL;
     PyObject* scale = NULL;
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int32(a[5], a[4], 1, "max_pages", &max_pages, &why) && to_int_or_shape(a[11], a[10], -1, &stride) &&
-        to_address(a[2], &q) && to_address(a[3], &pages) && has_elements(a[4], "page_tables", 4, 0, "int32", &why) && to_address(a[4], &tables) &&
+        to_address(a[2], &q) && to_address(a[3], &pages) && has_elements(a[4], "page_tables", 4, 0, "int32", &why) &&
+        is_dense(a[4], a[5], "page_tables", &why) && to_address(a[4], &tables) &&
         (scale = PyNumber_Float(a[8])) &&
-        to_address(a[9], &out) && has_elements(a[10], "weights", 4, 1, "float32", &why) && to_address(a[10], &weights) && to_handle(a[12], &stream)) {
+        to_address(a[9], &out) && has_elements(a[10], "weights", 4, 1, "float32", &why) &&
+        is_dense(a[10], a[11], "weights", &why) && to_address(a[10], &weights) && to_handle(a[12], &stream)) {
         const float s = (float)PyFloat_AS_DOUBLE(scale);
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
@@ -272,7 +284,8 @@ static PyObject* call_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     if (!int32_array(a[4], &len)) Py_RETURN_NONE;
     PyObject* result = NULL;
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int_or_shape(a[3], a[2], -1, &stride) && to_int_or_shape(a[9], a[8], -1, &keep_stride) &&
-        has_elements(a[2], "weights", 4, 1, "float32", &why) && has_elements(a[8], "keep", 4, 0, "int32", &why) &&
+        has_elements(a[2], "weights", 4, 1, "float32", &why) && is_dense(a[2], a[3], "weights", &why) &&
+        has_elements(a[8], "keep", 4, 0, "int32", &why) && is_dense(a[8], a[9], "keep", &why) &&
         to_address(a[2], &weights) && to_int32(a[5], NULL, 0, "budget", &budget, &why) && to_int32(a[6], NULL, 0, "sinks", &sinks, &why) &&
         to_int32(a[7], NULL, 0, "recent", &recent, &why) && to_address(a[8], &keep) && to_handle(a[10], &stream)) {
         int32_t status;
@@ -300,8 +313,8 @@ static PyObject* call_compact(PyObject* self, PyObject* const* a, Py_ssize_t n) 
     PyObject* result = NULL;
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_address(a[2], &pages) && to_int(a[3], &layer_stride) &&
         to_int32(a[4], NULL, 0, "num_layers", &layers, &why) && to_int32(a[6], a[5], 1, "max_pages", &max_pages, &why) && has_elements(a[5], "page_tables", 4, 0, "int32", &why) &&
-        to_address(a[5], &tables) && has_elements(a[7], "keep", 4, 0, "int32", &why) &&
-        has_elements(a[13], "weights", 4, 1, "float32", &why) && to_address(a[7], &keep) && to_int(a[8], &kl) && to_int(a[9], &ks) &&
+        is_dense(a[5], a[6], "page_tables", &why) && to_address(a[5], &tables) && has_elements(a[7], "keep", 4, 0, "int32", &why) &&
+        has_elements(a[13], "weights", 4, 1, "float32", &why) && is_dense(a[13], a[14], "weights", &why) && to_address(a[7], &keep) && to_int(a[8], &kl) && to_int(a[9], &ks) &&
         to_int(a[10], &kh) && (a[13] == Py_None || to_int_or_shape(a[14], a[13], -1, &stride)) && to_address(a[13], &weights) && to_handle(a[15], &stream)) {
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
@@ -333,11 +346,12 @@ PyMODINIT_FUNC PyInit_ppd_call(void) {
     s_shape = PyUnicode_InternFromString("shape");
     s_element_size = PyUnicode_InternFromString("element_size");
     s_is_floating_point = PyUnicode_InternFromString("is_floating_point");
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     PyObject* ctypes = PyImport_ImportModule("ctypes");
     if (!ctypes) return NULL;
     t_void_p = PyObject_GetAttrString(ctypes, "c_void_p");
     f_cast = PyObject_GetAttrString(ctypes, "cast");
     Py_DECREF(ctypes);
-    if (!s_data_ptr || !s_value || !s_shape || !s_element_size || !s_is_floating_point || !t_void_p || !f_cast) return NULL;
+    if (!s_data_ptr || !s_value || !s_shape || !s_element_size || !s_is_floating_point || !s_is_contiguous || !t_void_p || !f_cast) return NULL;
     return PyModule_Create(&kModule);
 }

@@ -86,3 +86,21 @@ def test_addresses_are_taken_as_they_are():
     assert status(weighted, weights=1 << 20, weight_stride=40) == -1
     assert status(tree, tree_mask=1 << 20, mask_words=1) == -1
     assert status(compact, keep=1 << 20, keep_strides=(0, 20, 0), weights=1 << 21, weight_stride=40, page_tables=1 << 22, max_pages=3) == -1
+
+
+def test_views_whose_strides_are_not_their_shapes_are_refused():
+    wide, lists = torch.zeros(2, 4, 60), torch.zeros(2, 4, 30, dtype=torch.int32)
+    for call in (weighted, select, compact):
+        assert refused(call, "weights", weights=wide[..., :40])
+        assert status(call, weights=wide[..., :40], weight_stride=60) == -1
+    assert refused(weighted, "weights", weights=torch.zeros(4, 2, 40).transpose(0, 1))
+    assert refused(select, "keep", keep=lists[..., :20])
+    assert status(select, keep=lists[..., :20], keep_stride=30) == -1
+    assert status(compact, keep=lists[..., :20]) == -1  # its strides are passed on
+    assert refused(tree, "tree_mask", tree_mask=torch.zeros(5, 2, dtype=torch.int64)[:, :1])
+    tables = torch.zeros(2, 5, dtype=torch.int32)
+    for call in (tree, weighted, compact):
+        assert refused(call, "page_tables", page_tables=tables[:, :3])
+        assert status(call, page_tables=tables[:, :3], max_pages=5) == -1
+    layers = torch.zeros(3, 2, 4, 40)
+    assert status(weighted, weights=layers[1]) == -1  # a layer's part is whole
