@@ -132,6 +132,7 @@ def ppd_create(num_q_heads, num_kv_heads, head_dim, page_size, num_pages, device
     shape = Shape(num_q_heads, num_kv_heads, head_dim, page_size, num_pages)
     handle = ctypes.c_void_p()
     _check(load_library().ppd_create(ctypes.byref(shape), device, ctypes.byref(handle)))
+    handle.num_kv_heads = int(num_kv_heads)  # for the checks of tensors that have a row for every KV head
     return handle
 
 
@@ -240,7 +241,7 @@ def ppd_kv_compact(ctx, kv_pages, page_tables, keep, first, count, layer_stride_
                    weight_stride=None, stream=None):
     """keep: int32 [sequences][n] (shared by heads and layers), [sequences][KV heads][n] (shared by layers) or [layers][sequences][KV heads][n],
     or an address with keep_strides = (layer, sequence, head).  weights: float32 [sequences][KV heads][stride], with a layer axis in front
-    if there are several, or None."""
+    if there are several (of as many layers and sequences as the call has), or None."""
     if _lib is None:
         load_library()
     if keep_strides is None:
@@ -248,6 +249,9 @@ def ppd_kv_compact(ctx, kv_pages, page_tables, keep, first, count, layer_stride_
         if len(strides) not in (2, 3, 4) or strides[-1] != 1 and keep.shape[-1] > 1:
             raise PPDError(-3, "keep has two, three or four axes, the last contiguous")
         first, count = _lengths(first, count)
+        heads = getattr(ctx, "num_kv_heads", None)
+        if keep.shape[-2 if len(strides) == 2 else -3] < len(first) or len(strides) > 2 and heads not in (None, keep.shape[-2]) or len(strides) == 4 and keep.shape[0] < num_layers:
+            raise PPDError(-3, "keep has fewer layers or sequences than the call, or not a list for every KV head")
         if keep.shape[-1] < count.max(initial=0):
             raise PPDError(-3, "keep has fewer entries than count")
         keep_strides = (0, strides[0], 0) if len(strides) == 2 else (0, strides[0], strides[1]) if len(strides) == 3 else strides[:3]

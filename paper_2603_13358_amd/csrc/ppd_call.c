@@ -7,7 +7,7 @@
 #include <Python.h>
 #include <stdint.h>
 
-static PyObject *s_data_ptr, *s_value, *s_shape, *s_element_size, *s_is_floating_point, *s_is_contiguous;
+static PyObject *s_data_ptr, *s_value, *s_shape, *s_dtype, *s_torch, *s_is_contiguous, *s_num_kv_heads;
 static PyObject *t_void_p, *f_cast;  // ctypes.c_void_p and ctypes.cast
 
 // What a ctypes parameter of type c_void_p takes: None, an int and a c_void_p (a context's handle) here, anything else --
@@ -56,15 +56,8 @@ static int to_int_or_shape(PyObject* o, PyObject* x, Py_ssize_t dim, int64_t* ou
     Py_DECREF(v);
     return ok;
 }
-// `o` as an int of 32 bits, or x.shape[dim] if it is None and x is given.  0 with *why set (and no error) if it does not fit: the call is refused
-// with that message.
-static int to_int32(PyObject* o, PyObject* x, Py_ssize_t dim, const char* name, int32_t* out, PyObject** why) {
-    if (o == Py_None && x) {
-        int64_t wide;
-        if (!to_int_or_shape(o, x, dim, &wide)) return 0;
-        *out = (int32_t)wide;
-        return 1;
-    }
+// `o` as an int of 32 bits.  0 with *why set (and no error) if it does not fit: the call is refused with that message.
+static int to_int32(PyObject* o, const char* name, int32_t* out, PyObject** why) {
     PyObject* v = PyNumber_Long(o);
     if (!v) return 0;
     int over;
@@ -78,30 +71,79 @@ static int to_int32(PyObject* o, PyObject* x, Py_ssize_t dim, const char* name, 
     *out = (int32_t)wide;
     return 1;
 }
-// Whether a tensor's elements are what the call takes (an address or None is taken on trust): 0 with *why set if not.
-static int call_int(PyObject* o, PyObject* method, int64_t* out) {
-    PyObject* v = PyObject_CallMethodNoArgs(o, method);
-    if (!v) return 0;
-    const int ok = to_int(v, out);
-    Py_DECREF(v);
+// Whether a tensor's elements are of one of two of torch's types (an address or None is taken on trust): 0 with *why set if not.  `types` holds the
+// type objects once torch has been found.
+typedef struct { const char* names[2]; PyObject* types[2]; } elem_types;
+static elem_types t_float32 = {{"float32", "float32"}, {NULL, NULL}}, t_int32 = {{"int32", "int32"}, {NULL, NULL}}, t_mask = {{"int64", "uint64"}, {NULL, NULL}};
+static int has_elements(PyObject* o, const char* name, elem_types* t, PyObject** why) {
+    if (o == Py_None || PyLong_Check(o)) return 1;
+    if (!t->types[1]) {
+        PyObject* torch = PyImport_GetModule(s_torch);
+        if (!torch) return !PyErr_Occurred();  // then it is not one of its tensors
+        for (int i = 0; i < 2; ++i)
+            if (!t->types[i] && !(t->types[i] = PyObject_GetAttrString(torch, t->names[i]))) {
+                Py_DECREF(torch);
+                return 0;
+            }
+        Py_DECREF(torch);
+    }
+    PyObject* type = PyObject_GetAttr(o, s_dtype);
+    if (!type) return 0;
+    const int ok = type == t->types[0] || type == t->types[1];
+    Py_DECREF(type);
+    if (!ok) *why = PyUnicode_FromFormat("%s has to be of type %s", name, t->names[0]);
     return ok;
 }
-static int has_elements(PyObject* o, const char* name, int64_t bytes, int floating, const char* type, PyObject** why) {
-    int64_t size, is_floating;
-    if (o == Py_None || PyLong_Check(o)) return 1;
-    if (!call_int(o, s_element_size, &size) || !call_int(o, s_is_floating_point, &is_floating)) return 0;
-    if (size == bytes && (is_floating != 0) == floating) return 1;
-    *why = PyUnicode_FromFormat("%s has to be of %s", name, type);
+// KV heads of the context behind a handle that ppd_create of the binding has made; 0 for another one
+static int64_t heads_of(PyObject* ctx) {
+    int64_t heads = 0;
+    PyObject* v = PyObject_GetAttr(ctx, s_num_kv_heads);
+    if (!v || !to_int(v, &heads)) {
+        PyErr_Clear();
+        heads = 0;
+    }
+    Py_XDECREF(v);
+    return heads;
+}
+// The stride of a tensor's rows: as given, or the last axis of a contiguous tensor of `outer` rows (at least; exactly, where further ones are
+// addressed behind these) for each of `heads` KV heads (0: not known).
+static int row_stride(PyObject* o, PyObject* stride, const char* name, int64_t outer, int64_t heads, int exact, int64_t* out, PyObject** why) {
+    if (stride != Py_None || o == Py_None || PyLong_Check(o)) return to_int_or_shape(stride, o, -1, out);
+    PyObject* v = PyObject_CallMethodNoArgs(o, s_is_contiguous);
+    const int dense = v ? PyObject_IsTrue(v) : -1;
+    Py_XDECREF(v);
+    if (dense == 0) *why = PyUnicode_FromFormat("%s has to be contiguous, or its stride given", name);
+    if (dense <= 0) return 0;
+    PyObject* shape = PyObject_GetAttr(o, s_shape);
+    if (!shape) return 0;
+    if (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) < 1) {
+        Py_DECREF(shape);
+        *why = PyUnicode_FromFormat("%s needs an axis of rows", name);
+        return 0;
+    }
+    const Py_ssize_t axes = PyTuple_GET_SIZE(shape);
+    int64_t rows = 1, axis = heads;
+    for (Py_ssize_t i = 0; i < axes; ++i) {
+        const int64_t len = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
+        if (i == axes - 1) *out = len;
+        else rows *= len;
+        if (axes > 2 && i == axes - 2) axis = len;
+    }
+    Py_DECREF(shape);
+    if (PyErr_Occurred()) return 0;
+    const int64_t want = outer * (heads > 0 ? heads : 1);
+    if ((heads <= 0 || axis == heads) && (!exact ? rows >= want : heads > 0 ? rows == want : want > 0 && rows % want == 0)) return 1;
+    *why = heads > 0 ? PyUnicode_FromFormat("%s has %lld rows, the call needs %lld for each of %lld KV heads", name, (long long)rows, (long long)outer, (long long)heads)
+                     : PyUnicode_FromFormat("%s has %lld rows, the call needs %lld for each KV head", name, (long long)rows, (long long)outer);
     return 0;
 }
-// Whether a tensor whose strides are taken from its shape (`stride` is None) has these strides.
-static int is_dense(PyObject* o, PyObject* stride, const char* name, PyObject** why) {
-    int64_t dense;
-    if (stride != Py_None || o == Py_None || PyLong_Check(o)) return 1;
-    if (!call_int(o, s_is_contiguous, &dense)) return 0;
-    if (dense) return 1;
-    *why = PyUnicode_FromFormat("%s has to be contiguous, or its stride given", name);
-    return 0;
+// The same in 32 bits, of a tensor of `outer` rows
+static int row_stride32(PyObject* o, PyObject* stride, const char* name, const char* stride_name, int64_t outer, int32_t* out, PyObject** why) {
+    int64_t wide;
+    if (stride != Py_None) return to_int32(stride, stride_name, out, why);
+    if (!row_stride(o, stride, name, outer, 0, 0, &wide, why)) return 0;
+    *out = wide <= INT32_MAX ? (int32_t)wide : INT32_MAX;
+    return 1;
 }
 static int expect(Py_ssize_t have, Py_ssize_t want) {
     if (have == want) return 1;
@@ -218,12 +260,14 @@ static PyObject* call_tree(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     (void)self;
     if (!expect(n, 13)) return NULL;
     if (!int32_arrays(a[8], a[9], &L, &nn)) Py_RETURN_NONE;
+    int64_t rows = 0;
+    for (Py_ssize_t i = 0; i < nn.shape[0]; ++i) rows += ((const int32_t*)nn.buf)[i];
     PyObject* result = NULL;
     PyObject* scale = NULL;
-    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int32(a[5], a[4], 1, "max_pages", &max_pages, &why) && to_int32(a[7], a[6], 1, "mask_words", &words, &why) &&
-        to_address(a[2], &q) && to_address(a[3], &pages) && has_elements(a[4], "page_tables", 4, 0, "int32", &why) &&
-        is_dense(a[4], a[5], "page_tables", &why) && to_address(a[4], &tables) &&
-        has_elements(a[6], "tree_mask", 8, 0, "int64 or uint64", &why) && is_dense(a[6], a[7], "tree_mask", &why) && to_address(a[6], &mask) &&
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_stride32(a[4], a[5], "page_tables", "max_pages", L.shape[0], &max_pages, &why) &&
+        row_stride32(a[6], a[7], "tree_mask", "mask_words", rows, &words, &why) &&
+        to_address(a[2], &q) && to_address(a[3], &pages) && has_elements(a[4], "page_tables", &t_int32, &why) && to_address(a[4], &tables) &&
+        has_elements(a[6], "tree_mask", &t_mask, &why) && to_address(a[6], &mask) &&
         (scale = PyNumber_Float(a[10])) && to_address(a[11], &out) && to_handle(a[12], &stream)) {
         const float s = (float)PyFloat_AS_DOUBLE(scale);
         int32_t status;
@@ -251,12 +295,10 @@ static PyObject* call_weighted(PyObject* self, PyObject* const* a, Py_ssize_t n)
     if (!int32_arrays(a[6], a[7], &L, &nn)) Py_RETURN_NONE;
     PyObject* result = NULL;
     PyObject* scale = NULL;
-    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int32(a[5], a[4], 1, "max_pages", &max_pages, &why) && to_int_or_shape(a[11], a[10], -1, &stride) &&
-        to_address(a[2], &q) && to_address(a[3], &pages) && has_elements(a[4], "page_tables", 4, 0, "int32", &why) &&
-        is_dense(a[4], a[5], "page_tables", &why) && to_address(a[4], &tables) &&
-        (scale = PyNumber_Float(a[8])) &&
-        to_address(a[9], &out) && has_elements(a[10], "weights", 4, 1, "float32", &why) &&
-        is_dense(a[10], a[11], "weights", &why) && to_address(a[10], &weights) && to_handle(a[12], &stream)) {
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_stride32(a[4], a[5], "page_tables", "max_pages", L.shape[0], &max_pages, &why) &&
+        row_stride(a[10], a[11], "weights", L.shape[0], heads_of(a[1]), 0, &stride, &why) &&
+        to_address(a[2], &q) && to_address(a[3], &pages) && has_elements(a[4], "page_tables", &t_int32, &why) && to_address(a[4], &tables) &&
+        (scale = PyNumber_Float(a[8])) && to_address(a[9], &out) && has_elements(a[10], "weights", &t_float32, &why) && to_address(a[10], &weights) && to_handle(a[12], &stream)) {
         const float s = (float)PyFloat_AS_DOUBLE(scale);
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
@@ -283,11 +325,12 @@ static PyObject* call_select(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     if (!expect(n, 11)) return NULL;
     if (!int32_array(a[4], &len)) Py_RETURN_NONE;
     PyObject* result = NULL;
-    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_int_or_shape(a[3], a[2], -1, &stride) && to_int_or_shape(a[9], a[8], -1, &keep_stride) &&
-        has_elements(a[2], "weights", 4, 1, "float32", &why) && is_dense(a[2], a[3], "weights", &why) &&
-        has_elements(a[8], "keep", 4, 0, "int32", &why) && is_dense(a[8], a[9], "keep", &why) &&
-        to_address(a[2], &weights) && to_int32(a[5], NULL, 0, "budget", &budget, &why) && to_int32(a[6], NULL, 0, "sinks", &sinks, &why) &&
-        to_int32(a[7], NULL, 0, "recent", &recent, &why) && to_address(a[8], &keep) && to_handle(a[10], &stream)) {
+    const int64_t heads = heads_of(a[1]);
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_stride(a[2], a[3], "weights", len.shape[0], heads, 0, &stride, &why) &&
+        row_stride(a[8], a[9], "keep", len.shape[0], heads, 0, &keep_stride, &why) &&
+        has_elements(a[2], "weights", &t_float32, &why) && has_elements(a[8], "keep", &t_int32, &why) &&
+        to_address(a[2], &weights) && to_int32(a[5], "budget", &budget, &why) && to_int32(a[6], "sinks", &sinks, &why) &&
+        to_int32(a[7], "recent", &recent, &why) && to_address(a[8], &keep) && to_handle(a[10], &stream)) {
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
         status = ((select_fn)fn)(ctx, (const float*)weights, stride, (const int32_t*)len.buf, (int32_t)len.shape[0], budget, sinks, recent,
@@ -312,10 +355,11 @@ static PyObject* call_compact(PyObject* self, PyObject* const* a, Py_ssize_t n) 
     if (!int32_arrays(a[11], a[12], &first, &count)) Py_RETURN_NONE;
     PyObject* result = NULL;
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && to_address(a[2], &pages) && to_int(a[3], &layer_stride) &&
-        to_int32(a[4], NULL, 0, "num_layers", &layers, &why) && to_int32(a[6], a[5], 1, "max_pages", &max_pages, &why) && has_elements(a[5], "page_tables", 4, 0, "int32", &why) &&
-        is_dense(a[5], a[6], "page_tables", &why) && to_address(a[5], &tables) && has_elements(a[7], "keep", 4, 0, "int32", &why) &&
-        has_elements(a[13], "weights", 4, 1, "float32", &why) && is_dense(a[13], a[14], "weights", &why) && to_address(a[7], &keep) && to_int(a[8], &kl) && to_int(a[9], &ks) &&
-        to_int(a[10], &kh) && (a[13] == Py_None || to_int_or_shape(a[14], a[13], -1, &stride)) && to_address(a[13], &weights) && to_handle(a[15], &stream)) {
+        to_int32(a[4], "num_layers", &layers, &why) && row_stride32(a[5], a[6], "page_tables", "max_pages", first.shape[0], &max_pages, &why) &&
+        has_elements(a[5], "page_tables", &t_int32, &why) && to_address(a[5], &tables) && has_elements(a[7], "keep", &t_int32, &why) &&
+        has_elements(a[13], "weights", &t_float32, &why) &&
+        (a[13] == Py_None || row_stride(a[13], a[14], "weights", layers * (int64_t)first.shape[0], heads_of(a[1]), layers > 1 && first.shape[0] > 0, &stride, &why)) &&
+        to_address(a[7], &keep) && to_int(a[8], &kl) && to_int(a[9], &ks) && to_int(a[10], &kh) && to_address(a[13], &weights) && to_handle(a[15], &stream)) {
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
         status = ((compact_fn)fn)(ctx, pages, layer_stride, layers, (const int32_t*)tables, max_pages, (const int32_t*)keep, kl, ks, kh,
@@ -344,14 +388,15 @@ PyMODINIT_FUNC PyInit_ppd_call(void) {
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_value = PyUnicode_InternFromString("value");
     s_shape = PyUnicode_InternFromString("shape");
-    s_element_size = PyUnicode_InternFromString("element_size");
-    s_is_floating_point = PyUnicode_InternFromString("is_floating_point");
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_torch = PyUnicode_InternFromString("torch");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    s_num_kv_heads = PyUnicode_InternFromString("num_kv_heads");
     PyObject* ctypes = PyImport_ImportModule("ctypes");
     if (!ctypes) return NULL;
     t_void_p = PyObject_GetAttrString(ctypes, "c_void_p");
     f_cast = PyObject_GetAttrString(ctypes, "cast");
     Py_DECREF(ctypes);
-    if (!s_data_ptr || !s_value || !s_shape || !s_element_size || !s_is_floating_point || !s_is_contiguous || !t_void_p || !f_cast) return NULL;
+    if (!s_data_ptr || !s_value || !s_shape || !s_dtype || !s_torch || !s_is_contiguous || !s_num_kv_heads || !t_void_p || !f_cast) return NULL;
     return PyModule_Create(&kModule);
 }

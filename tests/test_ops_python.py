@@ -104,3 +104,56 @@ def test_views_whose_strides_are_not_their_shapes_are_refused():
         assert status(call, page_tables=tables[:, :3], max_pages=5) == -1
     layers = torch.zeros(3, 2, 4, 40)
     assert status(weighted, weights=layers[1]) == -1  # a layer's part is whole
+
+
+def handle(heads):
+    """As ppd_create gives it, but of no context."""
+    h = ctypes.c_void_p()
+    h.num_kv_heads = heads
+    return h
+
+
+def test_tensors_with_too_few_rows_are_refused():
+    h = handle(4)
+    for call in (tree, weighted, select, compact):
+        assert status(call, h) == -1
+    for shape in [(1, 4, 40), (2, 3, 40), (2, 8, 40), (4, 40), (40,)]:
+        for call in (weighted, select, compact):
+            assert refused(call, "weights", h, weights=torch.zeros(*shape))
+    for shape in [(2, 4, 40), (3, 4, 40), (8, 40), (1, 2, 4, 40)]:
+        for call in (weighted, select, compact):
+            assert status(call, h, weights=torch.zeros(*shape)) == -1
+    for shape in [(1, 4, 20), (2, 2, 20), (20,)]:
+        assert refused(select, "keep", h, keep=torch.zeros(*shape, dtype=torch.int32))
+    for call in (tree, weighted, compact):
+        assert refused(call, "page_tables", h, page_tables=torch.zeros(1, 3, dtype=torch.int32))
+        assert status(call, h, page_tables=torch.zeros(3, 3, dtype=torch.int32)) == -1
+    assert refused(tree, "tree_mask", h, tree_mask=torch.zeros(4, 1, dtype=torch.int64))
+    assert status(tree, h, tree_mask=torch.zeros(6, 2, dtype=torch.int64)) == -1
+    # a handle of which the heads are not known: one row for a sequence at least
+    assert refused(weighted, "weights", weights=torch.zeros(1, 40))
+    assert status(weighted, weights=torch.zeros(2, 4, 40)) == -1
+
+
+@pytest.mark.parametrize("h", [None, handle(4)], ids=["address", "handle"])
+def test_weights_and_lists_of_several_layers(h):
+    """A move of several layers takes weights with a layer axis of just these layers, sequences and heads."""
+    layers = dict(num_layers=3, layer_stride_elems=1 << 20)
+    assert status(compact, h, **layers) == -1
+    assert refused(compact, "weights", h, weights=torch.zeros(2, 4, 40), **layers)
+    assert refused(compact, "weights", h, weights=torch.zeros(2, 40), **layers)
+    assert refused(compact, "weights", h, weights=torch.zeros(1, 2, 4, 40), **layers)
+    assert status(compact, h, weights=torch.zeros(3, 2, 4, 40), **layers) == -1
+    assert status(compact, h, weights=torch.zeros(3, 2, 4, 40), first=np.zeros(0, np.int32), count=np.zeros(0, np.int32), **layers) == -1
+    if h is not None:  # sequences behind the call's: the next layer starts behind them
+        assert refused(compact, "weights", h, weights=torch.zeros(3, 5, 4, 40), **layers)
+    assert status(compact, h, weights=torch.zeros(2, 4, 40), weight_stride=40, **layers) == -1  # on the caller's word
+    lists = lambda *shape: torch.zeros(*shape, 20, dtype=torch.int32)  # noqa: E731
+    assert status(compact, h, keep=lists(3, 2, 4), **layers) == -1
+    assert status(compact, h, keep=lists(2), **layers) == -1
+    assert status(compact, h, keep=lists(1, 1, 4).expand(3, 2, 4, 20), **layers) == -1
+    for shape in [(2, 2, 4), (3, 1, 4), (1, 4), (1,)]:
+        assert refused(compact, "keep", h, keep=lists(*shape), **layers)
+    if h is not None:
+        assert refused(compact, "keep", h, keep=lists(2, 3), **layers)
+        assert refused(compact, "keep", h, keep=lists(3, 2, 8), **layers)
