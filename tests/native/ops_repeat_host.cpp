@@ -145,11 +145,40 @@ static void longest() {
     ppd_destroy(ctx);
 }
 
+// Ranges that are split and several row blocks of a sequence at once: every block's groups name its own columns, so that the join
+// leaves the references of all rows.  (The lengths are those of the GPU's test of it.)
+static void split_blocks() {
+    struct { int32_t hq, hkv, dim, eb; std::vector<int32_t> L, n; } cases[] = {
+        {8, 1, 128, 2, {9000}, {70}}, {10, 2, 64, 1, {5000, 3}, {130, 60}}, {2, 1, 64, 2, {3000, 200, 2500}, {300, 1, 290}}};
+    for (const auto& c : cases) {
+        const ppd_shape s = {c.hq, c.hkv, c.dim, 16, 1 << 16};
+        const int G = c.hq / c.hkv;
+        ppd::TreePlan p;
+        CHECK(ppd::build_tree_plan(s, c.L.data(), c.n.data(), (int)c.L.size(), true, c.eb, 256, &p));
+        std::set<std::pair<int, int>> rows;  // (row, KV head) of split ranges of row blocks
+        bool behind_the_first = false;
+        for (const auto& g : p.groups) {
+            if (g.ncols <= ppd::kTreeCols && g.col0 == 0) continue;
+            behind_the_first |= g.col0 > 0 && g.nsplit > 1;
+            CHECK(g.col0 % G == 0 && g.ncols % G == 0);
+            for (int col = g.col0; col < g.col0 + g.ncols; col += G) CHECK(rows.emplace(g.grow0 + col / G, g.kvh).second);
+        }
+        CHECK(behind_the_first && p.weighs.size() > 0);
+        int split = 0;
+        for (size_t i = 0, at = 0; i < c.L.size(); at += c.n[i++])
+            if (rows.count({(int)at, 0}))
+                for (int j = 0; j < c.n[i]; ++j)
+                    for (int h = 0; h < c.hkv; ++h) CHECK(rows.count({(int)at + j, h}) && ++split);
+        CHECK(split == (int)rows.size());
+    }
+}
+
 int main(int, char** argv) {
     const std::string what = argv[1];
     if (what == "first_call_under_capture") first_call_under_capture();
     else if (what == "kinds") kinds();
     else if (what == "longest") longest();
+    else if (what == "split_blocks") split_blocks();
     else return 2;
     std::printf("ok\n");
     return 0;

@@ -63,3 +63,16 @@ def test_a_row_whose_every_score_is_minus_infinity_gives_zeros_and_no_weight(n, 
     assert not ref[0].any() and not out[0].any()
     within(out, ref, bound)
     within(w[0], *weights[0])
+
+
+@pytest.mark.parametrize("L,n,hq,hkv,dim,fp8", [([9000], [70], 8, 1, 128, False), ([5000, 3], [130, 60], 10, 2, 64, True),
+                                                ([3000, 200, 2500], [300, 1, 290], 2, 1, 64, False)], ids=["d128", "fp8", "d64"])
+def test_weights_of_split_ranges_and_several_row_blocks(L, n, hq, hkv, dim, fp8):
+    """Every row's reference comes from the join of its own block's partials."""
+    b = Batch(L, n, hq, hkv, dim, fp8, seed=62)
+    ref, bound, weights = b.reference()
+    w = torch.zeros((len(L), hkv, int((b.L + b.n).max())), device="cuda")
+    within(b.weighted(w), ref, bound)
+    for i, (ww, wb) in enumerate(weights):
+        within(w[i, :, :L[i] + n[i]], ww, wb + 2.0 ** -23 * ww)
+    assert b.flags() == 0
