@@ -94,12 +94,25 @@ bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int
     plan->score_floats = 0;
     plan->partial_floats = 0;
     plan->join_cols = 0;
+    // Measured on weighted and tree calls of 1, 6, 24 and 64 sequences (4 and 24 columns; D = 128 on bf16 and FP8 pages, D = 64): starts of 64 or
+    // 128 keys take up to 17 % longer (64 trees, D = 64: 24.4 -> 28.7 us), 512 and 1024 the same but for 24 trees at D = 128, which gain (63 ->
+    // 55.5 us, FP8 43 -> 35), as they do with columns of 0.02; joins of 64 to 2048 keys make no difference.
     const TileKind narrow = {kMaxTreeChunk, kTreeStep, 256, 256, 0, 2 * num_cus};
     // Measured over batches of 4, 6 and 32 sequences cut into 512 to 8192 keys (D = 128): a row block takes 6.6 us and 1.2 us per 64
-    // keys, a split launch 9.5 us more and 0.2 us per 1000 columns of partials.
+    // keys, a split launch 9.5 us more and 0.2 us per 1000 columns of partials.  On FP8 pages and at D = 64, where a step takes another
+    // time, the same numbers serve: over 2, 6 and 32 sequences, 5 and 8 query heads to a KV head, starts of 200 to 500 keys and joins
+    // of 250 to 1000 are within 2 %; a start of 700 costs 5-8 % on FP8 pages, twice the column 4-12 % at D = 128 (and gains up to 7 % for
+    // two sequences at D = 64), half of it up to 9 % at D = 64.
     const TileKind wide = {kMaxTreeBlockChunk, kTileTokens, 350, 500, 0.0114, num_cus};
     const int block_rows = kMfmaCols / G;
-    // Scores are kept where writing and reading them (8 bytes a column and key) moves less than reading K again.
+    // Scores are kept where writing and reading them (8 bytes a column and key) moves no more than reading K again.  Kept against computed
+    // again, us, decodes of 1, 8 and 64 sequences of 4K, 8K-16K and 1K-8K keys, 8 KV heads:
+    //   D = 128, bf16   8 columns 13.4 72 175 / 19 94 222    16: 14.3 81 198 / 20 94 226    32 (the last kept): 16.4 100 250 / 21 97 236
+    //   D = 128, FP8    8 columns 13.5 43 101 / 19 62 134    16 (the last kept): 14.3 54 123 / 20 62 136    32: 16.4 74 177 / 21 65 141
+    //   D = 64, bf16    8 columns 11.3 43 97 / 16 54 123     16 (the last kept): 11.9 54 118 / 17 54 124    32: 13.3 67 158 / 18 56 127
+    //   D = 64, FP8     8 columns (the last kept): 11.8 30 64 / 17 40 82     16: 12.3 42 87 / 17 40 83
+    // One sequence gains by them at any width, batches up to half of the rule's edge at least; at the edge on bf16 pages of D = 128 batches
+    // lose 3-6 %.
     auto keeps_scores = [&](int32_t rows) { return weighted && (int64_t)rows * G <= kTreeCols && (int64_t)rows * G * 8 <= (int64_t)D * kv_elem_bytes; };
     auto max_piece = [&](int32_t rows) {
         if ((int64_t)rows * G > kTreeCols) return wide.max_chunk;
