@@ -270,7 +270,9 @@ ppd_status ppd_weighted_attention(ppd_ctx *ctx, const void *q, const void *kv_pa
  *   length        HOST int32 [B], tokens of every sequence, 0 <= length_i <= weight_stride
  *   budget        >= 1; sinks, recent >= 0; sinks + recent <= budget
  *   keep          device int32 [B][Hkv][keep_stride], keep_stride >= min(budget, length_i): positions in ascending order; entries from
- *                 min(budget, length_i) on are not touched */
+ *                 min(budget, length_i) on are not touched
+ * Rows of more than 16384 tokens take a workspace: where a launch (of 512 sequences at a time) has one, 139 KB for every 16384 tokens
+ * or part of them of its longest row, for each KV head of each of its sequences. */
 ppd_status ppd_kv_select(ppd_ctx *ctx, const float *weights, int64_t weight_stride, const int32_t *length, int32_t B,
                          int32_t budget, int32_t sinks, int32_t recent, int32_t *keep, int64_t keep_stride, void *stream);
 

@@ -459,11 +459,12 @@ int launch_select(const SelectParams& p, int longest, void* stream) {
 // that leaves room for -- reads all of them, waits, and writes.  Every d is independent, so K, V and slices of d are workgroups of their
 // own; the weights are another.  Entries that do not ascend or lie outside the sequence's pages raise the sticky flag, and their
 // tokens stay where they are.
-// Bound by memory, in whole lines of 128 bytes: a line of K is 8 tokens' 8 d, a line of V 8 d of 8 tokens, and both are read for one token as
-// for eight.  32 evictions from 1K-8K to 1024 tokens, every head its own: 271 MB of kept tokens' bytes, in and out, are 610 MB of
-// lines, 126 us at 4.9 TB/s (a large copy's rate: 4.9); K alone takes 54 us, V alone 66.  The accepted paths of 16 trees over 32
-// layers: 22 MB, about 100 MB of lines, 22 us.  Nothing moves less in this layout.  Short lists are a chain of reads -- list, page,
-// token -- so there one workgroup takes all heads.
+// Bound by memory, in whole lines of 128 bytes: a line of K is 8 d of 8 tokens (of 16 on FP8 pages), a line of V 8 tokens of 8 d, and both
+// are read for one token as for all.  32 evictions from 1K-8K to 1024 tokens, every head its own: for 135 MB of kept tokens 392 MB are
+// read and 135 MB written (counters), 131 us, 4.0 TB/s, where a large copy reaches 4.9; called again on the same pool, part of which
+// the memory side still holds, 108 us.  FP8 pages: 216 and 68 MB, 70 us.  The accepted paths of 16 trees over 32 layers: for 11 MB
+// 56 MB read and 19 MB written, 23 us (FP8: 35 and 10 MB, 16 us).  Short lists are a chain of reads -- list, page, token -- so there
+// one workgroup takes all heads.
 constexpr int kCompactThreads = 256, kMoves = 128, kUnits = 4;  // units (granules) a thread moves at a time
 constexpr int kTogether = 2;  // granules of V whose sources a wave asks for at once
 constexpr int kCompactWidth = kUnits * kCompactThreads * 8 / kMoves;  // d of a slice
