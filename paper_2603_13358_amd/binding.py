@@ -196,9 +196,15 @@ def _check_call(status, ctx):
     _check(status, ctx)
 
 
+_INT32 = np.dtype(np.int32)
+
+
 def _lengths(*arrays):
-    """Host int32 arrays of one length."""
-    arrays = [_host_i32(a).reshape(-1) for a in arrays]
+    """Host int32 arrays of one length, of the same values as the arguments."""
+    given, arrays = arrays, [_host_i32(a).reshape(-1) for a in arrays]
+    for g, a in zip(given, arrays):
+        if getattr(g, "dtype", None) is not _INT32 and not np.array_equal(np.asarray(g).reshape(-1), a):
+            raise PPDError(-3, "the host arrays hold values that are not 32-bit integers")
     if any(a.shape != arrays[0].shape for a in arrays):
         raise PPDError(-3, "the host arrays differ in length")
     return arrays

@@ -157,3 +157,16 @@ def test_weights_and_lists_of_several_layers(h):
     if h is not None:
         assert refused(compact, "keep", h, keep=lists(2, 3), **layers)
         assert refused(compact, "keep", h, keep=lists(3, 2, 8), **layers)
+
+
+def test_lengths_that_are_not_32_bit_integers_are_refused():
+    for far in (np.array([(1 << 32) + 30, 5]), np.array([30.5, 5.0]), np.array([-(1 << 40), 5])):
+        for call in (tree, weighted):
+            assert refused(call, "32-bit", L=far)
+            assert refused(call, "32-bit", n=far)
+        assert refused(select, "32-bit", length=far)
+        assert refused(compact, "32-bit", first=far)
+        assert refused(compact, "32-bit", count=far)
+    for same in (L.astype(np.int64), L.astype(np.uint8), L.astype(np.float64), list(map(int, L)), torch.from_numpy(L), np.stack([L, L])[0]):
+        assert status(tree, L=same) == -1 and status(select, length=same) == -1
+        assert status(compact, first=same) == -1
