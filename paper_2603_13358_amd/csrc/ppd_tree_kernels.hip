@@ -43,8 +43,8 @@ __device__ __forceinline__ void stage_pages(const TreeParams& P, int seq, int kv
 // takes from the pool straight into registers in the layouts of the matrix instructions' operands: no LDS, no barrier.  The
 // waves' results meet in LDS at the end.  Probabilities enter the second product as bf16 numbers, as the matrix instruction takes them
 // (their sum is of the 32-bit ones); everything else is held in 32 bits.
-// Bound by memory where there is much to read: 64 decodes of 1K-8K keys (32 query heads, D = 128) 142 us, 6.6 TB/s (162 with the scores'
-// stores, FP8 pages 87, 5.3 TB/s), trees of 4-8 nodes on the same 171 us, 5.8 TB/s (FP8 91); by a chain of
+// Bound by memory where there is much to read: 64 decodes of 1K-8K keys (32 query heads, D = 128) 142 us, 6.6 TB/s (with the scores'
+// stores 162, on FP8 pages 87, 5.4 TB/s), trees of 4-8 nodes on the same 171 us, 5.8 TB/s (FP8 pages 91); by a chain of
 // dependent loads (tile, page ids, K) of 5 us in small launches.  More than 32 columns as several tiles side by side, their keys read
 // from L2 once more for every 32, were no faster than row blocks from 64 columns on (32 trees of 8-24 nodes, 8 query heads to a KV
 // head: 137-152 us against 137), and two launches where a batch has both kinds.
