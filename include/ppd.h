@@ -293,6 +293,64 @@ ppd_status ppd_kv_compact(ppd_ctx *ctx, void *kv_pages, int64_t layer_stride_ele
                           int64_t keep_seq_stride, int64_t keep_head_stride, const int32_t *first, const int32_t *count,
                           int32_t B, float *weights, int64_t weight_stride, void *stream);
 
+/* ---- Positions and shared prefixes ----
+ * What a serving loop needs around the append and the attention: queries and keys rotated by their positions, on their own or on the way
+ * into the pages, and attention of a batch that shares leading tokens.  All calls are asynchronous on `stream` and under the conventions
+ * above; ppd_rope and ppd_kv_append_rotated can always be captured. */
+
+/* The rotation.  Pair i of a head's first rotary_dim elements, (a, b), becomes
+ *     amplitude * (a cos t - b sin t, b cos t + a sin t),   t = position * inv_freq[i]
+ * in binary32, rounded once; elements from rotary_dim on keep their bits.
+ *   inv_freq      HOST double [rotary_dim / 2], radians per position, finite
+ *   rotary_dim    even, in [2, head_dim]
+ *   layout        PPD_ROPE_HALF: pair i is elements (i, i + rotary_dim / 2); PPD_ROPE_INTERLEAVED: (2i, 2i + 1)
+ *   amplitude     finite; a factor of what is rotated (1, but for some ways of stretching long contexts)
+ * Takes effect from the next call on; calls that are enqueued or captured keep what they were made with, so the layers of one step may
+ * differ.  Positions are 64-bit integers of either sign: whole turns are left out in integer arithmetic, which leaves an angle off by at most
+ * |position| * 2^-61 radians (frequencies of up to one radian) and 2^-23 on top; the sine and cosine of it are right to 2^-22. */
+#define PPD_ROPE_HALF 0
+#define PPD_ROPE_INTERLEAVED 1
+ppd_status ppd_set_rope(ppd_ctx *ctx, const double *inv_freq, int32_t rotary_dim, int32_t layout, float amplitude);
+
+/* Frequencies for ppd_set_rope (host only; inv_freq HOST double [rotary_dim / 2], 2 <= rotary_dim <= 128, even):
+ *   PPD_ROPE_SCALE_NONE      base^(-2i / rotary_dim)
+ *   PPD_ROPE_SCALE_LINEAR    the same over `factor`: positions are interpolated
+ *   PPD_ROPE_SCALE_BASE      of a base of base * factor^(rotary_dim / (rotary_dim - 2)): the slowest pair is stretched by `factor`, the
+ *                            fastest not at all (rotary_dim >= 4)
+ *   PPD_ROPE_SCALE_BY_PARTS  g f + (1 - g) f / factor, where g rises linearly from 0 to 1 between low_turns and high_turns turns that the
+ *                            pair makes in original_length positions: fast pairs keep their frequency, slow ones are interpolated
+ * Arguments that a scaling does not use are ignored.  Messages are read with ppd_last_error(NULL). */
+#define PPD_ROPE_SCALE_NONE 0
+#define PPD_ROPE_SCALE_LINEAR 1
+#define PPD_ROPE_SCALE_BASE 2
+#define PPD_ROPE_SCALE_BY_PARTS 3
+ppd_status ppd_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double original_length,
+                                double low_turns, double high_turns, double *inv_freq);
+
+/* Rotates the heads of T rows by their positions.  transpose != 0: by the transposed matrices, which are the gradient (and, over
+ * amplitude^2, the inverse).
+ *   x, out        device bf16 [T][heads][head_dim], rows x_stride and out_stride elements apart (multiples of 8, at least
+ *                 heads * head_dim; ignored for T = 1), 16-byte aligned.  out may be x with the same stride; any other overlap of the
+ *                 rows' ranges is refused.  What lies between out's rows is not touched
+ *   heads         1 .. 4096, whatever the context's
+ *   positions     device int64 [T] */
+ppd_status ppd_rope(ppd_ctx *ctx, const void *x, int64_t x_stride, int32_t heads, const int64_t *positions, int64_t T,
+                    int32_t transpose, void *out, int64_t out_stride, void *stream);
+
+/* ppd_kv_append with the rotation of the keys on the way, and of the step's queries in the same launch.
+ *   q             device bf16 [T][Hq][D], rows q_stride elements apart; or NULL together with q_out: keys and values alone
+ *   k, v          device bf16 [T][Hkv][D], rows k_stride and v_stride elements apart (strides as for ppd_rope: the three may be parts of
+ *                 a projection's rows)
+ *   positions     device int64 [T]: of queries and keys
+ *   q_out         device bf16 [T][Hq][D], contiguous, as the attention calls take it; q itself where that is contiguous, apart from q, k
+ *                 and v otherwise.  All T rows are written, those of skipped tokens too
+ *   the rest      as for ppd_kv_append
+ * Rotated keys are rounded once, to bf16 or, on FP8 pages, from binary32 to the code of K / k_scale; on bf16 pages the pool is
+ * bit-identical to ppd_rope followed by ppd_kv_append. */
+ppd_status ppd_kv_append_rotated(ppd_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                                 int64_t v_stride, const int64_t *positions, void *kv_pages, const int64_t *slot_mapping, int64_t T,
+                                 void *q_out, void *stream);
+
 /* Statistics of the plan built by the last ppd_mixed_attention call on this context. */
 ppd_status ppd_get_plan_stats(const ppd_ctx *ctx, ppd_plan_stats *stats);
 

@@ -12,7 +12,7 @@ _LIB_PATH = os.path.join(_HERE, "libppd.so")
 _CALL_PATH = os.path.join(_HERE, "ppd_call" + sysconfig.get_config_var("EXT_SUFFIX"))  # built for this interpreter's ABI
 _lib = None
 _call = None       # the call module
-_fn_append = _fn_land = _fn_mixed = _fn_mixed_static = _fn_tree = _fn_weighted = _fn_select = _fn_compact = None  # addresses of the entry points it calls
+_fn_append = _fn_land = _fn_mixed = _fn_mixed_static = _fn_tree = _fn_weighted = _fn_select = _fn_compact = _fn_rope = _fn_append_rotated = None  # addresses of the entry points it calls
 
 STATUS_NAMES = {0: "PPD_OK", -1: "PPD_ERR_NULL", -2: "PPD_ERR_SHAPE", -3: "PPD_ERR_RANGE",
                 -4: "PPD_ERR_PAGETABLE", -5: "PPD_ERR_WORKSPACE", -6: "PPD_ERR_HIP"}
@@ -48,6 +48,7 @@ class PlanStats(ctypes.Structure):
 EXPORTS = ["ppd_create", "ppd_destroy", "ppd_last_error", "ppd_set_option", "ppd_kv_append", "ppd_kv_land",
            "ppd_transfer_delay_s", "ppd_mixed_attention", "ppd_mixed_attention_static",
            "ppd_tree_attention", "ppd_weighted_attention", "ppd_kv_select", "ppd_kv_compact",
+           "ppd_set_rope", "ppd_rope_frequencies", "ppd_rope", "ppd_kv_append_rotated",
            "ppd_get_plan_stats", "ppd_plan_build", "ppd_device_error_flags", "ppd_last_kernel_ms", "ppd_timed_kernels_ms",
            "ppd_route_score", "ppd_route_table_build", "ppd_route_cell", "ppd_route_decide", "ppd_route_decide_batch", "ppd_version"]
 
@@ -58,7 +59,7 @@ def lib_path():
 
 def load_library():
     """Loads libppd.so; raises if it has not been built (no fallback of any kind)."""
-    global _lib, _call, _fn_append, _fn_land, _fn_mixed, _fn_mixed_static, _fn_tree, _fn_weighted, _fn_select, _fn_compact
+    global _lib, _call, _fn_append, _fn_land, _fn_mixed, _fn_mixed_static, _fn_tree, _fn_weighted, _fn_select, _fn_compact, _fn_rope, _fn_append_rotated
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH) or not os.path.exists(_CALL_PATH):
@@ -82,13 +83,17 @@ def load_library():
     lib.ppd_weighted_attention.argtypes = [vp, vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp, i64, vp]
     lib.ppd_kv_select.argtypes = [vp, vp, i64, vp, i32, i32, i32, i32, vp, i64, vp]
     lib.ppd_kv_compact.argtypes = [vp, vp, i64, i32, vp, i32, vp, i64, i64, i64, vp, vp, i32, vp, i64, vp]
+    dbl = ctypes.c_double
+    lib.ppd_set_rope.argtypes = [vp, vp, i32, i32, ctypes.c_float]
+    lib.ppd_rope_frequencies.argtypes = [i32, dbl, i32, dbl, dbl, dbl, dbl, vp]
+    lib.ppd_rope.argtypes = [vp, vp, i64, i32, vp, i64, i32, vp, i64, vp]
+    lib.ppd_kv_append_rotated.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp]
     lib.ppd_get_plan_stats.argtypes = [vp, ctypes.POINTER(PlanStats)]
     lib.ppd_plan_build.argtypes = [ctypes.POINTER(Shape), vp, vp, i32, i32, i32, i32, i32, i32,
                                    ctypes.POINTER(WorkItem), i64, ctypes.POINTER(PlanStats)]
     lib.ppd_device_error_flags.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_uint32)]
     lib.ppd_last_kernel_ms.argtypes = [vp, ctypes.POINTER(ctypes.c_float)]
     lib.ppd_timed_kernels_ms.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32)]
-    dbl = ctypes.c_double
     lib.ppd_route_score.argtypes = [dbl, dbl, dbl, dbl]
     lib.ppd_route_score.restype = dbl
     lib.ppd_route_table_build.argtypes = [vp, vp, dbl, dbl, vp]
@@ -107,6 +112,7 @@ def load_library():
         lib.ppd_kv_append, lib.ppd_kv_land, lib.ppd_mixed_attention, lib.ppd_mixed_attention_static))
     _fn_tree, _fn_weighted, _fn_select, _fn_compact = (ctypes.cast(f, vp).value for f in (
         lib.ppd_tree_attention, lib.ppd_weighted_attention, lib.ppd_kv_select, lib.ppd_kv_compact))
+    _fn_rope, _fn_append_rotated = (ctypes.cast(f, vp).value for f in (lib.ppd_rope, lib.ppd_kv_append_rotated))
     _lib = lib
     return lib
 
@@ -132,7 +138,8 @@ def ppd_create(num_q_heads, num_kv_heads, head_dim, page_size, num_pages, device
     shape = Shape(num_q_heads, num_kv_heads, head_dim, page_size, num_pages)
     handle = ctypes.c_void_p()
     _check(load_library().ppd_create(ctypes.byref(shape), device, ctypes.byref(handle)))
-    handle.num_kv_heads = int(num_kv_heads)  # for the checks of tensors that have a row for every KV head
+    # for the checks of tensors that have a row for every head
+    handle.num_q_heads, handle.num_kv_heads, handle.head_dim = int(num_q_heads), int(num_kv_heads), int(head_dim)
     return handle
 
 
@@ -265,6 +272,44 @@ def ppd_kv_compact(ctx, kv_pages, page_tables, keep, first, count, layer_stride_
     status = _call.kv_compact(*args, first, count, weights, weight_stride, stream)
     if status is None:
         status = _call.kv_compact(*args, *_lengths(first, count), weights, weight_stride, stream)
+    if status != 0:
+        _check_call(status, ctx)
+
+
+PPD_ROPE_HALF, PPD_ROPE_INTERLEAVED = 0, 1
+PPD_ROPE_SCALE_NONE, PPD_ROPE_SCALE_LINEAR, PPD_ROPE_SCALE_BASE, PPD_ROPE_SCALE_BY_PARTS = 0, 1, 2, 3
+
+
+def ppd_rope_frequencies(rotary_dim, base=10000.0, scaling=PPD_ROPE_SCALE_NONE, factor=1.0, original_length=0.0, low_turns=1.0, high_turns=32.0):
+    """float64 [rotary_dim / 2]: radians per position of every pair."""
+    inv_freq = np.zeros(max(1, int(rotary_dim) // 2), np.float64)
+    _check(load_library().ppd_rope_frequencies(int(rotary_dim), float(base), int(scaling), float(factor), float(original_length), float(low_turns),
+                                               float(high_turns), inv_freq.ctypes.data))
+    return inv_freq
+
+
+def ppd_set_rope(ctx, inv_freq, layout=PPD_ROPE_HALF, amplitude=1.0):
+    """inv_freq: one frequency for every pair, in radians per position; rotary_dim is twice their number."""
+    inv_freq = np.ascontiguousarray(inv_freq, dtype=np.float64).reshape(-1)
+    _check(load_library().ppd_set_rope(ctx, inv_freq.ctypes.data, 2 * inv_freq.size, int(layout), float(amplitude)), ctx)
+
+
+def ppd_rope(ctx, x, positions, out, transpose=False, heads=None, T=None, x_stride=None, out_stride=None, stream=None):
+    """x, out: bfloat16 [rows][heads][head_dim], the heads of a row contiguous, or addresses with heads and strides.  positions: int64 [T]; the
+    first T rows are rotated."""
+    if _lib is None:
+        load_library()
+    status = _call.rope(_fn_rope, ctx, x, x_stride, heads, positions, T, transpose, out, out_stride, stream)
+    if status != 0:
+        _check_call(status, ctx)
+
+
+def ppd_kv_append_rotated(ctx, q, k, v, positions, kv_pages, slot_mapping, q_out, T=None, q_stride=None, k_stride=None, v_stride=None, stream=None):
+    """q, k, v: bfloat16 [rows][heads][head_dim], the heads of a row contiguous, or addresses with strides; q and q_out may be None.  slot_mapping and
+    positions: int64 [T]; the first T rows are taken."""
+    if _lib is None:
+        load_library()
+    status = _call.kv_append_rotated(_fn_append_rotated, ctx, q, q_stride, k, k_stride, v, v_stride, positions, kv_pages, slot_mapping, T, q_out, stream)
     if status != 0:
         _check_call(status, ctx)
 
@@ -407,6 +452,15 @@ class Context:
 
     def kv_compact(self, kv_pages, page_tables, keep, first, count, layer_stride_elems=0, num_layers=1, weights=None, stream=None):
         ppd_kv_compact(self.handle, kv_pages, page_tables, keep, first, count, layer_stride_elems, num_layers, weights, stream=stream)
+
+    def set_rope(self, inv_freq, layout=PPD_ROPE_HALF, amplitude=1.0):
+        ppd_set_rope(self.handle, inv_freq, layout, amplitude)
+
+    def rope(self, x, positions, out, transpose=False, stream=None):
+        ppd_rope(self.handle, x, positions, out, transpose, stream=stream)
+
+    def kv_append_rotated(self, q, k, v, positions, kv_pages, slot_mapping, q_out, stream=None):
+        ppd_kv_append_rotated(self.handle, q, k, v, positions, kv_pages, slot_mapping, q_out, stream=stream)
 
     def plan_stats(self):
         return ppd_get_plan_stats(self.handle)

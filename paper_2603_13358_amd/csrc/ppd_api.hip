@@ -72,16 +72,6 @@ __global__ void ppd_mark_slots_kernel(const int64_t* slots, int64_t T, int64_t p
     }
 }
 
-// PPD_DEBUG_SLOTS=1: looks for duplicate slots among the T slots of an append (error flag bit 2), on `stream`.
-void check_duplicate_slots(ppd_ctx* ctx, const int64_t* slot_mapping, int64_t T, hipStream_t hs) {
-    if (!ctx->d_slot_seen || T <= 0) return;
-    const int64_t pool_slots = ctx->shape.num_pages * ppd::kPage;
-    const unsigned blocks = (unsigned)((T + 255) / 256);
-    for (int clear = 0; clear < 2; ++clear)
-        hipLaunchKernelGGL(ppd_mark_slots_kernel, dim3(blocks), dim3(256), 0, hs, slot_mapping, T, pool_slots, ctx->d_slot_seen,
-                           ctx->d_counters + 9, clear);
-}
-
 ppd_status mixed_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages, const int32_t* page_tables,
                                 int32_t max_pages, const int32_t* L, const int32_t* n, int32_t B, float scale,
                                 void* out, void* stream, bool use_static) {
@@ -385,6 +375,15 @@ ppd_status mixed_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_page
 
 }  // namespace
 
+void ppd::check_duplicate_slots(ppd_ctx* ctx, const int64_t* slot_mapping, int64_t T, hipStream_t hs) {
+    if (!ctx->d_slot_seen || T <= 0) return;
+    const int64_t pool_slots = ctx->shape.num_pages * ppd::kPage;
+    const unsigned blocks = (unsigned)((T + 255) / 256);
+    for (int clear = 0; clear < 2; ++clear)
+        hipLaunchKernelGGL(ppd_mark_slots_kernel, dim3(blocks), dim3(256), 0, hs, slot_mapping, T, pool_slots, ctx->d_slot_seen,
+                           ctx->d_counters + 9, clear);
+}
+
 extern "C" {
 
 const char* ppd_version(void) { return "0.2"; }
@@ -484,6 +483,7 @@ ppd_status ppd_destroy(ppd_ctx* ctx) {
             g_scratch_owner[ctx->device] = nullptr;
     }
     if (ctx->free_tree) ctx->free_tree(ctx->tree);
+    if (ctx->free_prefix) ctx->free_prefix(ctx->prefix);
     delete ctx;
     return PPD_OK;
 }
@@ -558,7 +558,7 @@ ppd_status ppd_kv_append(ppd_ctx* ctx, const void* k, const void* v, void* kv_pa
                                    1, 0, ctx->d_counters + 9, stream, ctx->fp8_pages, 1.0f / ctx->k_scale,
                                    1.0f / ctx->v_scale);
     if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch kv_append");
-    check_duplicate_slots(ctx, slot_mapping, T, static_cast<hipStream_t>(stream));
+    ppd::check_duplicate_slots(ctx, slot_mapping, T, static_cast<hipStream_t>(stream));
     if (ctx->log_calls) std::fprintf(stderr, "ppd: kv_append T=%lld\n", (long long)T);
     return PPD_OK;
 }
@@ -584,7 +584,7 @@ ppd_status ppd_kv_land(ppd_ctx* ctx, const void* k, const void* v, void* kv_page
                                    num_layers, layer_stride_elems, ctx->d_counters + 9, stream, ctx->fp8_pages,
                                    1.0f / ctx->k_scale, 1.0f / ctx->v_scale);
     if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch kv_land");
-    check_duplicate_slots(ctx, slot_mapping, T, static_cast<hipStream_t>(stream));
+    ppd::check_duplicate_slots(ctx, slot_mapping, T, static_cast<hipStream_t>(stream));
     if (ctx->log_calls) std::fprintf(stderr, "ppd: kv_land T=%lld layers=%d\n", (long long)T, (int)num_layers);
     return PPD_OK;
 }

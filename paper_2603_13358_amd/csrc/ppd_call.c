@@ -7,7 +7,7 @@
 #include <Python.h>
 #include <stdint.h>
 
-static PyObject *s_data_ptr, *s_value, *s_shape, *s_dtype, *s_torch, *s_is_contiguous, *s_num_kv_heads;
+static PyObject *s_data_ptr, *s_value, *s_shape, *s_stride, *s_dtype, *s_torch, *s_is_contiguous, *s_num_q_heads, *s_num_kv_heads, *s_head_dim;
 static PyObject *t_void_p, *f_cast;  // ctypes.c_void_p and ctypes.cast
 
 // What a ctypes parameter of type c_void_p takes: None, an int and a c_void_p (a context's handle) here, anything else --
@@ -75,6 +75,7 @@ static int to_int32(PyObject* o, const char* name, int32_t* out, PyObject** why)
 // type objects once torch has been found.
 typedef struct { const char* names[2]; PyObject* types[2]; } elem_types;
 static elem_types t_float32 = {{"float32", "float32"}, {NULL, NULL}}, t_int32 = {{"int32", "int32"}, {NULL, NULL}}, t_mask = {{"int64", "uint64"}, {NULL, NULL}};
+static elem_types t_bf16 = {{"bfloat16", "int16"}, {NULL, NULL}}, t_int64 = {{"int64", "int64"}, {NULL, NULL}};
 static int has_elements(PyObject* o, const char* name, elem_types* t, PyObject** why) {
     if (o == Py_None || PyLong_Check(o)) return 1;
     if (!t->types[1]) {
@@ -94,17 +95,18 @@ static int has_elements(PyObject* o, const char* name, elem_types* t, PyObject**
     if (!ok) *why = PyUnicode_FromFormat("%s has to be of type %s", name, t->names[0]);
     return ok;
 }
-// KV heads of the context behind a handle that ppd_create of the binding has made; 0 for another one
-static int64_t heads_of(PyObject* ctx) {
-    int64_t heads = 0;
-    PyObject* v = PyObject_GetAttr(ctx, s_num_kv_heads);
-    if (!v || !to_int(v, &heads)) {
+// What a handle that ppd_create of the binding has made says of its context's shape; 0 for another one
+static int64_t shape_of(PyObject* ctx, PyObject* name) {
+    int64_t value = 0;
+    PyObject* v = PyObject_GetAttr(ctx, name);
+    if (!v || !to_int(v, &value)) {
         PyErr_Clear();
-        heads = 0;
+        value = 0;
     }
     Py_XDECREF(v);
-    return heads;
+    return value;
 }
+static int64_t heads_of(PyObject* ctx) { return shape_of(ctx, s_num_kv_heads); }
 // The stride of a tensor's rows: as given, or the last axis of a contiguous tensor of `outer` rows (at least; exactly, where further ones are
 // addressed behind these) for each of `heads` KV heads (0: not known).
 static int row_stride(PyObject* o, PyObject* stride, const char* name, int64_t outer, int64_t heads, int exact, int64_t* out, PyObject** why) {
@@ -144,6 +146,79 @@ static int row_stride32(PyObject* o, PyObject* stride, const char* name, const c
     if (!row_stride(o, stride, name, outer, 0, 0, &wide, why)) return 0;
     *out = wide <= INT32_MAX ? (int32_t)wide : INT32_MAX;
     return 1;
+}
+// A tensor [rows][heads][dim] whose heads lie side by side: its row stride (as given, or the tensor's), and its heads.  It has to have `rows` rows at
+// least, and *heads heads of `dim` elements where these are known (not 0).  An address needs its stride given.
+static int head_rows(PyObject* o, PyObject* given, const char* name, int64_t rows, int64_t dim, int64_t* heads, int64_t* stride, PyObject** why) {
+    if (o == Py_None || PyLong_Check(o)) {
+        *stride = 0;
+        if (given != Py_None) return to_int(given, stride);
+        if (o == Py_None || rows <= 1) return 1;
+        *why = PyUnicode_FromFormat("%s is an address: its stride has to be given", name);
+        return 0;
+    }
+    if (!has_elements(o, name, &t_bf16, why)) return 0;
+    int64_t shape[3], strides[3];
+    PyObject* s = PyObject_GetAttr(o, s_shape);
+    PyObject* t = s ? PyObject_CallMethodNoArgs(o, s_stride) : NULL;
+    int ok = s && t;
+    if (ok && (!PyTuple_Check(s) || !PyTuple_Check(t) || PyTuple_GET_SIZE(s) != 3 || PyTuple_GET_SIZE(t) != 3)) {
+        *why = PyUnicode_FromFormat("%s has to have three axes: rows, heads, elements", name);
+        ok = 0;
+    }
+    for (int i = 0; ok && i < 3; ++i) {
+        shape[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(s, i));
+        strides[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
+        ok = !PyErr_Occurred();
+    }
+    Py_XDECREF(t);
+    Py_XDECREF(s);
+    if (!ok) return 0;
+    if (shape[0] < rows || (*heads > 0 && shape[1] != *heads) || (dim > 0 && shape[2] != dim)) {
+        *why = PyUnicode_FromFormat("%s is [%lld][%lld][%lld], the call needs %lld rows of %lld heads of %lld (0: any)", name, (long long)shape[0],
+                                    (long long)shape[1], (long long)shape[2], (long long)rows, (long long)*heads, (long long)dim);
+        return 0;
+    }
+    if (strides[2] != 1 || (shape[1] > 1 && strides[1] != shape[2]) || (rows > 1 && given != Py_None)) {
+        *why = strides[2] != 1 || (shape[1] > 1 && strides[1] != shape[2]) ? PyUnicode_FromFormat("the heads of a row of %s have to be contiguous", name)
+                                                                          : PyUnicode_FromFormat("%s is a tensor: its stride is its own", name);
+        return 0;
+    }
+    *heads = shape[1];
+    *stride = strides[0];
+    return 1;
+}
+// The same of a contiguous tensor, or an address
+static int dense_rows(PyObject* o, const char* name, int64_t rows, int64_t dim, int64_t* heads, PyObject** why) {
+    int64_t stride;
+    if (o == Py_None || PyLong_Check(o)) return 1;
+    if (!head_rows(o, Py_None, name, rows, dim, heads, &stride, why)) return 0;
+    PyObject* v = PyObject_CallMethodNoArgs(o, s_is_contiguous);
+    const int dense = v ? PyObject_IsTrue(v) : -1;
+    Py_XDECREF(v);
+    if (dense == 0) *why = PyUnicode_FromFormat("%s has to be contiguous", name);
+    return dense > 0;
+}
+// A contiguous int64 tensor of `rows` elements at least, or an address
+static int int64_vector(PyObject* o, const char* name, int64_t rows, PyObject** why) {
+    int64_t have;
+    if (o == Py_None || PyLong_Check(o)) return 1;
+    if (!has_elements(o, name, &t_int64, why) || !to_int_or_shape(Py_None, o, 0, &have)) return 0;
+    PyObject* v = PyObject_CallMethodNoArgs(o, s_is_contiguous);
+    const int dense = v ? PyObject_IsTrue(v) : -1;
+    Py_XDECREF(v);
+    if (dense < 0) return 0;
+    if (dense && have >= rows) return 1;
+    *why = dense ? PyUnicode_FromFormat("%s has %lld elements, the call needs %lld", name, (long long)have, (long long)rows) : PyUnicode_FromFormat("%s has to be contiguous", name);
+    return 0;
+}
+// `o` as an int, or the length of a tensor's first axis if it is None; an address needs it given
+static int row_count(PyObject* o, PyObject* x, const char* name, int64_t* out, PyObject** why) {
+    if (o == Py_None && (x == Py_None || PyLong_Check(x))) {
+        *why = PyUnicode_FromFormat("%s is an address: T has to be given", name);
+        return 0;
+    }
+    return to_int_or_shape(o, x, 0, out);
 }
 static int expect(Py_ssize_t have, Py_ssize_t want) {
     if (have == want) return 1;
@@ -372,6 +447,59 @@ static PyObject* call_compact(PyObject* self, PyObject* const* a, Py_ssize_t n) 
     return why ? why : result;
 }
 
+typedef int32_t (*rope_fn)(void*, const void*, int64_t, int32_t, const int64_t*, int64_t, int32_t, void*, int64_t, void*);
+typedef int32_t (*append_rotated_fn)(void*, const void*, int64_t, const void*, int64_t, const void*, int64_t, const int64_t*, void*, const int64_t*, int64_t, void*, void*);
+
+// rope(fn, ctx, x, x_stride, heads, positions, T, transpose, out, out_stride, stream) -> status, or, for arguments that cannot be passed on, a message
+static PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *fn, *ctx, *x, *positions, *out, *stream;
+    int64_t T, heads = 0, x_stride, out_stride;
+    int32_t heads32;
+    PyObject* why = NULL;
+    (void)self;
+    if (!expect(n, 11)) return NULL;
+    const int64_t dim = shape_of(a[1], s_head_dim);
+    if (a[4] != Py_None) {
+        if (!to_int32(a[4], "heads", &heads32, &why)) return why;
+        heads = heads32;
+    }
+    const int transpose = PyObject_IsTrue(a[7]);
+    if (transpose >= 0 && to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_count(a[6], a[5], "positions", &T, &why) && int64_vector(a[5], "positions", T, &why) &&
+        head_rows(a[2], a[3], "x", T, dim, &heads, &x_stride, &why) && head_rows(a[8], a[9], "out", T, dim, &heads, &out_stride, &why) &&
+        to_address(a[2], &x) && to_address(a[5], &positions) && to_address(a[8], &out) && to_handle(a[10], &stream)) {
+        int32_t status;
+        Py_BEGIN_ALLOW_THREADS
+        status = ((rope_fn)fn)(ctx, x, x_stride, (int32_t)(heads <= INT32_MAX ? heads : INT32_MAX), (const int64_t*)positions, T, transpose, out, out_stride, stream);
+        Py_END_ALLOW_THREADS
+        return PyLong_FromLong(status);
+    }
+    return why;
+}
+
+// kv_append_rotated(fn, ctx, q, q_stride, k, k_stride, v, v_stride, positions, kv_pages, slot_mapping, T, q_out, stream) -> the same
+static PyObject* call_append_rotated(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *fn, *ctx, *q, *k, *v, *positions, *pages, *slots, *q_out, *stream;
+    int64_t T, q_stride, k_stride, v_stride;
+    PyObject* why = NULL;
+    (void)self;
+    if (!expect(n, 14)) return NULL;
+    const int64_t dim = shape_of(a[1], s_head_dim);
+    int64_t hq = shape_of(a[1], s_num_q_heads), hkv = shape_of(a[1], s_num_kv_heads);
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_count(a[11], a[10], "slot_mapping", &T, &why) && int64_vector(a[10], "slot_mapping", T, &why) &&
+        int64_vector(a[8], "positions", T, &why) && head_rows(a[2], a[3], "q", T, dim, &hq, &q_stride, &why) &&
+        dense_rows(a[12], "q_out", T, dim, &hq, &why) &&
+        head_rows(a[4], a[5], "k", T, dim, &hkv, &k_stride, &why) && head_rows(a[6], a[7], "v", T, dim, &hkv, &v_stride, &why) &&
+        to_address(a[2], &q) && to_address(a[4], &k) && to_address(a[6], &v) && to_address(a[8], &positions) && to_address(a[9], &pages) &&
+        to_address(a[10], &slots) && to_address(a[12], &q_out) && to_handle(a[13], &stream)) {
+        int32_t status;
+        Py_BEGIN_ALLOW_THREADS
+        status = ((append_rotated_fn)fn)(ctx, q, q_stride, k, k_stride, v, v_stride, (const int64_t*)positions, pages, (const int64_t*)slots, T, q_out, stream);
+        Py_END_ALLOW_THREADS
+        return PyLong_FromLong(status);
+    }
+    return why;
+}
+
 static PyMethodDef kMethods[] = {
     {"kv_append", (PyCFunction)(void (*)(void))call_append, METH_FASTCALL, NULL},
     {"kv_land", (PyCFunction)(void (*)(void))call_land, METH_FASTCALL, NULL},
@@ -380,6 +508,8 @@ static PyMethodDef kMethods[] = {
     {"weighted_attention", (PyCFunction)(void (*)(void))call_weighted, METH_FASTCALL, NULL},
     {"kv_select", (PyCFunction)(void (*)(void))call_select, METH_FASTCALL, NULL},
     {"kv_compact", (PyCFunction)(void (*)(void))call_compact, METH_FASTCALL, NULL},
+    {"rope", (PyCFunction)(void (*)(void))call_rope, METH_FASTCALL, NULL},
+    {"kv_append_rotated", (PyCFunction)(void (*)(void))call_append_rotated, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "ppd_call", "Calls of libppd's per-layer entry points.", -1, kMethods, NULL, NULL, NULL, NULL};
@@ -392,11 +522,14 @@ PyMODINIT_FUNC PyInit_ppd_call(void) {
     s_torch = PyUnicode_InternFromString("torch");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_num_kv_heads = PyUnicode_InternFromString("num_kv_heads");
+    s_num_q_heads = PyUnicode_InternFromString("num_q_heads");
+    s_head_dim = PyUnicode_InternFromString("head_dim");
+    s_stride = PyUnicode_InternFromString("stride");
     PyObject* ctypes = PyImport_ImportModule("ctypes");
     if (!ctypes) return NULL;
     t_void_p = PyObject_GetAttrString(ctypes, "c_void_p");
     f_cast = PyObject_GetAttrString(ctypes, "cast");
     Py_DECREF(ctypes);
-    if (!s_data_ptr || !s_value || !s_shape || !s_dtype || !s_torch || !s_is_contiguous || !s_num_kv_heads || !t_void_p || !f_cast) return NULL;
+    if (!s_data_ptr || !s_value || !s_shape || !s_dtype || !s_torch || !s_is_contiguous || !s_num_kv_heads || !s_num_q_heads || !s_head_dim || !s_stride || !t_void_p || !f_cast) return NULL;
     return PyModule_Create(&kModule);
 }

@@ -4,6 +4,8 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <exception>
+#include <new>
 #include <string>
 #include <thread>
 #include <utility>
@@ -76,11 +78,22 @@ struct ppd_ctx {
     // drafting and eviction (ppd_ops_api.hip): their plan and workspace, made by the first call that needs one
     void* tree = nullptr;
     void (*free_tree)(void*) = nullptr;
+    // positions and shared prefixes: the rotation (ppd_set_rope; rotary_dim 0: none yet), and the plan and workspace of prefix attention
+    ppd::Rotation rotation = {};
+    void* prefix = nullptr;
+    void (*free_prefix)(void*) = nullptr;
 };
+
+namespace ppd {
+inline thread_local std::string g_create_error;  // message of the last failing call that has no context
+
+// PPD_DEBUG_SLOTS=1: looks for duplicate slots among the T slots of an append (error flag bit 2), on `stream`.
+void check_duplicate_slots(ppd_ctx* ctx, const int64_t* slot_mapping, int64_t T, hipStream_t stream);
+}  // namespace ppd
 
 namespace {
 
-thread_local std::string g_create_error;
+using ppd::g_create_error;
 
 ppd_status fail(ppd_ctx* ctx, ppd_status st, const std::string& msg) {
     if (ctx) ctx->error = msg; else g_create_error = msg;
@@ -98,7 +111,7 @@ ppd_status hip_fail(ppd_ctx* ctx, hipError_t e, const char* what) {
     } while (0)
 
 // Grows a device buffer (contents are not kept).  Waits for the stream first: the old buffer may be in use.
-ppd_status grow_device(ppd_ctx* ctx, void** ptr, size_t* have, size_t need, hipStream_t st) {
+inline ppd_status grow_device(ppd_ctx* ctx, void** ptr, size_t* have, size_t need, hipStream_t st) {
     if (need <= *have) return PPD_OK;
     PPD_HIP(ctx, hipStreamSynchronize(st));
     if (*ptr) PPD_HIP(ctx, hipFree(*ptr));
@@ -150,6 +163,63 @@ void wait_staging_read(const Staging& sg) {
         if (spins < 1 << 10) ++spins;
         else std::this_thread::yield();
     }
+}
+
+// A context serves one stream at a time: what the call before enqueued on another one has to finish first.
+inline ppd_status follow_stream(ppd_ctx* ctx, hipStream_t hs) {
+    if (ctx->have_plan_stream && ctx->plan_stream != hs) PPD_HIP(ctx, hipStreamSynchronize(ctx->plan_stream));
+    ctx->plan_stream = hs;
+    ctx->have_plan_stream = true;
+    return PPD_OK;
+}
+
+// Nothing may leave a C entry point but a status.
+template <class F>
+ppd_status guarded(ppd_ctx* ctx, F f) {
+    try {
+        return f();
+    } catch (const std::bad_alloc&) {
+        return ctx ? fail(ctx, PPD_ERR_WORKSPACE, "out of host memory") : PPD_ERR_WORKSPACE;
+    } catch (const std::exception& e) {
+        return ctx ? fail(ctx, PPD_ERR_WORKSPACE, e.what()) : PPD_ERR_WORKSPACE;
+    }
+}
+
+// The next of a ring of staging buffers, free and with room for `bytes`.
+inline ppd_status next_staging(ppd_ctx* ctx, Staging* ring, int* next, size_t bytes, Staging** out) {
+    Staging& sg = ring[*next];
+    wait_staging_read(sg);
+    *next = (*next + 1) % kStagingSlots;
+    if (sg.bytes < bytes) {
+        if (sg.host) PPD_HIP(ctx, hipHostFree(sg.host));
+        sg.host = nullptr;
+        sg.bytes = 0;
+        const size_t want = bytes + bytes / 4 + 4096;
+        if (hipHostMalloc(&sg.host, want, kStagingFlags) != hipSuccess) {
+            (void)hipGetLastError();
+            sg.host = nullptr;
+            return fail(ctx, PPD_ERR_WORKSPACE, "pinned staging allocation failed");
+        }
+        sg.bytes = want;
+    }
+    *out = &sg;
+    return PPD_OK;
+}
+
+// Enqueues the upload of a staged plan of `bytes`, a multiple of 16.
+inline ppd_status enqueue_upload(ppd_ctx* ctx, Staging& sg, void* to, size_t bytes, hipStream_t hs) {
+    const uint4* src = static_cast<const uint4*>(sg.host);
+    uint4* dst = static_cast<uint4*>(to);
+    int64_t granules = (int64_t)(bytes / 16);
+    uint32_t serial = ++sg.serial;
+    void* args[] = {&src, &dst, &granules, &ctx->d_counters, &sg.read, &serial};
+    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&ppd_upload_kernel),
+                                         dim3((unsigned)((granules + kUploadThreads - 1) / kUploadThreads)), dim3(kUploadThreads), args, 0, hs);
+    if (e != hipSuccess) {
+        sg.serial -= 1;  // nothing was enqueued: the buffer is free
+        return hip_fail(ctx, e, "launch plan upload");
+    }
+    return PPD_OK;
 }
 
 }  // namespace

@@ -82,6 +82,16 @@ constexpr int kCursorStride = 32;  // words between cursors
 constexpr int kCounterWords = kCursorBase + kCursors * kCursorStride;
 constexpr int kMergeCols = 16;     // columns of a merge group one block of the merge kernel takes
 
+// The rotation of queries and keys by their positions (ppd_set_rope).  Angles are counted in turns: pair i advances by turns[i] / 2^64
+// of one per position.
+constexpr int kMaxPairs = 64;
+struct Rotation {
+    uint64_t turns[kMaxPairs];
+    int32_t rotary_dim;   // elements of a head that are rotated: pairs 0 .. rotary_dim / 2 - 1; 0: no rotation is set
+    int32_t interleaved;  // pair i is elements (2i, 2i + 1); otherwise (i, i + rotary_dim / 2)
+    float amplitude;
+};
+
 // One merge group: a row block whose key range was split over `nsplit` tiles with consecutive partials.
 struct MergeGroup {
     int32_t grow0;

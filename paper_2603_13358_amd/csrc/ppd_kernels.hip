@@ -11,6 +11,7 @@
 
 #include <type_traits>
 
+#include "ppd_append.h"
 #include "ppd_device.h"
 #include "ppd_internal.h"
 #include "ppd_ops.h"
@@ -40,28 +41,6 @@ __device__ __forceinline__ int64_t checked_page(const KParams& P, int page) {
         page = 0;
     }
     return page;
-}
-
-// Clamp to the code's range with the NaN-propagating minimum and maximum: magnitudes from 448 on (infinities included)
-// become 448, a NaN stays one.
-__device__ __forceinline__ float e4m3_clamp(float y) {
-    return __builtin_elementwise_minimum(__builtin_elementwise_maximum(y, -448.0f), 448.0f);
-}
-__device__ __forceinline__ float bf16_bits_to_f32(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
-
-// Codes of x * inv for the four bf16 of two dwords, in order: one binary32 product each, clamped, then the conversion
-// instruction (two values each; nearest, ties to the even code; a clamped value cannot overflow).  Its treatment of
-// ties and subnormals is what the definition asks for -- the tests compare every bf16 bit pattern with the oracle.
-// 5 vector instructions per element; the same decision in integer arithmetic on the bits took ~25 and bound the
-// append of FP8 pages (landing of 5589 tokens x 32 layers: 314 us, now 255).
-__device__ __forceinline__ uint32_t e4m3_codes(uint32_t lo, uint32_t hi, float inv) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_clamp(bf16_bits_to_f32(lo & 0xFFFFu) * inv),
-                                            e4m3_clamp(__builtin_bit_cast(float, lo & 0xFFFF0000u) * inv), 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_clamp(bf16_bits_to_f32(hi & 0xFFFFu) * inv),
-                                        e4m3_clamp(__builtin_bit_cast(float, hi & 0xFFFF0000u) * inv), w, true);
-    // the instruction gives every NaN the same sign: the codes take theirs from the inputs (inv > 0)
-    const uint32_t signs = __builtin_amdgcn_perm(hi, lo, 0x07050301u);  // the upper byte of each bf16
-    return ((uint32_t)w & 0x7F7F7F7Fu) | (signs & 0x80808080u);
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -1954,10 +1933,6 @@ __global__ __launch_bounds__(kSmallThreads) void ppd_merge_kernel(const MergePar
 // 32 layers 260 -> 232 us (5.8 TB/s read + write; a plain copy of the same bytes 4.9-5.2), FP8 pages 301 -> 180 us (5.6 TB/s),
 // 11188 tokens of first prompts 32 -> 26 us, 3900 of append-prefills 13.8 -> 10.8 us, 256 decodes 8.8 -> 7.0 us.
 // ---------------------------------------------------------------------------------------------------
-// source and pool are each touched once: non-temporal loads and stores (the landing of a whole request runs 7 %
-// faster with them)
-#define APPEND_LOAD(p) __builtin_nontemporal_load(p)
-#define APPEND_STORE(v, p) __builtin_nontemporal_store(v, p)
 // FP8: the pool's elements are bytes; element x of K is stored as the code of x * inv_k (of V: x * inv_v), one
 // binary32 product each.
 template <int D, int TOK, bool FP8>
@@ -1982,7 +1957,6 @@ __global__ __launch_bounds__(kSmallThreads) void ppd_kv_append_kernel(const uint
     v += (int64_t)blockIdx.z * T * HD + blockIdx.y * D;
     pool += (int64_t)blockIdx.z * pool_layer_stride;
     const int tid = threadIdx.x;
-    const int lane = tid & 63;
     const int64_t t0 = (int64_t)blockIdx.x * TOK;
     u32x4 val[LOADS];
 #pragma unroll
@@ -1992,34 +1966,9 @@ __global__ __launch_bounds__(kSmallThreads) void ppd_kv_append_kernel(const uint
         if (u < 2 * UNITS && t0 + row < T)
             val[p] = APPEND_LOAD(reinterpret_cast<const u32x4*>((u < UNITS ? k : v) + (t0 + row) * HD + (u % GR) * 8));
     }
-    // Window of slots: batch tokens t0-7 .. t0+TOK+6, one per lane (lane 7 holds token t0), in every wave; tokens
-    // outside the batch and slots outside the pool count as skipped.  What follows is a handful of wave-wide
-    // votes: the per-workgroup bookkeeping has to stay far below the cost of moving the tokens.
-    constexpr int kWin = TOK + 14;
-    constexpr uint32_t kOwn = (1u << TOK) - 1;
-    const int64_t tw = t0 - 7 + lane;
-    int64_t ws = -1;
-    if (lane < kWin && tw >= 0 && tw < T) ws = slots[tw];
-    const bool outside = ws >= num_pages * kPage;
-    if (__ballot(outside && lane >= 7 && lane < 7 + TOK) != 0 && tid == 0 && blockIdx.y == 0 && blockIdx.z == 0)
-        atomicOr(err_flags, 1u);
-    if (outside) ws = -1;
-    // bit i of `runs`: entry i+1 holds the slot after entry i's; bit c of `octets`: the 8 tokens from entry c on
-    // sit in the 8 slots of one V granule, in order
-    const int64_t ws_next = __shfl_down(ws, 1);
-    const uint64_t runs = __ballot(lane < kWin - 1 && ws_next == ws + 1);
-    const uint64_t starts = __ballot(ws >= 0 && (ws & 7) == 0);
-    const uint32_t octets = (uint32_t)(starts & runs & (runs >> 1) & (runs >> 2) & (runs >> 3) & (runs >> 4) &
-                                       (runs >> 5) & (runs >> 6)) & ((1u << (TOK + 7)) - 1);
-    // own tokens: which of them no octet covers (a token with slot s would be entry s % 8 of one), and the
-    // octets that start at one of them
-    const int my_start = (ws >= 0 && lane >= 7) ? lane - (int)(ws & 7) : 0;
-    const uint32_t single =
-        (uint32_t)(__ballot(lane >= 7 && lane < 7 + TOK && ws >= 0 && !((octets >> my_start) & 1u)) >> 7) & kOwn;
-    const uint32_t own_octets = (octets >> 7) & kOwn;  // at most TOK / 8
-    // rows beyond the own ones that the last octet reaches into
-    const int last_oct = own_octets ? 31 - __builtin_clz(own_octets) : 0;
-    const int extra = own_octets && last_oct + 8 > TOK ? last_oct + 8 - TOK : 0;
+    const AppendWindow w = append_window<TOK>(slots, t0, T, num_pages, blockIdx.y == 0 && blockIdx.z == 0, err_flags);
+    const int64_t ws = w.slot;
+    const int extra = w.extra;
     if (tid < extra * GR)
         *reinterpret_cast<u32x4*>(sv + (TOK + tid / GR) * ROW + (tid % GR) * 8) =
             APPEND_LOAD(reinterpret_cast<const u32x4*>(v + (t0 + TOK + tid / GR) * HD + (tid % GR) * 8));
@@ -2050,42 +1999,7 @@ __global__ __launch_bounds__(kSmallThreads) void ppd_kv_append_kernel(const uint
             APPEND_STORE(g, reinterpret_cast<u32x4*>(dst));
         }
     }
-    // V, whole granules: work unit = (octet, d)
-    uint32_t left = own_octets;
-#pragma unroll
-    for (int o = 0; o < TOK / 8; ++o) {
-        if (!left) break;
-        const int tok = __builtin_ctz(left);
-        left &= left - 1;
-        const int64_t s = __shfl(ws, 7 + tok);
-        // the octets take turns at starting with the first thread, so that at D < 256 each has threads of its own
-        const int d = (tid + o * D) % kSmallThreads;
-        if (d < D) {
-            uint32_t g[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                g[e] = (uint32_t)sv[(tok + 2 * e) * ROW + d] | ((uint32_t)sv[(tok + 2 * e + 1) * ROW + d] << 16);
-            auto* dst = pool + (s >> 4) * S + voff + (int)((s & 15) >> 3) * (D * 8) + d * 8;
-            if constexpr (FP8) {
-                const u32x2 codes = {e4m3_codes(g[0], g[1], inv_v), e4m3_codes(g[2], g[3], inv_v)};
-                APPEND_STORE(codes, reinterpret_cast<u32x2*>(dst));
-            } else {
-                APPEND_STORE((u32x4{g[0], g[1], g[2], g[3]}), reinterpret_cast<u32x4*>(dst));
-            }
-        }
-    }
-    // V, element by element: work unit = (token, d)
-    if (single) {
-        for (int u = tid; u < D * TOK; u += kSmallThreads) {
-            const int tok = u / D, d = u % D;
-            const int64_t s = __shfl(ws, 7 + tok);  // before any lane drops out
-            if (!((single >> tok) & 1u)) continue;
-            const int off = (int)(s & 15);
-            const uint16_t x = sv[tok * ROW + d];
-            auto* dst = pool + (s >> 4) * S + voff + (off >> 3) * (D * 8) + d * 8 + (off & 7);
-            if constexpr (FP8) *dst = (uint8_t)e4m3_codes(x, 0u, inv_v); else *dst = x;
-        }
-    }
+    store_v<D, TOK, FP8>(w, sv, ROW, pool + voff, S, inv_v);
 }
 
 // Tree and weighted attention of more than kTreeCols query columns: a workgroup to a row block (tree tiles of fewer columns are

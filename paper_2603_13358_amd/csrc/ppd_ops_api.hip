@@ -76,14 +76,6 @@ ppd_status tree_state(ppd_ctx* ctx, TreeState** out) {
     return PPD_OK;
 }
 
-// A context serves one stream at a time: what the call before enqueued on another one has to finish first.
-ppd_status follow_stream(ppd_ctx* ctx, hipStream_t hs) {
-    if (ctx->have_plan_stream && ctx->plan_stream != hs) PPD_HIP(ctx, hipStreamSynchronize(ctx->plan_stream));
-    ctx->plan_stream = hs;
-    ctx->have_plan_stream = true;
-    return PPD_OK;
-}
-
 template <class T>
 size_t bytes_of(const std::vector<T>& v) { return v.size() * sizeof(T); }
 
@@ -96,22 +88,10 @@ ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, TreeSlot* slot, const in
     const size_t items = bytes_of(plan.items), blocks = bytes_of(plan.blocks), groups = bytes_of(plan.groups);
     const size_t weighs = bytes_of(plan.weighs), score_weighs = bytes_of(plan.score_weighs);
     const size_t total = items + blocks + groups + weighs + score_weighs, upload = (total + 15) / 16 * 16;
-    Staging& sg = t->staging[t->next_slot];
-    wait_staging_read(sg);
-    t->next_slot = (t->next_slot + 1) % kStagingSlots;
-    if (sg.bytes < upload) {
-        if (sg.host) PPD_HIP(ctx, hipHostFree(sg.host));
-        sg.host = nullptr;
-        sg.bytes = 0;
-        const size_t want = upload + upload / 4 + 4096;
-        if (hipHostMalloc(&sg.host, want, kStagingFlags) != hipSuccess) {
-            (void)hipGetLastError();
-            sg.host = nullptr;
-            return fail(ctx, PPD_ERR_WORKSPACE, "pinned staging allocation failed");
-        }
-        sg.bytes = want;
-    }
-    ppd_status st = grow_device(ctx, &slot->d_plan, &slot->d_plan_bytes, upload, hs);
+    Staging* sg = nullptr;
+    ppd_status st = next_staging(ctx, t->staging, &t->next_slot, upload, &sg);
+    if (st != PPD_OK) return st;
+    st = grow_device(ctx, &slot->d_plan, &slot->d_plan_bytes, upload, hs);
     if (st == PPD_OK) st = grow_device(ctx, &t->d_partials, &t->d_partials_bytes, (size_t)plan.partial_floats * sizeof(float), hs);
     if (st == PPD_OK && weighted) st = grow_device(ctx, &t->d_stats, &t->d_stats_bytes, (size_t)plan.rows * ctx->shape.num_q_heads * 2 * sizeof(float), hs);
     if (st == PPD_OK) st = grow_device(ctx, &t->d_scores, &t->d_scores_bytes, (size_t)plan.score_floats * sizeof(float), hs);
@@ -120,24 +100,15 @@ ppd_status upload_tree_plan(ppd_ctx* ctx, TreeState* t, TreeSlot* slot, const in
             for (auto& s : kind) s.on_device = false;
         return st;
     }
-    char* host = static_cast<char*>(sg.host);
+    char* host = static_cast<char*>(sg->host);
     if (items) std::memcpy(host, plan.items.data(), items);
     if (blocks) std::memcpy(host + items, plan.blocks.data(), blocks);
     if (groups) std::memcpy(host + items + blocks, plan.groups.data(), groups);
     if (weighs) std::memcpy(host + items + blocks + groups, plan.weighs.data(), weighs);
     if (score_weighs) std::memcpy(host + items + blocks + groups + weighs, plan.score_weighs.data(), score_weighs);
     std::memset(host + total, 0, upload - total);
-    const uint4* src = reinterpret_cast<const uint4*>(host);
-    uint4* dst = static_cast<uint4*>(slot->d_plan);
-    int64_t granules = (int64_t)(upload / 16);
-    uint32_t serial = ++sg.serial;
-    void* args[] = {&src, &dst, &granules, &ctx->d_counters, &sg.read, &serial};
-    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&ppd_upload_kernel),
-                                         dim3((unsigned)((granules + kUploadThreads - 1) / kUploadThreads)), dim3(kUploadThreads), args, 0, hs);
-    if (e != hipSuccess) {
-        sg.serial -= 1;  // nothing was enqueued: the buffer is free
-        return hip_fail(ctx, e, "launch plan upload");
-    }
+    st = enqueue_upload(ctx, *sg, slot->d_plan, upload, hs);
+    if (st != PPD_OK) return st;
     slot->L.assign(L, L + B);
     slot->n.assign(n, n + B);
     slot->on_device = true;
@@ -271,18 +242,6 @@ ppd_status tree_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pages
         std::fprintf(stderr, "ppd: %s_attention%s B=%d tiles=%d row blocks=%d joined groups=%d plan=%s\n", weighted ? "weighted" : "tree", ctx->fp8_pages ? " (FP8 pages)" : "",
                      (int)B, (int)p.n_items, (int)plan.blocks.size(), (int)p.n_groups, reuse ? "reused" : "built");
     return PPD_OK;
-}
-
-// Nothing may leave a C entry point but a status.
-template <class F>
-ppd_status guarded(ppd_ctx* ctx, F f) {
-    try {
-        return f();
-    } catch (const std::bad_alloc&) {
-        return ctx ? fail(ctx, PPD_ERR_WORKSPACE, "out of host memory") : PPD_ERR_WORKSPACE;
-    } catch (const std::exception& e) {
-        return ctx ? fail(ctx, PPD_ERR_WORKSPACE, e.what()) : PPD_ERR_WORKSPACE;
-    }
 }
 
 // Rows of more than one chunk leave histograms and candidates in the workspace between their launches.

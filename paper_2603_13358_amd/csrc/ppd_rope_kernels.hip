@@ -1,0 +1,290 @@
+// gfx950 kernels of the rotation by positions.
+//
+//   (a, b) -> A (a cos t - b sin t, b cos t + a sin t),   t = position * frequency of the pair
+//
+// The angle is an integer: a frequency is a fraction of a turn in units of 2^-64, so position * frequency modulo 2^64 is the angle
+// without its whole turns, off by position * 2^-65 turns at most, for every 64-bit position.  Its upper 32 bits become a binary32
+// fraction of a turn in [-1/2, 1/2), which is what the sine and cosine instructions take.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "ppd_append.h"
+#include "ppd_rope.h"
+
+namespace ppd {
+
+namespace {
+
+// Where pair i of a head is: elements (i, i + rotary_dim / 2) with whole granules of 8 on both sides, or without, or (2i, 2i + 1).
+// What is not rotated counts as pairs (2i, 2i + 1) behind.
+enum Layout { HALF, HALF_ODD, INTERLEAVED };
+
+// 8 pairs of a head, as they lie in memory: two granules (HALF, INTERLEAVED), or first and second elements (HALF_ODD).
+struct Unit {
+    u32x4 g[2];
+};
+
+template <Layout LAYOUT>
+__device__ __forceinline__ int granule_of(int unit, int which, int rotary_dim) {
+    const int rotated = rotary_dim / 16;
+    if (LAYOUT == HALF && unit < rotated) return unit + which * rotated;
+    return 2 * unit + which;
+}
+__device__ __forceinline__ int element_of(int pair, int which, int rotary_dim) {
+    return pair < rotary_dim / 2 ? pair + which * (rotary_dim / 2) : 2 * pair + which;
+}
+
+template <Layout LAYOUT>
+__device__ __forceinline__ Unit load_unit(const uint16_t* head, int unit, int rotary_dim) {
+    Unit x;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        if constexpr (LAYOUT == HALF_ODD) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x.g[w][e] = (uint32_t)head[element_of(unit * 8 + 2 * e, w, rotary_dim)] | ((uint32_t)head[element_of(unit * 8 + 2 * e + 1, w, rotary_dim)] << 16);
+        } else {
+            x.g[w] = APPEND_LOAD(reinterpret_cast<const u32x4*>(head + granule_of<LAYOUT>(unit, w, rotary_dim) * 8));
+        }
+    }
+    return x;
+}
+
+__device__ __forceinline__ float element(const u32x4& g, int e) {
+    return e & 1 ? __builtin_bit_cast(float, g[e >> 1] & 0xFFFF0000u) : bf16_bits_to_f32(g[e >> 1] & 0xFFFFu);
+}
+
+// The unit's 16 elements after the rotation, in binary32, where they lie in x.  What is not rotated is x itself: infinities there
+// meet no sine.
+struct Rotated {
+    float v[2][8];
+};
+template <int D, Layout LAYOUT>
+__device__ __forceinline__ Rotated rotate(const Unit& x, int unit, int rotary_dim, const f32x4* table) {
+    constexpr int UNITS = D / 16;
+    Rotated y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const f32x4 cs = table[j * UNITS + unit];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int p = 2 * j + k;  // of the unit's 8 pairs
+            const int w0 = LAYOUT == INTERLEAVED ? p / 4 : 0, e0 = LAYOUT == INTERLEAVED ? p % 4 * 2 : p;
+            const int w1 = LAYOUT == INTERLEAVED ? p / 4 : 1, e1 = LAYOUT == INTERLEAVED ? p % 4 * 2 + 1 : p;
+            const float a = element(x.g[w0], e0), b = element(x.g[w1], e1), c = cs[2 * k], s = cs[2 * k + 1];
+            const bool turns = unit * 8 + p < rotary_dim / 2;
+            y.v[w0][e0] = turns ? __builtin_fmaf(a, c, -(b * s)) : a;
+            y.v[w1][e1] = turns ? __builtin_fmaf(b, c, a * s) : b;
+        }
+    }
+    return y;
+}
+// The same rounded to bf16; what is not rotated keeps its bits.
+template <int D, Layout LAYOUT>
+__device__ __forceinline__ Unit rotate_bf16(const Unit& x, int unit, int rotary_dim, const f32x4* table) {
+    const Rotated y = rotate<D, LAYOUT>(x, unit, rotary_dim, table);
+    Unit z;
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t both = pack_bf16(y.v[w][2 * i], y.v[w][2 * i + 1]);
+            if constexpr (LAYOUT == INTERLEAVED) {
+                z.g[w][i] = unit * 8 + w * 4 + i < rotary_dim / 2 ? both : x.g[w][i];
+            } else {
+                const uint32_t mask = (unit * 8 + 2 * i < rotary_dim / 2 ? 0x0000FFFFu : 0u) | (unit * 8 + 2 * i + 1 < rotary_dim / 2 ? 0xFFFF0000u : 0u);
+                z.g[w][i] = (both & mask) | (x.g[w][i] & ~mask);
+            }
+        }
+    return z;
+}
+
+// element `which`, e of the unit, as a place in its head
+template <Layout LAYOUT>
+__device__ __forceinline__ void store_unit(uint16_t* head, const Unit& x, int unit, int rotary_dim) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        if constexpr (LAYOUT == HALF_ODD) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) head[element_of(unit * 8 + e, w, rotary_dim)] = (uint16_t)(x.g[w][e >> 1] >> ((e & 1) * 16));
+        } else {
+            *reinterpret_cast<u32x4*>(head + granule_of<LAYOUT>(unit, w, rotary_dim) * 8) = x.g[w];
+        }
+    }
+}
+
+// Cosines and sines of TOK rows from t0 on, times the amplitude, to LDS: table[row][j][unit] has pairs 2j and 2j + 1 of the unit, so that
+// neighbouring units' reads of 16 bytes lie side by side.  Rows behind the last have the last's.
+template <int D, int TOK>
+__device__ __forceinline__ void fill_table(const Rotation& rot, const int64_t* positions, int64_t t0, int64_t T, float sin_sign, f32x4* table) {
+    constexpr int PAIRS = D / 2, UNITS = D / 16;
+    for (int i = threadIdx.x; i < TOK * PAIRS; i += kSmallThreads) {
+        const int row = i / PAIRS, pair = i % PAIRS;
+        if (pair >= rot.rotary_dim / 2) continue;
+        const uint64_t angle = (uint64_t)positions[t0 + row < T ? t0 + row : T - 1] * rot.turns[pair];
+        const float turn = (float)(int32_t)(angle >> 32) * 0x1p-32f;
+        reinterpret_cast<f32x2*>(table)[((row * 4 + pair % 8 / 2) * UNITS + pair / 8) * 2 + pair % 2] =
+            f32x2{__builtin_amdgcn_cosf(turn) * rot.amplitude, __builtin_amdgcn_sinf(turn) * (rot.amplitude * sin_sign)};
+    }
+}
+
+constexpr int kRopeTokens = 4;
+
+}  // namespace
+
+template <int D, Layout LAYOUT>
+__global__ __launch_bounds__(kSmallThreads) void ppd_rope_kernel(const RopeParams P) {
+    constexpr int UNITS = D / 16, TOK = kRopeTokens;
+    __shared__ f32x4 table[TOK * 4 * UNITS];
+    const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    fill_table<D, TOK>(P.rot, P.positions, t0, P.T, P.sin_sign, table);
+    __syncthreads();
+    const int unit = threadIdx.x % UNITS;
+    for (int i = threadIdx.x / UNITS; i < TOK * P.heads; i += kSmallThreads / UNITS) {
+        const int row = i / P.heads, head = i % P.heads;
+        if (t0 + row >= P.T) break;
+        const Unit x = load_unit<LAYOUT>(P.x + (t0 + row) * P.x_stride + head * D, unit, P.rot.rotary_dim);
+        store_unit<LAYOUT>(P.out + (t0 + row) * P.out_stride + head * D, rotate_bf16<D, LAYOUT>(x, unit, P.rot.rotary_dim, table + row * 4 * UNITS), unit, P.rot.rotary_dim);
+    }
+}
+
+// Append of rotated keys, and of values, to the page pool; queries rotated beside.  A workgroup has TOK tokens and one KV head
+// (blockIdx.y < Hkv), whose rows it stages in LDS and writes as ppd_kv_append_kernel does, or kQueryHeads query heads.
+constexpr int kQueryHeads = 4;
+template <int D, int TOK, bool FP8, Layout LAYOUT>
+__global__ __launch_bounds__(kSmallThreads) void ppd_rotated_append_kernel(const RotatedAppendParams P) {
+    using Elem = std::conditional_t<FP8, uint8_t, uint16_t>;
+    constexpr int UNITS = D / 16, GR = D / 8;
+    constexpr int KROW = D + 16 / (int)sizeof(Elem);  // elements of a staged row: 16 bytes of padding spread the rows over the banks
+    constexpr int VROW = D + 8;
+    __shared__ f32x4 table[TOK * 4 * UNITS];
+    __shared__ __attribute__((aligned(16))) Elem sk[TOK * KROW];
+    __shared__ __attribute__((aligned(16))) uint16_t sv[(TOK + 7) * VROW];
+    const int tid = threadIdx.x;
+    const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    const int rotary = P.rot.rotary_dim;
+    if ((int)blockIdx.y >= P.Hkv) {
+        const int head0 = ((int)blockIdx.y - P.Hkv) * kQueryHeads, unit = tid % UNITS;
+        constexpr int STEP = kSmallThreads / UNITS, ROUNDS = (TOK * kQueryHeads + STEP - 1) / STEP;
+        Unit x[ROUNDS];
+        bool there[ROUNDS];
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int i = tid / UNITS + r * STEP, row = i / kQueryHeads, head = head0 + i % kQueryHeads;
+            there[r] = row < TOK && t0 + row < P.T && head < P.Hq;
+            if (there[r]) x[r] = load_unit<LAYOUT>(P.q + (t0 + row) * P.q_stride + head * D, unit, rotary);
+        }
+        fill_table<D, TOK>(P.rot, P.positions, t0, P.T, 1.f, table);
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int i = tid / UNITS + r * STEP, row = i / kQueryHeads, head = head0 + i % kQueryHeads;
+            if (there[r])
+                store_unit<LAYOUT>(P.q_out + ((t0 + row) * P.Hq + head) * D, rotate_bf16<D, LAYOUT>(x[r], unit, rotary, table + row * 4 * UNITS), unit, rotary);
+        }
+        return;
+    }
+    // K: the first threads, 8 pairs each; V: the last ones, a granule each
+    constexpr int KUNITS = TOK * UNITS, VGRANULES = TOK * GR;
+    static_assert(KUNITS <= kSmallThreads && VGRANULES <= kSmallThreads, "a round of loads");
+    const int kh = blockIdx.y, krow = tid / UNITS, unit = tid % UNITS;
+    const int vg = kSmallThreads - 1 - tid, vrow = vg / GR;
+    Unit xk;
+    u32x4 xv = {0, 0, 0, 0};
+    const bool has_k = tid < KUNITS && t0 + krow < P.T, has_v = vg < VGRANULES;
+    if (has_k) xk = load_unit<LAYOUT>(P.k + (t0 + krow) * P.k_stride + kh * D, unit, rotary);
+    if (has_v && t0 + vrow < P.T) xv = APPEND_LOAD(reinterpret_cast<const u32x4*>(P.v + (t0 + vrow) * P.v_stride + kh * D + vg % GR * 8));
+    const AppendWindow w = append_window<TOK>(P.slots, t0, P.T, P.num_pages, blockIdx.y == 0, P.err_flags);
+    if (tid < w.extra * GR)
+        *reinterpret_cast<u32x4*>(sv + (TOK + tid / GR) * VROW + (tid % GR) * 8) =
+            APPEND_LOAD(reinterpret_cast<const u32x4*>(P.v + (t0 + TOK + tid / GR) * P.v_stride + kh * D + (tid % GR) * 8));
+    fill_table<D, TOK>(P.rot, P.positions, t0, P.T, 1.f, table);
+    if (has_v) *reinterpret_cast<u32x4*>(sv + vrow * VROW + vg % GR * 8) = xv;
+    __syncthreads();
+    if (has_k) {
+        Elem* const row = sk + krow * KROW;
+        if constexpr (FP8) {
+            const Rotated y = rotate<D, LAYOUT>(xk, unit, rotary, table + krow * 4 * UNITS);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                u32x2 codes;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) codes[i] = e4m3_codes(y.v[g][4 * i], y.v[g][4 * i + 1], y.v[g][4 * i + 2], y.v[g][4 * i + 3], P.inv_k);
+                if constexpr (LAYOUT == HALF_ODD) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) row[element_of(unit * 8 + e, g, rotary)] = (uint8_t)(codes[e >> 2] >> ((e & 3) * 8));
+                } else {
+                    *reinterpret_cast<u32x2*>(row + granule_of<LAYOUT>(unit, g, rotary) * 8) = codes;
+                }
+            }
+        } else {
+            store_unit<LAYOUT>(row, rotate_bf16<D, LAYOUT>(xk, unit, rotary, table + krow * 4 * UNITS), unit, rotary);
+        }
+    }
+    __syncthreads();
+    const int64_t S = 2LL * P.Hkv * kPage * D;
+    Elem* const to = static_cast<Elem*>(P.pool) + (int64_t)kh * kPage * D;
+    // K: work unit = (granule, token), token fastest; whole waves take part
+#pragma unroll
+    for (int p = 0; p < (TOK * GR + kSmallThreads - 1) / kSmallThreads; ++p) {
+        const int u = tid + p * kSmallThreads;
+        if (u >= TOK * GR) break;
+        const int tok = u % TOK, c = u / TOK;
+        const int64_t s = __shfl(w.slot, 7 + tok);
+        if (s < 0) continue;
+        typedef std::conditional_t<FP8, u32x2, u32x4> Granule;
+        APPEND_STORE(*reinterpret_cast<const Granule*>(sk + tok * KROW + c * 8), reinterpret_cast<Granule*>(to + (s >> 4) * S + c * (kPage * 8) + (int)(s & 15) * 8));
+    }
+    store_v<D, TOK, FP8>(w, sv, VROW, to + (int64_t)P.Hkv * kPage * D, S, P.inv_v);
+}
+
+namespace {
+
+Layout layout_of(const Rotation& rot) { return rot.interleaved ? INTERLEAVED : rot.rotary_dim % 16 == 0 ? HALF : HALF_ODD; }
+
+// Calls `go` with the layout as a constant.
+template <class F>
+void by_layout(const Rotation& rot, F go) {
+    switch (layout_of(rot)) {
+        case HALF: go(std::integral_constant<Layout, HALF>{}); break;
+        case HALF_ODD: go(std::integral_constant<Layout, HALF_ODD>{}); break;
+        case INTERLEAVED: go(std::integral_constant<Layout, INTERLEAVED>{}); break;
+    }
+}
+
+template <int D, int TOK, bool FP8>
+void append_launch(const RotatedAppendParams& p, hipStream_t hs) {
+    const unsigned queries = p.q ? (unsigned)(p.Hq + kQueryHeads - 1) / kQueryHeads : 0u;
+    const dim3 grid((unsigned)((p.T + TOK - 1) / TOK), (unsigned)p.Hkv + queries);
+    by_layout(p.rot, [&](auto layout) { hipLaunchKernelGGL((ppd_rotated_append_kernel<D, TOK, FP8, decltype(layout)::value>), grid, dim3(kSmallThreads), 0, hs, p); });
+}
+
+}  // namespace
+
+int launch_rope(const RopeParams& p, int head_dim, void* stream) {
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    const dim3 grid((unsigned)((p.T + kRopeTokens - 1) / kRopeTokens));
+    by_layout(p.rot, [&](auto layout) {
+        constexpr Layout LAYOUT = decltype(layout)::value;
+        if (head_dim == 128) hipLaunchKernelGGL((ppd_rope_kernel<128, LAYOUT>), grid, dim3(kSmallThreads), 0, hs, p);
+        else hipLaunchKernelGGL((ppd_rope_kernel<64, LAYOUT>), grid, dim3(kSmallThreads), 0, hs, p);
+    });
+    return (int)hipGetLastError();
+}
+
+int launch_rotated_append(const RotatedAppendParams& p, int head_dim, bool fp8_pages, void* stream) {
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    // tokens of a workgroup: as of ppd_kv_append
+    const bool wide = p.T * p.Hkv >= 8192;
+    if (head_dim == 128) {
+        if (wide) fp8_pages ? append_launch<128, 16, true>(p, hs) : append_launch<128, 16, false>(p, hs);
+        else fp8_pages ? append_launch<128, 8, true>(p, hs) : append_launch<128, 8, false>(p, hs);
+    } else {
+        if (wide) fp8_pages ? append_launch<64, 16, true>(p, hs) : append_launch<64, 16, false>(p, hs);
+        else fp8_pages ? append_launch<64, 8, true>(p, hs) : append_launch<64, 8, false>(p, hs);
+    }
+    return (int)hipGetLastError();
+}
+
+}  // namespace ppd
