@@ -351,6 +351,21 @@ ppd_status ppd_kv_append_rotated(ppd_ctx *ctx, const void *q, int64_t q_stride, 
                                  int64_t v_stride, const int64_t *positions, void *kv_pages, const int64_t *slot_mapping, int64_t T,
                                  void *q_out, void *stream);
 
+/* ppd_mixed_attention of a batch whose sequences share leading tokens, each shared range read once for all rows that have it: answers that
+ * are sampled from one prompt, conversations behind one system prompt, next turns over one document.  Sequences are ordered so that
+ * those with more in common are neighbours; what they share may nest (all of them a system prompt, some a document behind it).
+ *   shared        HOST int32 [B]: the tokens 0 .. shared_i - 1 of sequence i lie in the same pages as those of sequence i - 1 (the two
+ *                 rows of page_tables agree there); 0 <= shared_i <= min(L_i, L_{i-1}), shared_0 = 0.  The ids of a shared range are read
+ *                 from the row of the first sequence that has it; sharing is used in steps of 64 tokens
+ *   the rest      as for ppd_mixed_attention; L and n count all tokens of a sequence, shared ones too
+ * The result is that of ppd_mixed_attention but for rounding, bitwise the same from run to run.  A row whose scores are all minus infinity
+ * gives zeros; infinities and NaN of new tokens that a row does not see do not reach it.  As for the other attention calls a plan is
+ * kept while shared, L and n do not change; one that changes under capture is refused, and a captured graph may be replayed until a
+ * call of ppd_prefix_attention on the same context has planned another batch. */
+ppd_status ppd_prefix_attention(ppd_ctx *ctx, const void *q, const void *kv_pages, const int32_t *page_tables,
+                                int32_t max_pages, const int32_t *shared, const int32_t *L, const int32_t *n, int32_t B,
+                                float scale, void *out, void *stream);
+
 /* Statistics of the plan built by the last ppd_mixed_attention call on this context. */
 ppd_status ppd_get_plan_stats(const ppd_ctx *ctx, ppd_plan_stats *stats);
 

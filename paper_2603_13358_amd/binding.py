@@ -12,7 +12,7 @@ _LIB_PATH = os.path.join(_HERE, "libppd.so")
 _CALL_PATH = os.path.join(_HERE, "ppd_call" + sysconfig.get_config_var("EXT_SUFFIX"))  # built for this interpreter's ABI
 _lib = None
 _call = None       # the call module
-_fn_append = _fn_land = _fn_mixed = _fn_mixed_static = _fn_tree = _fn_weighted = _fn_select = _fn_compact = _fn_rope = _fn_append_rotated = None  # addresses of the entry points it calls
+_fn_append = _fn_land = _fn_mixed = _fn_mixed_static = _fn_tree = _fn_weighted = _fn_select = _fn_compact = _fn_rope = _fn_append_rotated = _fn_prefix = None  # addresses of the entry points it calls
 
 STATUS_NAMES = {0: "PPD_OK", -1: "PPD_ERR_NULL", -2: "PPD_ERR_SHAPE", -3: "PPD_ERR_RANGE",
                 -4: "PPD_ERR_PAGETABLE", -5: "PPD_ERR_WORKSPACE", -6: "PPD_ERR_HIP"}
@@ -48,7 +48,7 @@ class PlanStats(ctypes.Structure):
 EXPORTS = ["ppd_create", "ppd_destroy", "ppd_last_error", "ppd_set_option", "ppd_kv_append", "ppd_kv_land",
            "ppd_transfer_delay_s", "ppd_mixed_attention", "ppd_mixed_attention_static",
            "ppd_tree_attention", "ppd_weighted_attention", "ppd_kv_select", "ppd_kv_compact",
-           "ppd_set_rope", "ppd_rope_frequencies", "ppd_rope", "ppd_kv_append_rotated",
+           "ppd_set_rope", "ppd_rope_frequencies", "ppd_rope", "ppd_kv_append_rotated", "ppd_prefix_attention",
            "ppd_get_plan_stats", "ppd_plan_build", "ppd_device_error_flags", "ppd_last_kernel_ms", "ppd_timed_kernels_ms",
            "ppd_route_score", "ppd_route_table_build", "ppd_route_cell", "ppd_route_decide", "ppd_route_decide_batch", "ppd_version"]
 
@@ -59,7 +59,7 @@ def lib_path():
 
 def load_library():
     """Loads libppd.so; raises if it has not been built (no fallback of any kind)."""
-    global _lib, _call, _fn_append, _fn_land, _fn_mixed, _fn_mixed_static, _fn_tree, _fn_weighted, _fn_select, _fn_compact, _fn_rope, _fn_append_rotated
+    global _lib, _call, _fn_append, _fn_land, _fn_mixed, _fn_mixed_static, _fn_tree, _fn_weighted, _fn_select, _fn_compact, _fn_rope, _fn_append_rotated, _fn_prefix
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH) or not os.path.exists(_CALL_PATH):
@@ -88,6 +88,7 @@ def load_library():
     lib.ppd_rope_frequencies.argtypes = [i32, dbl, i32, dbl, dbl, dbl, dbl, vp]
     lib.ppd_rope.argtypes = [vp, vp, i64, i32, vp, i64, i32, vp, i64, vp]
     lib.ppd_kv_append_rotated.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp]
+    lib.ppd_prefix_attention.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, i32, ctypes.c_float, vp, vp]
     lib.ppd_get_plan_stats.argtypes = [vp, ctypes.POINTER(PlanStats)]
     lib.ppd_plan_build.argtypes = [ctypes.POINTER(Shape), vp, vp, i32, i32, i32, i32, i32, i32,
                                    ctypes.POINTER(WorkItem), i64, ctypes.POINTER(PlanStats)]
@@ -112,7 +113,7 @@ def load_library():
         lib.ppd_kv_append, lib.ppd_kv_land, lib.ppd_mixed_attention, lib.ppd_mixed_attention_static))
     _fn_tree, _fn_weighted, _fn_select, _fn_compact = (ctypes.cast(f, vp).value for f in (
         lib.ppd_tree_attention, lib.ppd_weighted_attention, lib.ppd_kv_select, lib.ppd_kv_compact))
-    _fn_rope, _fn_append_rotated = (ctypes.cast(f, vp).value for f in (lib.ppd_rope, lib.ppd_kv_append_rotated))
+    _fn_rope, _fn_append_rotated, _fn_prefix = (ctypes.cast(f, vp).value for f in (lib.ppd_rope, lib.ppd_kv_append_rotated, lib.ppd_prefix_attention))
     _lib = lib
     return lib
 
@@ -314,6 +315,17 @@ def ppd_kv_append_rotated(ctx, q, k, v, positions, kv_pages, slot_mapping, q_out
         _check_call(status, ctx)
 
 
+def ppd_prefix_attention(ctx, q, kv_pages, page_tables, shared, L, n, scale, out, max_pages=None, stream=None):
+    """q, out: bfloat16 [rows][query heads][head_dim], contiguous; shared, L, n: host int32 [sequences]."""
+    if _lib is None:
+        load_library()
+    status = _call.prefix_attention(_fn_prefix, ctx, q, kv_pages, page_tables, max_pages, shared, L, n, scale, out, stream)
+    if status is None:  # lengths in another type, layout or container
+        status = _call.prefix_attention(_fn_prefix, ctx, q, kv_pages, page_tables, max_pages, *_lengths(shared, L, n), scale, out, stream)
+    if status != 0:
+        _check_call(status, ctx)
+
+
 def ppd_get_plan_stats(ctx):
     st = PlanStats()
     _check(load_library().ppd_get_plan_stats(ctx, ctypes.byref(st)), ctx)
@@ -461,6 +473,9 @@ class Context:
 
     def kv_append_rotated(self, q, k, v, positions, kv_pages, slot_mapping, q_out, stream=None):
         ppd_kv_append_rotated(self.handle, q, k, v, positions, kv_pages, slot_mapping, q_out, stream=stream)
+
+    def prefix_attention(self, q, kv_pages, page_tables, shared, L, n, scale, out, stream=None):
+        ppd_prefix_attention(self.handle, q, kv_pages, page_tables, shared, L, n, scale, out, stream=stream)
 
     def plan_stats(self):
         return ppd_get_plan_stats(self.handle)

@@ -11,8 +11,8 @@ CALL = os.path.join(HERE, "ppd_call" + sysconfig.get_config_var("EXT_SUFFIX"))  
 CALL_SOURCE = os.path.join(CSRC, "ppd_call.c")
 SOURCES = ["ppd_api.hip", "ppd_kernels.hip", "ppd_plan.cpp", "ppd_route.cpp",
            "ppd_ops_api.hip", "ppd_tree_kernels.hip", "ppd_cache_kernels.hip", "ppd_tree_plan.cpp",
-           "ppd_rope_api.hip", "ppd_rope_kernels.hip"]
-HEADERS = ["ppd_internal.h", "ppd_context.h", "ppd_device.h", "ppd_ops.h", "ppd_append.h", "ppd_rope.h", os.path.join("..", "..", "include", "ppd.h")]
+           "ppd_rope_api.hip", "ppd_rope_kernels.hip", "ppd_prefix_api.hip", "ppd_prefix_kernels.hip", "ppd_prefix_plan.cpp"]
+HEADERS = ["ppd_internal.h", "ppd_context.h", "ppd_device.h", "ppd_ops.h", "ppd_append.h", "ppd_rope.h", "ppd_prefix.h", os.path.join("..", "..", "include", "ppd.h")]
 
 # Packed-FP32 instructions are switched off for all device code (the host pass does not know the feature
 # and says so; that warning is harmless).

@@ -500,6 +500,49 @@ static PyObject* call_append_rotated(PyObject* self, PyObject* const* a, Py_ssiz
     return why;
 }
 
+typedef int32_t (*prefix_fn)(void*, const void*, const void*, const int32_t*, int32_t, const int32_t*, const int32_t*, const int32_t*, int32_t, float, void*, void*);
+
+// prefix_attention(fn, ctx, q, kv_pages, page_tables, max_pages, shared, L, n, scale, out, stream) -> status, or None if shared, L and n are not plain
+// int32 arrays of one length yet, or, for arguments that cannot be passed on, a message
+static PyObject* call_prefix(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *fn, *ctx, *q, *pages, *tables, *out, *stream;
+    int32_t max_pages;
+    PyObject* why = NULL;
+    Py_buffer shared, L, nn;
+    (void)self;
+    if (!expect(n, 12)) return NULL;
+    if (!int32_arrays(a[7], a[8], &L, &nn)) Py_RETURN_NONE;
+    const int plain = int32_array(a[6], &shared);
+    if (!plain || shared.shape[0] != L.shape[0]) {
+        if (plain) PyBuffer_Release(&shared);
+        PyBuffer_Release(&nn);
+        PyBuffer_Release(&L);
+        Py_RETURN_NONE;
+    }
+    PyObject* result = NULL;
+    PyObject* scale = NULL;
+    const int64_t dim = shape_of(a[1], s_head_dim);
+    int64_t rows = 0, hq = shape_of(a[1], s_num_q_heads);
+    for (Py_ssize_t i = 0; i < nn.shape[0]; ++i) rows += ((const int32_t*)nn.buf)[i];
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_stride32(a[4], a[5], "page_tables", "max_pages", L.shape[0], &max_pages, &why) &&
+        has_elements(a[4], "page_tables", &t_int32, &why) && dense_rows(a[2], "q", rows, dim, &hq, &why) && dense_rows(a[10], "out", rows, dim, &hq, &why) &&
+        to_address(a[2], &q) && to_address(a[3], &pages) && to_address(a[4], &tables) && (scale = PyNumber_Float(a[9])) && to_address(a[10], &out) &&
+        to_handle(a[11], &stream)) {
+        const float s = (float)PyFloat_AS_DOUBLE(scale);
+        int32_t status;
+        Py_BEGIN_ALLOW_THREADS
+        status = ((prefix_fn)fn)(ctx, q, pages, (const int32_t*)tables, max_pages, (const int32_t*)shared.buf, (const int32_t*)L.buf, (const int32_t*)nn.buf,
+                                 (int32_t)L.shape[0], s, out, stream);
+        Py_END_ALLOW_THREADS
+        result = PyLong_FromLong(status);
+    }
+    Py_XDECREF(scale);
+    PyBuffer_Release(&shared);
+    PyBuffer_Release(&nn);
+    PyBuffer_Release(&L);
+    return why ? why : result;
+}
+
 static PyMethodDef kMethods[] = {
     {"kv_append", (PyCFunction)(void (*)(void))call_append, METH_FASTCALL, NULL},
     {"kv_land", (PyCFunction)(void (*)(void))call_land, METH_FASTCALL, NULL},
@@ -509,6 +552,7 @@ static PyMethodDef kMethods[] = {
     {"kv_select", (PyCFunction)(void (*)(void))call_select, METH_FASTCALL, NULL},
     {"kv_compact", (PyCFunction)(void (*)(void))call_compact, METH_FASTCALL, NULL},
     {"rope", (PyCFunction)(void (*)(void))call_rope, METH_FASTCALL, NULL},
+    {"prefix_attention", (PyCFunction)(void (*)(void))call_prefix, METH_FASTCALL, NULL},
     {"kv_append_rotated", (PyCFunction)(void (*)(void))call_append_rotated, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };

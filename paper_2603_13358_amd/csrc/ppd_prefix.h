@@ -1,0 +1,81 @@
+// Internal declarations of attention over shared prefixes.
+#pragma once
+#include <stdint.h>
+
+#include <vector>
+
+#include "ppd_ops.h"
+
+namespace ppd {
+
+constexpr int kSharedStep = kTileTokens;  // sharing is used in steps of this many tokens: the key ranges of row blocks begin at multiples of it
+constexpr int kMinSavedKeys = 256;        // keys that a shared range has to save
+constexpr int kMaxNested = 16;            // shared ranges one behind the other, at most, that a sequence is part of
+constexpr int kPrefixCols = 128;          // query columns of a prefix tile at most: 32 for each wave
+constexpr int kMaxPrefixChunk = kMaxTreeChunk;  // keys of one at most (its page ids are staged in LDS)
+
+// A tile: `ncols` query columns (row-major over the G heads of a group) of consecutive rows against keys [kv_begin, kv_end), which are read
+// by the page table of sequence `seq`.  Row j sees the keys up to L + j (a shared range: all, its L is its end).
+struct PrefixItem {
+    int32_t seq, kvh;
+    int32_t grow0, ncols;
+    int32_t L, kv_total;
+    int32_t kv_begin, kv_end;
+    int64_t part_off;          // floats, of this tile's partial; -1 where the tile has all keys of its rows and writes `out`
+};
+
+// Waves of a tile that have the same columns, each with every waves-th slab of the keys.
+constexpr int prefix_key_waves(int ncols) { return ncols <= 32 ? 4 : ncols <= 64 ? 2 : 1; }
+
+// Partials of some columns: `nsplit` of [ncols][D] sums, then [ncols] (m, l) pairs, one behind the other, and behind these the next KV head's.
+struct JoinSource {
+    int64_t part_off;
+    int32_t ncols, col0;       // col0: where the unit's first column is among them
+    int32_t nsplit, unused;
+};
+
+// Rows whose columns have the same sources.
+struct JoinUnit {
+    int32_t grow0, nrows;
+    int32_t source0, nsources;
+};
+
+struct PrefixPlan {
+    std::vector<PrefixItem> items;
+    std::vector<ppd_work_item> blocks;     // row blocks: columns beyond kPrefixCols
+    std::vector<JoinUnit> units;
+    std::vector<JoinSource> sources;
+    int64_t partial_floats = 0;
+    int32_t join_cols = 0;                 // most columns of a unit
+    int64_t keys_read = 0, keys_alone = 0; // keys per KV head that tiles are over, and without sharing
+};
+
+// Builds the tile list of a prefix attention call, whose arguments the caller has checked (shared[i] of sequence i > 0: tokens it has in
+// common with the one before, at most what either has cached); false if it has more than kMaxTiles tiles.
+bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t* L, const int32_t* n, int32_t B, int num_cus, PrefixPlan* plan);
+
+struct PrefixParams {
+    const uint16_t* q;
+    uint16_t* out;
+    const void* pool;
+    const int32_t* page_tables;
+    const PrefixItem* items;
+    const JoinUnit* units;
+    const JoinSource* sources;
+    float* partials;
+    uint32_t* err_flags;
+    int64_t num_pages;
+    int64_t page_stride;       // elements
+    int32_t max_pages;
+    int32_t Hq, Hkv, G, invG;  // invG = 65536 / G + 1: col / G == (col * invG) >> 16
+    int32_t n_items, n_units;
+    int32_t join_cols;
+    float scale_log2e;         // softmax scale * log2(e), times the K scale of FP8 pages
+    float v_scale;
+};
+
+// Launchers; stream is a hipStream_t, the result a hipError_t.
+int launch_prefix(const PrefixParams& p, int head_dim, bool fp8_pages, void* stream);
+int launch_prefix_join(const PrefixParams& p, int head_dim, void* stream);
+
+}  // namespace ppd

@@ -1,0 +1,178 @@
+// Tile list of attention over shared prefixes: which rows meet which keys in which workgroup, and whose partials make a row's result.
+#include <algorithm>
+
+#include "ppd_prefix.h"
+
+namespace ppd {
+
+namespace {
+
+// A range of keys and the sequences [lo, hi] that have it, in the same pages: a shared one, or a sequence's own end with its new tokens.
+struct Segment {
+    int32_t lo, hi;
+    int32_t begin, end;
+    bool own;
+};
+
+// The shared ranges of sequences [lo, hi] from key `start` on, and their own ends.  common[i] is what sequence i has in common with the one
+// before; the least of them is in common to all, and where it occurs they fall apart.
+class Segments {
+public:
+    Segments(const std::vector<int32_t>& common, const int32_t* L, const int32_t* n) : common_(common), L_(L), n_(n) {}
+    std::vector<Segment> list;
+
+    // Every level shares 64 keys at least.  One that saves too little is left to the sequences below, and then they are fewer than five; with
+    // that and kMaxNested the levels are few.
+    void add(int32_t lo, int32_t hi, int32_t start, int level) {
+        if (lo == hi || level == kMaxNested) {
+            for (int32_t i = lo; i <= hi; ++i) list.push_back({i, i, start, L_[i] + n_[i], true});
+            return;
+        }
+        const int32_t least = *std::min_element(common_.begin() + lo + 1, common_.begin() + hi + 1);
+        if ((int64_t)(hi - lo) * (least - start) >= kMinSavedKeys) {
+            list.push_back({lo, hi, start, least, false});
+            start = least;
+            ++level;
+        }
+        for (int32_t from = lo; from <= hi;) {
+            int32_t to = from;
+            while (to < hi && common_[to + 1] > least) ++to;
+            add(from, to, start, level);
+            from = to + 1;
+        }
+    }
+
+private:
+    const std::vector<int32_t>& common_;
+    const int32_t *L_, *n_;
+};
+
+int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
+
+}  // namespace
+
+bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t* L, const int32_t* n, int32_t B, int num_cus, PrefixPlan* plan) {
+    const int G = s.num_q_heads / s.num_kv_heads, Hkv = s.num_kv_heads, D = s.head_dim;
+    *plan = PrefixPlan();
+    std::vector<int32_t> common(B, 0), row0(B + 1, 0);
+    for (int i = 0; i < B; ++i) {
+        row0[i + 1] = row0[i] + n[i];
+        if (i > 0) common[i] = shared[i] / kSharedStep * kSharedStep;
+        plan->keys_alone += (int64_t)L[i] + n[i];
+    }
+    Segments segments(common, L, n);
+    for (int32_t from = 0; from < B;) {  // what shares nothing stands alone
+        int32_t to = from;
+        while (to + 1 < B && common[to + 1] > 0) ++to;
+        segments.add(from, to, 0, 0);
+        from = to + 1;
+    }
+    const TileKind narrow = {kMaxPrefixChunk * 4, kTreeStep, 256, 256, 0, 2 * num_cus};
+    const TileKind wide = {kMaxTreeBlockChunk, kTileTokens, 350, 500, 0.0114, num_cus};
+    // How a segment is cut: `tiles` column ranges of `rows` rows each, `keys` of time each (a tile whose waves have columns of their own goes
+    // over its keys in one wave's time each).
+    struct Cut { bool is_wide; int32_t tiles, rows, key_waves; };
+    auto rows_of = [&](const Segment& g) { return row0[g.hi + 1] - row0[g.lo]; };
+    bool any_wide = false;
+    for (const Segment& g : segments.list) any_wide |= g.own && (int64_t)rows_of(g) * G > kPrefixCols;
+    auto cut_of = [&](const Segment& g) {
+        const int32_t rows = rows_of(g);
+        Cut c;
+        c.is_wide = any_wide && (int64_t)rows * G > kPrefixCols;
+        const int32_t most = (c.is_wide ? kMfmaCols : kPrefixCols) / G;
+        c.tiles = ceil_div(rows, most);
+        c.rows = ceil_div(rows, c.tiles);
+        c.key_waves = prefix_key_waves(std::min<int32_t>(c.rows * G, kPrefixCols));
+        return c;
+    };
+    double fewest = 0;
+    std::vector<KeyRange> narrow_ranges, wide_ranges;
+    for (const Segment& g : segments.list) {
+        const Cut c = cut_of(g);
+        const int64_t keys = g.end - g.begin;
+        (c.is_wide ? wide_ranges : narrow_ranges).push_back({c.is_wide ? keys : keys * (4 / c.key_waves), c.tiles, c.rows * G});
+        fewest += (double)c.tiles * Hkv * ((double)keys / (c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk) + 1);
+    }
+    if (fewest > kMaxTiles) return false;
+    const int32_t narrow_chunk = narrow_ranges.empty() ? 0 : choose_chunk(narrow, narrow_ranges, Hkv);
+    const int32_t wide_chunk = wide_ranges.empty() ? 0 : choose_chunk(wide, wide_ranges, Hkv);
+
+    // Sources of the rows, in the order of the segments: a sequence's shared ranges come before its own end.
+    struct Placed { int32_t row0, rows, tile_rows, total_rows, nsplit; int64_t part_off; };
+    std::vector<Placed> path;  // of the segment at hand: the shared ranges around it
+    std::vector<const Segment*> around;
+    for (const Segment& g : segments.list) {
+        while (!around.empty() && around.back()->hi < g.lo) {
+            around.pop_back();
+            path.pop_back();
+        }
+        const Cut c = cut_of(g);
+        const int32_t keys = g.end - g.begin, total_rows = rows_of(g);
+        const int32_t step = c.is_wide ? kTileTokens : kSlab * c.key_waves, most = c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk;
+        const int32_t chunk = std::max(step, std::min(most, c.is_wide ? wide_chunk : narrow_chunk / (4 / c.key_waves)));
+        const int32_t pieces = ceil_div(keys, chunk);
+        const int32_t piece = std::min(most, ceil_div(ceil_div(keys, pieces), step) * step);
+        const int32_t nsplit = ceil_div(keys, piece);
+        const bool direct = g.own && around.empty() && nsplit == 1;
+        const Placed placed = {row0[g.lo], total_rows, c.rows, total_rows, nsplit, plan->partial_floats};
+        plan->keys_read += (int64_t)keys * c.tiles;
+        for (int32_t r = 0; r < total_rows; r += c.rows) {
+            const int32_t nrows = std::min(c.rows, total_rows - r), cols = nrows * G;
+            const int64_t stride = (int64_t)cols * (D + 2);
+            for (int h = 0; h < Hkv; ++h)
+                for (int32_t p = 0; p < nsplit; ++p) {
+                    const int32_t begin = g.begin + p * piece, end = std::min(g.end, begin + piece);
+                    const int64_t part = direct ? -1 : plan->partial_floats + ((int64_t)h * nsplit + p) * stride;
+                    if (c.is_wide) {
+                        ppd_work_item it{};
+                        it.kind = 1;
+                        it.seq = g.lo;
+                        it.kvh = h;
+                        it.row0 = g.own ? r : 0;
+                        it.nrows = nrows;
+                        it.grow0 = row0[g.lo] + r;
+                        it.L = g.own ? L[g.lo] : g.end;
+                        it.kv_total = g.end;
+                        it.kv_begin = begin;
+                        it.kv_end = end;
+                        it.group = -1;
+                        it.part_off = part;
+                        plan->blocks.push_back(it);
+                    } else {
+                        plan->items.push_back({g.lo, h, row0[g.lo] + r, cols, g.own ? L[g.lo] + r : g.end, g.end, begin, end, part});
+                    }
+                }
+            if (!direct) plan->partial_floats += stride * nsplit * Hkv;
+            if (plan->items.size() + plan->blocks.size() > (size_t)kMaxTiles) return false;
+        }
+        if (!g.own) {
+            around.push_back(&g);
+            path.push_back(placed);
+            continue;
+        }
+        if (direct) continue;
+        // The sequence's rows, cut where a tile of any of its ranges ends.
+        path.push_back(placed);
+        for (int32_t r = row0[g.lo]; r < row0[g.lo + 1];) {
+            int32_t end = row0[g.lo + 1];
+            for (const Placed& x : path) end = std::min(end, x.row0 + ((r - x.row0) / x.tile_rows + 1) * x.tile_rows);
+            plan->units.push_back({r, end - r, (int32_t)plan->sources.size(), (int32_t)path.size()});
+            plan->join_cols = std::max(plan->join_cols, (end - r) * G);
+            for (const Placed& x : path) {
+                const int32_t tile = (r - x.row0) / x.tile_rows, first = tile * x.tile_rows;
+                const int32_t cols = std::min(x.tile_rows, x.rows - first) * G;
+                plan->sources.push_back({x.part_off + (int64_t)first * G * (D + 2) * x.nsplit * Hkv, cols, (r - x.row0 - first) * G, x.nsplit, 0});
+            }
+            r = end;
+        }
+        path.pop_back();
+    }
+    // the longest first, in their waves' time
+    std::stable_sort(plan->items.begin(), plan->items.end(), [](const PrefixItem& a, const PrefixItem& b) {
+        return (int64_t)(a.kv_end - a.kv_begin) / prefix_key_waves(a.ncols) > (int64_t)(b.kv_end - b.kv_begin) / prefix_key_waves(b.ncols);
+    });
+    std::stable_sort(plan->blocks.begin(), plan->blocks.end(), [](const ppd_work_item& a, const ppd_work_item& b) { return a.kv_end - a.kv_begin > b.kv_end - b.kv_begin; });
+    return true;
+}
+
+}  // namespace ppd
