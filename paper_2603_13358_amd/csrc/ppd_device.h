@@ -104,6 +104,18 @@ __device__ __forceinline__ uint32_t e4m3_codes(float a, float b, float c, float 
     return ((uint32_t)w & 0x7F7F7F7Fu) | ((lo | hi) & 0x80808080u);
 }
 
+// 16 bytes per lane from global memory straight into LDS: lane i of the wave writes lds_base + 16*i
+// (lds_base is wave-uniform and travels in M0).  Written as inline asm so that the compiler's wait-count pass
+// does not see an LDS write it would have to order every later LDS read behind (it would drain the memory
+// counter before the first operand read of each tile); completion is awaited explicitly with s_waitcnt vmcnt.
+// The global address is a wave-uniform base (scalar register pair) plus a 32-bit byte offset per lane.
+__device__ __forceinline__ void lds_direct_load16_at(const void* gbase, uint32_t lane_off, uint32_t lds_addr) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(lane_off), "s"(gbase), "s"(lds_addr)
+                 : "memory", "m0");
+}
+
 // Zeroes the bf16 elements e of a granule of 8 tokens whose position first + e is >= kv_total (never written).
 __device__ __forceinline__ u32x4 zero_unwritten(u32x4 v, int first, int kv_total) {
 #pragma unroll

@@ -53,19 +53,6 @@ __device__ __forceinline__ int64_t checked_page(const KParams& P, int page) {
 //   one barrier per iteration, after K(i+2) and V(i+1) have landed (loads issued in the last NS-2 iterations may
 //   still be in flight); half of the waves take it between their two phases (see the loop).
 // ---------------------------------------------------------------------------------------------------
-// 16 bytes per lane from global memory straight into LDS: lane i of the wave writes lds_base + 16*i
-// (lds_base is wave-uniform and travels in M0).  Written as inline asm so that the compiler's wait-count pass
-// does not see an LDS write it would have to order every later LDS read behind (it would drain the memory
-// counter before the first operand read of each tile); completion is awaited explicitly with s_waitcnt vmcnt.
-// The global address is a wave-uniform base (scalar register pair) plus a 32-bit byte offset per lane.
-__device__ __forceinline__ void lds_direct_load16(const void* gbase, uint32_t lane_off, const char* lds_base) {
-    const uint32_t lds_off = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)lds_base;
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                 :
-                 : "v"(lane_off), "s"(gbase), "s"(__builtin_amdgcn_readfirstlane(lds_off))
-                 : "memory", "m0");
-}
-
 // HALF = false: the vector phase covers the 64 keys of a tile, then the matrix phase (the loop described above).
 // HALF = true: the same tile is worked in two halves of 32 keys -- vector phase, matrix phase, vector phase, matrix
 // phase -- with S^T of 32 keys and half of the packed probabilities live at a time: 24 registers less per lane,
@@ -80,13 +67,6 @@ __device__ __forceinline__ int ring_add(int x, int k) {
     if constexpr ((N & (N - 1)) == 0) return (x + k) & (N - 1);
     const int y = x + k;
     return y >= N ? y - N : y;
-}
-// The same with the LDS byte address given as a wave-uniform integer (no pointer cast per load).
-__device__ __forceinline__ void lds_direct_load16_at(const void* gbase, uint32_t lane_off, uint32_t lds_addr) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                 :
-                 : "v"(lane_off), "s"(gbase), "s"(lds_addr)
-                 : "memory", "m0");
 }
 __device__ __forceinline__ uint32_t lds_base(const char* p) {
     uint32_t a = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;

@@ -11,7 +11,7 @@ namespace ppd {
 constexpr int kSharedStep = kTileTokens;  // sharing is used in steps of this many tokens: the key ranges of row blocks begin at multiples of it
 constexpr int kMinSavedKeys = 256;        // keys that a shared range has to save
 constexpr int kMaxNested = 16;            // shared ranges one behind the other, at most, that a sequence is part of
-constexpr int kPrefixCols = 128;          // query columns of a prefix tile at most: 32 for each wave
+constexpr int kPrefixCols = 128;          // query columns of a prefix tile at most: 32 for each of its four waves
 constexpr int kMaxPrefixChunk = kMaxTreeChunk;  // keys of one at most (its page ids are staged in LDS)
 
 // A tile: `ncols` query columns (row-major over the G heads of a group) of consecutive rows against keys [kv_begin, kv_end), which are read

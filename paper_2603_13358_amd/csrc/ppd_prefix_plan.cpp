@@ -1,5 +1,6 @@
 // Tile list of attention over shared prefixes: which rows meet which keys in which workgroup, and whose partials make a row's result.
 #include <algorithm>
+#include <tuple>
 
 #include "ppd_prefix.h"
 
@@ -48,6 +49,33 @@ private:
 };
 
 int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
+
+// The longest tiles first, and those of the same keys (the column ranges of one segment, head and piece) one after the other on one XCD:
+// workgroups go round the XCDs, each of which has an L2 of its own.
+template <class Item, class Time>
+void order_for_xcds(std::vector<Item>& items, Time time) {
+    auto same_keys = [](const Item& a, const Item& b) { return a.seq == b.seq && a.kvh == b.kvh && a.kv_begin == b.kv_begin && a.kv_end == b.kv_end && a.kv_total == b.kv_total; };
+    std::vector<size_t> index(items.size());
+    for (size_t i = 0; i < items.size(); ++i) index[i] = i;
+    auto key = [&](size_t i) { return std::make_tuple(-time(items[i]), items[i].seq, items[i].kvh, items[i].kv_begin, items[i].kv_total); };
+    std::stable_sort(index.begin(), index.end(), [&](size_t a, size_t b) { return key(a) < key(b); });
+    std::vector<size_t> lists[kXcds];
+    for (size_t i = 0; i < index.size();) {
+        size_t to = i + 1;
+        while (to < index.size() && same_keys(items[index[i]], items[index[to]])) ++to;
+        auto* const least = std::min_element(lists, lists + kXcds, [](const auto& a, const auto& b) { return a.size() < b.size(); });
+        least->insert(least->end(), index.begin() + i, index.begin() + to);
+        i = to;
+    }
+    std::vector<Item> ordered;
+    ordered.reserve(items.size());
+    size_t longest = 0;
+    for (const auto& l : lists) longest = std::max(longest, l.size());
+    for (size_t k = 0; k < longest; ++k)
+        for (const auto& l : lists)
+            if (k < l.size()) ordered.push_back(items[l[k]]);
+    items.swap(ordered);
+}
 
 }  // namespace
 
@@ -167,11 +195,8 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
         }
         path.pop_back();
     }
-    // the longest first, in their waves' time
-    std::stable_sort(plan->items.begin(), plan->items.end(), [](const PrefixItem& a, const PrefixItem& b) {
-        return (int64_t)(a.kv_end - a.kv_begin) / prefix_key_waves(a.ncols) > (int64_t)(b.kv_end - b.kv_begin) / prefix_key_waves(b.ncols);
-    });
-    std::stable_sort(plan->blocks.begin(), plan->blocks.end(), [](const ppd_work_item& a, const ppd_work_item& b) { return a.kv_end - a.kv_begin > b.kv_end - b.kv_begin; });
+    order_for_xcds(plan->items, [](const PrefixItem& x) { return (int64_t)(x.kv_end - x.kv_begin) / prefix_key_waves(x.ncols); });
+    order_for_xcds(plan->blocks, [](const ppd_work_item& x) { return (int64_t)(x.kv_end - x.kv_begin); });
     return true;
 }
 
