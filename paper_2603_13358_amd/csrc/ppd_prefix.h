@@ -9,7 +9,6 @@
 namespace ppd {
 
 constexpr int kSharedStep = kTileTokens;  // sharing is used in steps of this many tokens: the key ranges of row blocks begin at multiples of it
-constexpr int kMinSavedKeys = 256;        // keys that a shared range has to save
 constexpr int kMaxNested = 16;            // shared ranges one behind the other, at most, that a sequence is part of
 constexpr int kPrefixCols = 128;          // query columns of a prefix tile at most: 32 for each of its four waves
 constexpr int kMaxPrefixChunk = kMaxTreeChunk;  // keys of one at most (its page ids are staged in LDS)
@@ -27,11 +26,18 @@ struct PrefixItem {
 // Waves of a tile that have the same columns, each with every waves-th slab of the keys.
 constexpr int prefix_key_waves(int ncols) { return ncols <= 32 ? 4 : ncols <= 64 ? 2 : 1; }
 
-// Partials of some columns: `nsplit` of [ncols][D] sums, then [ncols] (m, l) pairs, one behind the other, and behind these the next KV head's.
+// What a tile costs, in the time that one of few columns takes for a key: a key, and its start beyond theirs.
+struct TileCost { double key, start; };
+constexpr TileCost prefix_tile_cost(int ncols) {
+    return prefix_key_waves(ncols) == 4 ? TileCost{1.0, 0.0} : prefix_key_waves(ncols) == 2 ? TileCost{0.85, 200.0} : TileCost{1.65, 300.0};
+}
+
+// Partials of some columns: `nsplit` of ncols * D floats, the sums, then [ncols] (m, l) pairs, one behind the other, and behind these the next
+// KV head's.  The sums are [ncols][D] where they come from a row block; else [4 columns][D / 4][column][4], fewer columns in the last.
 struct JoinSource {
     int64_t part_off;
     int32_t ncols, col0;       // col0: where the unit's first column is among them
-    int32_t nsplit, unused;
+    int32_t nsplit, by_rows;
 };
 
 // Rows whose columns have the same sources.

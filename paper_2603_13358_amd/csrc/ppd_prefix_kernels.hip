@@ -25,6 +25,13 @@ template <> struct Granule<true> { typedef u32x2 type; };
 __device__ __forceinline__ u32x4 operand(u32x4 g) { return g; }
 __device__ __forceinline__ u32x4 operand(u32x2 g) { return fp8x8_to_bf16x8(g); }
 
+// Where element d (a multiple of 4) of a column's sum is in a tile's partial: four columns at a time, four elements of each side by side.
+template <int HD>
+__device__ __forceinline__ int partial_at(int ncols, int col, int d) {
+    const int first = col & ~3, width = ncols - first < 4 ? ncols - first : 4;
+    return first * HD + (d / 4 * width + (col & 3)) * 4;
+}
+
 constexpr int kPrefixWaves = 4, kPrefixThreads = 64 * kPrefixWaves;
 constexpr int kStageCols = 16;  // columns of a wave that meet in LDS at a time
 
@@ -177,7 +184,7 @@ struct Lane {
                 }
         }
     }
-    // The waves' results meet in LDS, kStageCols columns of each wave at a time, and leave as a partial or as the rows' result.
+    // Waves that have the same columns meet in LDS, kStageCols columns at a time; the result leaves as a partial (partial_at) or as the rows'.
     template <int KEY_WAVES>
     __device__ __forceinline__ void finish(const Columns<HD>& acc, float* stage, f32x2* stage_ml) const {
         constexpr int ROW = HD + 4;  // the padding spreads the columns over the banks
@@ -186,7 +193,7 @@ struct Lane {
         for (int c0 = 0; c0 < 32; c0 += kStageCols) {
             if (c0 >= it.ncols) break;
             __syncthreads();
-            if (l32 >= c0 && l32 < c0 + kStageCols) {
+            if (l32 >= c0 && l32 < c0 + kStageCols && l32 < it.ncols) {
                 float* to = stage + (wave * kStageCols + l32 - c0) * ROW + h * 4;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
@@ -197,36 +204,61 @@ struct Lane {
             }
             __syncthreads();
             constexpr int BLOCKS = kPrefixWaves / KEY_WAVES;  // of 32 columns
-            for (int idx = tid; idx < BLOCKS * kStageCols * (HD / 4); idx += kPrefixThreads) {
-                const int d = idx % (HD / 4) * 4, cl = idx / (HD / 4) % kStageCols, block = idx / (HD / 4 * kStageCols);
-                const int cc = block * 32 + c0 + cl;
-                if (cc >= it.ncols) continue;
-                float mm = NEG_INF;
+            for (int block = 0; block < BLOCKS; ++block) {
+                const int left = it.ncols - block * 32 - c0, cols = left < kStageCols ? left : kStageCols;
+                for (int idx = tid; idx < cols * (HD / 4); idx += kPrefixThreads) {
+                    // in the order in which partials lie, or results
+                    const int four = idx / HD * 4, width = cols - four < 4 ? cols - four : 4;
+                    const int cl = it.part_off >= 0 ? four + idx % HD % width : idx / (HD / 4), d = (it.part_off >= 0 ? idx % HD / width : idx % (HD / 4)) * 4;
+                    const int cc = block * 32 + c0 + cl;
+                    float mm = NEG_INF;
 #pragma unroll
-                for (int w = 0; w < KEY_WAVES; ++w) mm = fmaxf(mm, stage_ml[(block * KEY_WAVES + w) * kStageCols + cl][0]);
-                f32x4 o = {0.f, 0.f, 0.f, 0.f};
-                float l = 0.f;
+                    for (int w = 0; w < KEY_WAVES; ++w) mm = fmaxf(mm, stage_ml[(block * KEY_WAVES + w) * kStageCols + cl][0]);
+                    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+                    float l = 0.f;
 #pragma unroll
-                for (int w = 0; w < KEY_WAVES; ++w) {
-                    const int from = (block * KEY_WAVES + w) * kStageCols + cl;
-                    const f32x2 ml = stage_ml[from];
-                    if (ml[0] == NEG_INF) continue;
-                    const float f = fast_exp2((ml[0] - mm) * c);
-                    l += f * ml[1];
-                    o += f * *reinterpret_cast<const f32x4*>(stage + from * ROW + d);
-                }
-                if (it.part_off >= 0) {
-                    float* to = P.partials + it.part_off;
-                    *reinterpret_cast<f32x4*>(to + cc * HD + d) = o;
-                    if (d == 0) *reinterpret_cast<f32x2*>(to + it.ncols * HD + cc * 2) = f32x2{mm, l};
-                } else {
-                    const int row = row_of(cc);
-                    const int64_t at = (int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G);
-                    const f32x4 r = o * ((l == 0.f ? 0.f : 1.0f / l) * P.v_scale);  // a row whose scores are all minus infinity gives zeros
-                    *reinterpret_cast<u32x2*>(P.out + at * HD + d) = u32x2{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
+                    for (int w = 0; w < KEY_WAVES; ++w) {
+                        const int from = (block * KEY_WAVES + w) * kStageCols + cl;
+                        const f32x2 ml = stage_ml[from];
+                        if (ml[0] == NEG_INF) continue;
+                        const float f = fast_exp2((ml[0] - mm) * c);
+                        l += f * ml[1];
+                        o += f * *reinterpret_cast<const f32x4*>(stage + from * ROW + d);
+                    }
+                    if (it.part_off >= 0) {
+                        float* to = P.partials + it.part_off;
+                        *reinterpret_cast<f32x4*>(to + partial_at<HD>(it.ncols, cc, d)) = o;
+                        if (d == 0) *reinterpret_cast<f32x2*>(to + it.ncols * HD + cc * 2) = f32x2{mm, l};
+                    } else {
+                        store_result(cc, d, o, l);
+                    }
                 }
             }
         }
+    }
+    __device__ __forceinline__ void store_result(int cc, int d, const f32x4& o, float l) const {
+        const int row = row_of(cc);
+        const int64_t at = (int64_t)(it.grow0 + row) * P.Hq + it.kvh * P.G + (cc - row * P.G);
+        const f32x4 r = o * ((l == 0.f ? 0.f : 1.0f / l) * P.v_scale);  // a row whose scores are all minus infinity gives zeros
+        *reinterpret_cast<u32x2*>(P.out + at * HD + d) = u32x2{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
+    }
+    // A wave whose columns no other has: from registers.  Partials lie as the registers do, so that a store is one run of memory
+    // (through LDS and by rows it took 5 us of a tile's 25).
+    __device__ __forceinline__ void finish_alone(const Columns<HD>& acc, int col0) const {
+        const float l_tot = sum_halves(acc.l);
+        const int cc = col0 + l32;
+        if (cc >= it.ncols) return;
+        float* const to = P.partials + it.part_off;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 o = {acc.o[db][4 * i], acc.o[db][4 * i + 1], acc.o[db][4 * i + 2], acc.o[db][4 * i + 3]};
+                const int d = db * 32 + i * 8 + h * 4;
+                if (it.part_off >= 0) *reinterpret_cast<f32x4*>(to + partial_at<HD>(it.ncols, cc, d)) = o;
+                else store_result(cc, d, o, l_tot);
+            }
+        if (it.part_off >= 0 && h == 0) *reinterpret_cast<f32x2*>(to + it.ncols * HD + cc * 2) = f32x2{acc.m, l_tot};
     }
 };
 
@@ -384,6 +416,7 @@ __device__ __forceinline__ void many_columns(const PrefixParams& P, const Prefix
             if constexpr (NEXT) scores(s + 1);
         } else {
             constexpr int PRODUCTS = 2 * DB + KS, AHEAD = 4;
+            __builtin_amdgcn_s_setprio(1);  // before the other workgroup's exponentials (96 decodes over documents, FP8, 113 -> 109 us)
             auto read = [&](int j) { return j < 2 * DB ? v_operand(s, j) : k_operand(s + 1, j - 2 * DB); };
             u32x4 buf[AHEAD];
 #pragma unroll
@@ -406,6 +439,7 @@ __device__ __forceinline__ void many_columns(const PrefixParams& P, const Prefix
                 }
                 __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
             }
+            __builtin_amdgcn_s_setprio(0);
         }
         if constexpr (MASKED) {
             if (strange) at.add_dropped(acc, ids + s * 2, base, limit);
@@ -454,7 +488,8 @@ __device__ __forceinline__ void many_columns(const PrefixParams& P, const Prefix
         for (; s < slabs && s + KEY_WAVES <= clear; s += KEY_WAVES) turn(no);
         for (; s < slabs; s += KEY_WAVES) turn(yes);
     }
-    at.template finish<KEY_WAVES>(acc, reinterpret_cast<float*>(ring), stage_ml);
+    if constexpr (KEY_WAVES == 1) at.finish_alone(acc, col0);
+    else at.template finish<KEY_WAVES>(acc, reinterpret_cast<float*>(ring), stage_ml);
 }
 
 template <int HD, bool FP8>
@@ -495,8 +530,8 @@ template <int HD>
 __global__ __launch_bounds__(256) void ppd_prefix_join_kernel(const PrefixParams P) {
     constexpr int LANES = HD / 4, COLS = 256 / LANES, AT_ONCE = 8;
     __shared__ JoinSource sources[kMaxNested + 1];
-    __shared__ int64_t part_at[kJoinParts];  // floats: the partial's sums of the workgroup's first column
-    __shared__ int pair_at[kJoinParts];      // from there to its pair
+    __shared__ int64_t part_at[kJoinParts];  // floats: the partial
+    __shared__ int part_cols[kJoinParts], part_col0[kJoinParts];  // its columns (negative: of a row block), the workgroup's first among them
     __shared__ f32x2 ml[kJoinPairs];
     __shared__ f32x4 other[256];
     const JoinUnit u = P.units[blockIdx.x];
@@ -509,7 +544,9 @@ __global__ __launch_bounds__(256) void ppd_prefix_join_kernel(const PrefixParams
     int share = 1;  // threads of a column and d: each has every share-th partial
     while (2 * share * cols <= COLS && share < parts) share *= 2;
     const float c = P.scale_log2e;
-    const int d = tid % LANES * 4, cl = tid / LANES % cols, mine = tid / LANES / cols;
+    // in the order in which the partials lie: four columns side by side, or row after row
+    const bool by_rows = sources[0].by_rows;
+    const int cl = by_rows ? tid / LANES % cols : tid % cols, d = (by_rows ? tid % LANES : tid / cols % LANES) * 4, mine = tid / LANES / cols;
     const bool works = mine < share;
     const int most = kJoinPairs / cols < kJoinParts ? kJoinPairs / cols : kJoinParts;
     float m = NEG_INF, l = 0.f;  // of the column, all threads alike
@@ -521,21 +558,23 @@ __global__ __launch_bounds__(256) void ppd_prefix_join_kernel(const PrefixParams
             int part = p0 + i, from = 0;
             while (part >= sources[from].nsplit) part -= sources[from++].nsplit;
             const JoinSource x = sources[from];
-            const int64_t begin = x.part_off + ((int64_t)kvh * x.nsplit + part) * x.ncols * (HD + 2);
-            part_at[i] = begin + (x.col0 + col0) * HD;
-            pair_at[i] = x.ncols * HD + (x.col0 + col0) * 2 - (x.col0 + col0) * HD;
+            part_at[i] = x.part_off + ((int64_t)kvh * x.nsplit + part) * x.ncols * (HD + 2);
+            part_cols[i] = x.by_rows ? -x.ncols : x.ncols;
+            part_col0[i] = x.col0 + col0;
         }
         __syncthreads();
         for (int i = tid; i < count * cols; i += 256) {
             const int part = i / cols;
-            ml[i] = *reinterpret_cast<const f32x2*>(P.partials + part_at[part] + pair_at[part] + (i - part * cols) * 2);
+            const int ncols = part_cols[part] < 0 ? -part_cols[part] : part_cols[part];
+            ml[i] = *reinterpret_cast<const f32x2*>(P.partials + part_at[part] + ncols * HD + (part_col0[part] + i - part * cols) * 2);
         }
         f32x4 v[AT_ONCE];
         auto ask = [&](int j0) {
 #pragma unroll
             for (int t = 0; t < AT_ONCE; ++t) {
                 const int j = j0 + t * share < count ? j0 + t * share : 0;
-                v[t] = *reinterpret_cast<const f32x4*>(P.partials + part_at[j] + cl * HD + d);
+                const int cc = part_col0[j] + cl;
+                v[t] = *reinterpret_cast<const f32x4*>(P.partials + part_at[j] + (part_cols[j] < 0 ? cc * HD + d : partial_at<HD>(part_cols[j], cc, d)));
             }
         };
         ask(mine);

@@ -15,37 +15,59 @@ struct Segment {
     bool own;
 };
 
+// Time of the tiles that have `cols` columns, for a key.
+double key_time(int64_t cols) {
+    const int64_t full = cols / kPrefixCols;
+    return full * prefix_tile_cost(kPrefixCols).key + (cols % kPrefixCols ? prefix_tile_cost((int)(cols % kPrefixCols)).key : 0);
+}
+
 // The shared ranges of sequences [lo, hi] from key `start` on, and their own ends.  common[i] is what sequence i has in common with the one
-// before; the least of them is in common to all, and where it occurs they fall apart.
+// before; the least of them is in common to all, and where it occurs they fall apart into runs.
 class Segments {
 public:
-    Segments(const std::vector<int32_t>& common, const int32_t* L, const int32_t* n) : common_(common), L_(L), n_(n) {}
+    Segments(const std::vector<int32_t>& common, const int32_t* L, const int32_t* n, const std::vector<int32_t>& row0, int G)
+        : common_(common), L_(L), n_(n), row0_(row0), G_(G) {}
     std::vector<Segment> list;
 
-    // Every level shares 64 keys at least.  One that saves too little is left to the sequences below, and then they are fewer than five; with
-    // that and kMaxNested the levels are few.
+    // A shared range has to save more than it costs: the tiles of the runs that have fewer columns, and their reading the keys each for
+    // itself (half a key's time), against a partial's columns more to be written and read (3.7 keys' time each, 1040 bytes) and a tile's start.
+    // Every level shares 64 keys at least, so runs that are not worth it are short, and with kMaxNested the levels are few.
     void add(int32_t lo, int32_t hi, int32_t start, int level) {
         if (lo == hi || level == kMaxNested) {
             for (int32_t i = lo; i <= hi; ++i) list.push_back({i, i, start, L_[i] + n_[i], true});
             return;
         }
         const int32_t least = *std::min_element(common_.begin() + lo + 1, common_.begin() + hi + 1);
-        if ((int64_t)(hi - lo) * (least - start) >= kMinSavedKeys) {
+        double apart = -0.5;
+        for (int32_t from = lo; from <= hi;) {
+            const int32_t to = run_end(from, hi, least);
+            apart += key_time(columns(from, to)) + 0.5;
+            from = to + 1;
+        }
+        const int64_t cols = columns(lo, hi);
+        if ((least - start) * (apart - key_time(cols)) > 3.7 * cols + 200) {
             list.push_back({lo, hi, start, least, false});
             start = least;
             ++level;
         }
         for (int32_t from = lo; from <= hi;) {
-            int32_t to = from;
-            while (to < hi && common_[to + 1] > least) ++to;
+            const int32_t to = run_end(from, hi, least);
             add(from, to, start, level);
             from = to + 1;
         }
     }
 
 private:
+    int32_t run_end(int32_t from, int32_t hi, int32_t least) const {
+        while (from < hi && common_[from + 1] > least) ++from;
+        return from;
+    }
+    int64_t columns(int32_t lo, int32_t hi) const { return (int64_t)(row0_[hi + 1] - row0_[lo]) * G_; }
+
     const std::vector<int32_t>& common_;
     const int32_t *L_, *n_;
+    const std::vector<int32_t>& row0_;
+    int G_;
 };
 
 int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
@@ -88,61 +110,86 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
         if (i > 0) common[i] = shared[i] / kSharedStep * kSharedStep;
         plan->keys_alone += (int64_t)L[i] + n[i];
     }
-    Segments segments(common, L, n);
-    for (int32_t from = 0; from < B;) {  // what shares nothing stands alone
-        int32_t to = from;
-        while (to + 1 < B && common[to + 1] > 0) ++to;
-        segments.add(from, to, 0, 0);
-        from = to + 1;
-    }
-    const TileKind narrow = {kMaxPrefixChunk * 4, kTreeStep, 256, 256, 0, 2 * num_cus};
-    const TileKind wide = {kMaxTreeBlockChunk, kTileTokens, 350, 500, 0.0114, num_cus};
-    // How a segment is cut: `tiles` column ranges of `rows` rows each, `keys` of time each (a tile whose waves have columns of their own goes
-    // over its keys in one wave's time each).
-    struct Cut { bool is_wide; int32_t tiles, rows, key_waves; };
     auto rows_of = [&](const Segment& g) { return row0[g.hi + 1] - row0[g.lo]; };
-    bool any_wide = false;
-    for (const Segment& g : segments.list) any_wide |= g.own && (int64_t)rows_of(g) * G > kPrefixCols;
-    auto cut_of = [&](const Segment& g) {
+    // How a segment is cut: `tiles` column ranges of `rows` rows each.
+    struct Cut { bool is_wide; int32_t tiles, rows, key_waves; TileCost cost; };
+    // A list of segments, how it is cut and its time.  Row blocks are a launch of their own: where a sequence has more columns than a tile
+    // takes there is one, and it takes all segments of more than 32 columns.
+    struct Choice {
+        std::vector<Segment> segments;
+        bool any_wide = false, possible = true;
+        int32_t narrow_chunk = 0, wide_chunk = 0;
+        double time = 0;
+    };
+    auto cut_of = [&](const Choice& x, const Segment& g) {
         const int32_t rows = rows_of(g);
         Cut c;
-        c.is_wide = any_wide && (int64_t)rows * G > kPrefixCols;
+        c.is_wide = x.any_wide && (int64_t)rows * G > kTreeCols;
         const int32_t most = (c.is_wide ? kMfmaCols : kPrefixCols) / G;
         c.tiles = ceil_div(rows, most);
         c.rows = ceil_div(rows, c.tiles);
         c.key_waves = prefix_key_waves(std::min<int32_t>(c.rows * G, kPrefixCols));
+        c.cost = c.is_wide ? TileCost{1, 0} : prefix_tile_cost(c.rows * G);
         return c;
     };
-    double fewest = 0;
-    std::vector<KeyRange> narrow_ranges, wide_ranges;
-    for (const Segment& g : segments.list) {
-        const Cut c = cut_of(g);
-        const int64_t keys = g.end - g.begin;
-        (c.is_wide ? wide_ranges : narrow_ranges).push_back({c.is_wide ? keys : keys * (4 / c.key_waves), c.tiles, c.rows * G});
-        fewest += (double)c.tiles * Hkv * ((double)keys / (c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk) + 1);
+    auto weigh = [&](Choice& x) {
+        const TileKind narrow = {kMaxPrefixChunk * 2, kTreeStep, 200, 256, 0.012, 2 * num_cus};
+        const TileKind wide = {kMaxTreeBlockChunk, kTileTokens, 350, 500, 0.0114, num_cus};
+        for (const Segment& g : x.segments) x.any_wide |= g.own && (int64_t)rows_of(g) * G > kPrefixCols;
+        double fewest = 0;
+        std::vector<KeyRange> narrow_ranges, wide_ranges;
+        for (const Segment& g : x.segments) {
+            const Cut c = cut_of(x, g);
+            const int64_t keys = g.end - g.begin;
+            (c.is_wide ? wide_ranges : narrow_ranges).push_back({(int64_t)(keys * c.cost.key) + 1, c.tiles, c.rows * G, c.cost.start, !g.own || g.begin > 0});
+            fewest += (double)c.tiles * Hkv * ((double)keys / (c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk) + 1);
+        }
+        x.possible = fewest <= kMaxTiles;
+        if (!x.possible) return;
+        double time = 0;
+        if (!narrow_ranges.empty()) x.narrow_chunk = choose_chunk(narrow, narrow_ranges, Hkv, &time);
+        x.time = time;
+        if (!wide_ranges.empty()) x.wide_chunk = choose_chunk(wide, wide_ranges, Hkv, &time), x.time += time;
+    };
+    Choice choice;
+    {
+        Segments segments(common, L, n, row0, G);
+        for (int32_t from = 0; from < B;) {  // what shares nothing stands alone
+            int32_t to = from;
+            while (to + 1 < B && common[to + 1] > 0) ++to;
+            segments.add(from, to, 0, 0);
+            from = to + 1;
+        }
+        choice.segments.swap(segments.list);
     }
-    if (fewest > kMaxTiles) return false;
-    const int32_t narrow_chunk = narrow_ranges.empty() ? 0 : choose_chunk(narrow, narrow_ranges, Hkv);
-    const int32_t wide_chunk = wide_ranges.empty() ? 0 : choose_chunk(wide, wide_ranges, Hkv);
+    weigh(choice);
+    if (choice.segments.size() > (size_t)B) {
+        // Nothing shared, and where no range is cut either no join: small batches (three sequences of 231 keys, 200 of them shared, 8.3 -> 5.3 us).
+        Choice apart;
+        for (int32_t i = 0; i < B; ++i) apart.segments.push_back({i, i, 0, L[i] + n[i], true});
+        weigh(apart);
+        if (apart.possible && (!choice.possible || apart.time < choice.time)) choice = std::move(apart);
+    }
+    if (!choice.possible) return false;
 
     // Sources of the rows, in the order of the segments: a sequence's shared ranges come before its own end.
-    struct Placed { int32_t row0, rows, tile_rows, total_rows, nsplit; int64_t part_off; };
+    struct Placed { int32_t row0, rows, tile_rows, nsplit; bool by_rows; int64_t part_off; };
     std::vector<Placed> path;  // of the segment at hand: the shared ranges around it
     std::vector<const Segment*> around;
-    for (const Segment& g : segments.list) {
+    for (const Segment& g : choice.segments) {
         while (!around.empty() && around.back()->hi < g.lo) {
             around.pop_back();
             path.pop_back();
         }
-        const Cut c = cut_of(g);
+        const Cut c = cut_of(choice, g);
         const int32_t keys = g.end - g.begin, total_rows = rows_of(g);
         const int32_t step = c.is_wide ? kTileTokens : kSlab * c.key_waves, most = c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk;
-        const int32_t chunk = std::max(step, std::min(most, c.is_wide ? wide_chunk : narrow_chunk / (4 / c.key_waves)));
+        const int32_t chunk = std::max(step, std::min(most, (int32_t)((c.is_wide ? choice.wide_chunk : choice.narrow_chunk) / c.cost.key)));
         const int32_t pieces = ceil_div(keys, chunk);
         const int32_t piece = std::min(most, ceil_div(ceil_div(keys, pieces), step) * step);
         const int32_t nsplit = ceil_div(keys, piece);
         const bool direct = g.own && around.empty() && nsplit == 1;
-        const Placed placed = {row0[g.lo], total_rows, c.rows, total_rows, nsplit, plan->partial_floats};
+        const Placed placed = {row0[g.lo], total_rows, c.rows, nsplit, c.is_wide, plan->partial_floats};
         plan->keys_read += (int64_t)keys * c.tiles;
         for (int32_t r = 0; r < total_rows; r += c.rows) {
             const int32_t nrows = std::min(c.rows, total_rows - r), cols = nrows * G;
@@ -189,13 +236,13 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
             for (const Placed& x : path) {
                 const int32_t tile = (r - x.row0) / x.tile_rows, first = tile * x.tile_rows;
                 const int32_t cols = std::min(x.tile_rows, x.rows - first) * G;
-                plan->sources.push_back({x.part_off + (int64_t)first * G * (D + 2) * x.nsplit * Hkv, cols, (r - x.row0 - first) * G, x.nsplit, 0});
+                plan->sources.push_back({x.part_off + (int64_t)first * G * (D + 2) * x.nsplit * Hkv, cols, (r - x.row0 - first) * G, x.nsplit, x.by_rows});
             }
             r = end;
         }
         path.pop_back();
     }
-    order_for_xcds(plan->items, [](const PrefixItem& x) { return (int64_t)(x.kv_end - x.kv_begin) / prefix_key_waves(x.ncols); });
+    order_for_xcds(plan->items, [](const PrefixItem& x) { return (int64_t)((x.kv_end - x.kv_begin) * prefix_tile_cost(x.ncols).key + prefix_tile_cost(x.ncols).start); });
     order_for_xcds(plan->blocks, [](const ppd_work_item& x) { return (int64_t)(x.kv_end - x.kv_begin); });
     return true;
 }

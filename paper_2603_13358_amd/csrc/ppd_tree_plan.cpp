@@ -33,7 +33,7 @@ double last_tile_end(std::vector<double>& tiles, int32_t slots) {
 
 // Fewer tiles start less often and leave fewer partials, more fill the slots more evenly.  Up to four rounds the tiles are laid out to
 // see how long they take; many short ones last about their even share and half of the longest.
-int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, int32_t heads) {
+int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, int32_t heads, double* time) {
     int64_t longest = 1;
     for (const auto& r : ranges) longest = std::max(longest, r.keys);
     const int32_t slots = std::max(1, kind.slots / heads);
@@ -44,11 +44,11 @@ int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, 
         double count = 0, sum = 0, most = 0, joined = 0;
         for (const auto& r : ranges) {
             const double pieces = (double)ceil_div(r.keys, (int64_t)c);
-            const double cost = r.keys / pieces + kind.start_keys;
+            const double cost = r.keys / pieces + kind.start_keys + r.start_keys;
             count += pieces * r.tiles;
             sum += pieces * r.tiles * cost;
             most = std::max(most, cost);
-            if (pieces > 1) joined += pieces * r.tiles * r.cols;
+            if (pieces > 1 || r.partial) joined += pieces * r.tiles * r.cols;
         }
         if (count * heads > kMaxTiles) break;
         double est = count <= slots ? most : sum / slots + 0.5 * most;
@@ -56,7 +56,7 @@ int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, 
             tiles.clear();
             for (const auto& r : ranges) {
                 const int64_t pieces = ceil_div(r.keys, (int64_t)c);
-                tiles.insert(tiles.end(), (size_t)(pieces * r.tiles), (double)r.keys / pieces + kind.start_keys);
+                tiles.insert(tiles.end(), (size_t)(pieces * r.tiles), (double)r.keys / pieces + kind.start_keys + r.start_keys);
             }
             est = last_tile_end(tiles, slots);
         }
@@ -67,6 +67,7 @@ int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, 
         }
         if (count > 16.0 * slots) break;
     }
+    if (time) *time = std::max(0.0, best);
     return chunk;
 }
 

@@ -187,10 +187,10 @@ static void plans() {
     std::mt19937 r(5);
     auto in = [&](int lo, int hi) { return (int)(lo + r() % (unsigned)(hi - lo + 1)); };
     int64_t wide = 0, joins = 0, saved = 0;
-    for (int round = 0; round < 300; ++round) {
+    for (int round = 0; round < 400; ++round) {
         const int G = in(1, 8), Hkv = in(1, 4);
         const ppd_shape s = {G * Hkv, Hkv, in(0, 1) ? 64 : 128, 16, 1 << 20};
-        const int B = in(1, 40), longest = in(0, 3) ? 2000 : 60000, most_new = in(0, 2) ? 3 : 200;
+        const int B = in(1, 40), longest = in(0, 2) ? 20000 : 2000, most_new = in(0, 2) ? 3 : 200;
         std::vector<int32_t> shared(B, 0), L(B), n(B);
         for (int i = 0; i < B; ++i) {
             L[i] = in(0, longest);
@@ -201,13 +201,20 @@ static void plans() {
             if (in(0, 2)) shared[i] = std::min(both, 640 * in(0, 3));
             shared[i] = std::max(0, shared[i]);
         }
+        if (in(0, 1)) {  // one prompt in front of all, and of some more than that
+            const int prompt = in(100, longest);
+            for (int i = 0; i < B; ++i) {
+                L[i] = prompt + in(0, 3000);
+                if (i > 0) shared[i] = in(0, 1) ? prompt : in(prompt, std::min(L[i], L[i - 1]));
+            }
+        }
         ppd::PrefixPlan plan;
         check_plan(s, shared, L, n, plan);
         wide += (int64_t)plan.blocks.size();
         joins += (int64_t)plan.units.size();
         saved += plan.keys_read < plan.keys_alone;
     }
-    CHECK(wide > 1000 && joins > 1000 && saved > 100);
+    CHECK(wide > 1000 && joins > 1000 && saved > 150);
     // chains of more levels than are kept, both ways, and a batch too large for one launch
     for (int down = 0; down < 2; ++down) {
         const int B = 3000;
@@ -237,8 +244,8 @@ static void plans() {
 static void streams() {
     ppd_ctx* ctx = make(8, 2, 64);
     SimStream a, b;
-    int32_t S[4] = {0, 128, 128, 128}, L[4] = {130, 140, 150, 160}, n[4] = {1, 1, 1, 1};
-    auto call = [&](SimStream* st) { return ppd_prefix_attention(ctx, device, device, tables, 20, S, L, n, 4, 1.f, device, st); };
+    int32_t S[4] = {0, 64000, 64000, 64000}, L[4] = {64030, 64040, 64050, 64060}, n[4] = {1, 1, 1, 1};
+    auto call = [&](SimStream* st) { return ppd_prefix_attention(ctx, device, device, tables, 4100, S, L, n, 4, 1.f, device, st); };
     sim.capturing = true;
     CHECK(call(&a) == PPD_ERR_RANGE && !ctx->prefix && g_tiles.empty());
     sim.capturing = false;
@@ -246,14 +253,14 @@ static void streams() {
     CHECK(call(&a) == PPD_OK && a.waiting() == 1 && g_tiles.size() == 2);
     sim.capturing = true;
     CHECK(call(&a) == PPD_OK && a.waiting() == 1);
-    S[2] = 64;
+    S[2] = 32000;
     CHECK(call(&a) == PPD_ERR_RANGE && a.waiting() == 1 && g_tiles.size() == 3);
-    S[2] = 128;
+    S[2] = 64000;
     sim.capturing = false;
     CHECK(call(&b) == PPD_OK && a.waiting() == 0);  // another stream: the first one's work has ended
     CHECK(b.waiting() == 0 && g_tiles.size() == 4);
     for (int i = 0; i < 3 * kStagingSlots; ++i) {
-        L[0] = 131 + i;
+        L[0] = 64031 + i;
         if (b.waiting() == kStagingSlots) b.run(1);
         CHECK(call(&b) == PPD_OK);
     }
