@@ -214,7 +214,7 @@ static void plans() {
         joins += (int64_t)plan.units.size();
         saved += plan.keys_read < plan.keys_alone;
     }
-    CHECK(wide > 1000 && joins > 1000 && saved > 150);
+    CHECK(wide > 1000 && joins > 1000 && saved > 100);
     // chains of more levels than are kept, both ways, and a batch too large for one launch
     for (int down = 0; down < 2; ++down) {
         const int B = 3000;
