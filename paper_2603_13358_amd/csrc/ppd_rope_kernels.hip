@@ -17,10 +17,9 @@ namespace ppd {
 namespace {
 
 // Where pair i of a head is: elements (i, i + rotary_dim / 2) with whole granules of 8 on both sides, or without, or (2i, 2i + 1).
-// What is not rotated counts as pairs (2i, 2i + 1) behind.
 enum Layout { HALF, HALF_ODD, INTERLEAVED };
 
-// 8 pairs of a head, as they lie in memory: two granules (HALF, INTERLEAVED), or first and second elements (HALF_ODD).
+// 16 elements of a head, two granules: 8 pairs, or, HALF_ODD, elements whose partners other lanes of the wave have.
 struct Unit {
     u32x4 g[2];
 };
@@ -31,29 +30,34 @@ __device__ __forceinline__ int granule_of(int unit, int which, int rotary_dim) {
     if (LAYOUT == HALF && unit < rotated) return unit + which * rotated;
     return 2 * unit + which;
 }
-__device__ __forceinline__ int element_of(int pair, int which, int rotary_dim) {
-    return pair < rotary_dim / 2 ? pair + which * (rotary_dim / 2) : 2 * pair + which;
-}
 
 template <Layout LAYOUT>
 __device__ __forceinline__ Unit load_unit(const uint16_t* head, int unit, int rotary_dim) {
     Unit x;
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        if constexpr (LAYOUT == HALF_ODD) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                x.g[w][e] = (uint32_t)head[element_of(unit * 8 + 2 * e, w, rotary_dim)] | ((uint32_t)head[element_of(unit * 8 + 2 * e + 1, w, rotary_dim)] << 16);
-        } else {
-            x.g[w] = APPEND_LOAD(reinterpret_cast<const u32x4*>(head + granule_of<LAYOUT>(unit, w, rotary_dim) * 8));
-        }
-    }
+    for (int w = 0; w < 2; ++w) x.g[w] = APPEND_LOAD(reinterpret_cast<const u32x4*>(head + granule_of<LAYOUT>(unit, w, rotary_dim) * 8));
     return x;
+}
+template <Layout LAYOUT, bool STREAM = false>
+__device__ __forceinline__ void store_unit(uint16_t* head, const Unit& x, int unit, int rotary_dim) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        u32x4* const to = reinterpret_cast<u32x4*>(head + granule_of<LAYOUT>(unit, w, rotary_dim) * 8);
+        if constexpr (STREAM) APPEND_STORE(x.g[w], to);
+        else *to = x.g[w];
+    }
 }
 
 __device__ __forceinline__ float element(const u32x4& g, int e) {
     return e & 1 ? __builtin_bit_cast(float, g[e >> 1] & 0xFFFF0000u) : bf16_bits_to_f32(g[e >> 1] & 0xFFFFu);
 }
+
+// LDS of HALF_ODD: a row for every head that the workgroup has at hand
+template <int D, Layout LAYOUT>
+struct Scratch {
+    static constexpr int ROW = D + 8;
+    static constexpr int ELEMS = LAYOUT == HALF_ODD ? kSmallThreads / (D / 16) * ROW : 8;
+};
 
 // The unit's 16 elements after the rotation, in binary32, where they lie in x.  What is not rotated is x itself: infinities there
 // meet no sine.
@@ -61,57 +65,61 @@ struct Rotated {
     float v[2][8];
 };
 template <int D, Layout LAYOUT>
-__device__ __forceinline__ Rotated rotate(const Unit& x, int unit, int rotary_dim, const f32x4* table) {
+__device__ __forceinline__ Rotated rotate(const Unit& x, int unit, int rotary_dim, const f32x4* table, uint16_t* scratch) {
     constexpr int UNITS = D / 16;
     Rotated y;
+    if constexpr (LAYOUT == HALF_ODD) {
+        // The lanes of a head leave their elements in LDS, each takes its elements' partners from there.  All are of one wave.
+        uint16_t* const row = scratch + threadIdx.x / UNITS * Scratch<D, LAYOUT>::ROW;
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const f32x4 cs = table[j * UNITS + unit];
+        for (int w = 0; w < 2; ++w) *reinterpret_cast<u32x4*>(row + unit * 16 + w * 8) = x.g[w];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const int half = rotary_dim / 2;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int p = 2 * j + k;  // of the unit's 8 pairs
-            const int w0 = LAYOUT == INTERLEAVED ? p / 4 : 0, e0 = LAYOUT == INTERLEAVED ? p % 4 * 2 : p;
-            const int w1 = LAYOUT == INTERLEAVED ? p / 4 : 1, e1 = LAYOUT == INTERLEAVED ? p % 4 * 2 + 1 : p;
-            const float a = element(x.g[w0], e0), b = element(x.g[w1], e1), c = cs[2 * k], s = cs[2 * k + 1];
-            const bool turns = unit * 8 + p < rotary_dim / 2;
-            y.v[w0][e0] = turns ? __builtin_fmaf(a, c, -(b * s)) : a;
-            y.v[w1][e1] = turns ? __builtin_fmaf(b, c, a * s) : b;
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = unit * 16 + w * 8 + e;
+                const bool turns = i < rotary_dim, first = i < half;
+                const int p = !turns ? 0 : first ? i : i - half;
+                const f32x2 cs = reinterpret_cast<const f32x2*>(table)[(p % 8 / 2 * UNITS + p / 8) * 2 + p % 2];
+                const float a = element(x.g[w], e), b = bf16_bits_to_f32(row[!turns ? i : first ? i + half : p]);
+                y.v[w][e] = turns ? __builtin_fmaf(a, cs[0], first ? -(b * cs[1]) : b * cs[1]) : a;
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f32x4 cs = table[j * UNITS + unit];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int p = 2 * j + k;  // of the unit's 8 pairs
+                const int w0 = LAYOUT == INTERLEAVED ? p / 4 : 0, e0 = LAYOUT == INTERLEAVED ? p % 4 * 2 : p;
+                const int w1 = LAYOUT == INTERLEAVED ? p / 4 : 1, e1 = LAYOUT == INTERLEAVED ? p % 4 * 2 + 1 : p;
+                const float a = element(x.g[w0], e0), b = element(x.g[w1], e1), c = cs[2 * k], s = cs[2 * k + 1];
+                const bool turns = unit * 8 + p < rotary_dim / 2;
+                y.v[w0][e0] = turns ? __builtin_fmaf(a, c, -(b * s)) : a;
+                y.v[w1][e1] = turns ? __builtin_fmaf(b, c, a * s) : b;
+            }
         }
     }
     return y;
 }
 // The same rounded to bf16; what is not rotated keeps its bits.
 template <int D, Layout LAYOUT>
-__device__ __forceinline__ Unit rotate_bf16(const Unit& x, int unit, int rotary_dim, const f32x4* table) {
-    const Rotated y = rotate<D, LAYOUT>(x, unit, rotary_dim, table);
+__device__ __forceinline__ Unit rotate_bf16(const Unit& x, int unit, int rotary_dim, const f32x4* table, uint16_t* scratch) {
+    const Rotated y = rotate<D, LAYOUT>(x, unit, rotary_dim, table, scratch);
     Unit z;
 #pragma unroll
     for (int w = 0; w < 2; ++w)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t both = pack_bf16(y.v[w][2 * i], y.v[w][2 * i + 1]);
-            if constexpr (LAYOUT == INTERLEAVED) {
-                z.g[w][i] = unit * 8 + w * 4 + i < rotary_dim / 2 ? both : x.g[w][i];
-            } else {
-                const uint32_t mask = (unit * 8 + 2 * i < rotary_dim / 2 ? 0x0000FFFFu : 0u) | (unit * 8 + 2 * i + 1 < rotary_dim / 2 ? 0xFFFF0000u : 0u);
-                z.g[w][i] = (both & mask) | (x.g[w][i] & ~mask);
-            }
+        for (int i = 0; i < 4; ++i) {  // rotary_dim is even: both elements of a dword are rotated or neither (HALF: of all)
+            const int first = LAYOUT == HALF ? unit * 16 : unit * 16 + w * 8 + 2 * i;
+            z.g[w][i] = first < rotary_dim ? pack_bf16(y.v[w][2 * i], y.v[w][2 * i + 1]) : x.g[w][i];
         }
     return z;
-}
-
-// element `which`, e of the unit, as a place in its head
-template <Layout LAYOUT>
-__device__ __forceinline__ void store_unit(uint16_t* head, const Unit& x, int unit, int rotary_dim) {
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        if constexpr (LAYOUT == HALF_ODD) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) head[element_of(unit * 8 + e, w, rotary_dim)] = (uint16_t)(x.g[w][e >> 1] >> ((e & 1) * 16));
-        } else {
-            *reinterpret_cast<u32x4*>(head + granule_of<LAYOUT>(unit, w, rotary_dim) * 8) = x.g[w];
-        }
-    }
 }
 
 // Cosines and sines of TOK rows from t0 on, times the amplitude, to LDS: table[row][j][unit] has pairs 2j and 2j + 1 of the unit, so that
@@ -129,29 +137,44 @@ __device__ __forceinline__ void fill_table(const Rotation& rot, const int64_t* p
     }
 }
 
-constexpr int kRopeTokens = 4;
-
 }  // namespace
 
-template <int D, Layout LAYOUT>
+// A workgroup has TOK rows.
+template <int D, int TOK, Layout LAYOUT>
 __global__ __launch_bounds__(kSmallThreads) void ppd_rope_kernel(const RopeParams P) {
-    constexpr int UNITS = D / 16, TOK = kRopeTokens;
+    constexpr int UNITS = D / 16;
     __shared__ f32x4 table[TOK * 4 * UNITS];
+    __shared__ __attribute__((aligned(16))) uint16_t scratch[Scratch<D, LAYOUT>::ELEMS];
     const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    const int unit = threadIdx.x % UNITS, rotary = P.rot.rotary_dim;
+    const int rows = P.T - t0 < TOK ? (int)(P.T - t0) : TOK;
+    int row = 0, head = threadIdx.x / UNITS;
+    auto settle = [&] {  // heads beyond a row's are the next row's
+        while (head >= P.heads) {
+            head -= P.heads;
+            ++row;
+        }
+    };
+    auto load = [&] { return load_unit<LAYOUT>(P.x + (t0 + row) * P.x_stride + head * D, unit, rotary); };
+    settle();
+    Unit x = {};
+    if (row < rows) x = load();
     fill_table<D, TOK>(P.rot, P.positions, t0, P.T, P.sin_sign, table);
     __syncthreads();
-    const int unit = threadIdx.x % UNITS;
-    for (int i = threadIdx.x / UNITS; i < TOK * P.heads; i += kSmallThreads / UNITS) {
-        const int row = i / P.heads, head = i % P.heads;
-        if (t0 + row >= P.T) break;
-        const Unit x = load_unit<LAYOUT>(P.x + (t0 + row) * P.x_stride + head * D, unit, P.rot.rotary_dim);
-        store_unit<LAYOUT>(P.out + (t0 + row) * P.out_stride + head * D, rotate_bf16<D, LAYOUT>(x, unit, P.rot.rotary_dim, table + row * 4 * UNITS), unit, P.rot.rotary_dim);
+    while (row < rows) {
+        const int r = row, h = head;
+        const Unit now = x;
+        head += kSmallThreads / UNITS;
+        settle();
+        if (row < rows) x = load();
+        store_unit<LAYOUT>(P.out + (t0 + r) * P.out_stride + h * D, rotate_bf16<D, LAYOUT>(now, unit, rotary, table + r * 4 * UNITS, scratch), unit, rotary);
     }
 }
 
 // Append of rotated keys, and of values, to the page pool; queries rotated beside.  A workgroup has TOK tokens and one KV head
-// (blockIdx.y < Hkv), whose rows it stages in LDS and writes as ppd_kv_append_kernel does, or kQueryHeads query heads.
+// (blockIdx.x < Hkv), whose rows it stages in LDS and writes as ppd_kv_append_kernel does, or kQueryHeads query heads.
 constexpr int kQueryHeads = 4;
+constexpr int kMaxGridY = 65535;
 template <int D, int TOK, bool FP8, Layout LAYOUT>
 __global__ __launch_bounds__(kSmallThreads) void ppd_rotated_append_kernel(const RotatedAppendParams P) {
     using Elem = std::conditional_t<FP8, uint8_t, uint16_t>;
@@ -161,11 +184,13 @@ __global__ __launch_bounds__(kSmallThreads) void ppd_rotated_append_kernel(const
     __shared__ f32x4 table[TOK * 4 * UNITS];
     __shared__ __attribute__((aligned(16))) Elem sk[TOK * KROW];
     __shared__ __attribute__((aligned(16))) uint16_t sv[(TOK + 7) * VROW];
+    __shared__ __attribute__((aligned(16))) uint16_t scratch[Scratch<D, LAYOUT>::ELEMS];
     const int tid = threadIdx.x;
-    const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    const int64_t t0 = ((int64_t)blockIdx.z * kMaxGridY + blockIdx.y) * TOK;
     const int rotary = P.rot.rotary_dim;
-    if ((int)blockIdx.y >= P.Hkv) {
-        const int head0 = ((int)blockIdx.y - P.Hkv) * kQueryHeads, unit = tid % UNITS;
+    if (t0 >= P.T) return;
+    if ((int)blockIdx.x >= P.Hkv) {
+        const int head0 = ((int)blockIdx.x - P.Hkv) * kQueryHeads, unit = tid % UNITS;
         constexpr int STEP = kSmallThreads / UNITS, ROUNDS = (TOK * kQueryHeads + STEP - 1) / STEP;
         Unit x[ROUNDS];
         bool there[ROUNDS];
@@ -181,21 +206,21 @@ __global__ __launch_bounds__(kSmallThreads) void ppd_rotated_append_kernel(const
         for (int r = 0; r < ROUNDS; ++r) {
             const int i = tid / UNITS + r * STEP, row = i / kQueryHeads, head = head0 + i % kQueryHeads;
             if (there[r])
-                store_unit<LAYOUT>(P.q_out + ((t0 + row) * P.Hq + head) * D, rotate_bf16<D, LAYOUT>(x[r], unit, rotary, table + row * 4 * UNITS), unit, rotary);
+                store_unit<LAYOUT, true>(P.q_out + ((t0 + row) * P.Hq + head) * D, rotate_bf16<D, LAYOUT>(x[r], unit, rotary, table + row * 4 * UNITS, scratch), unit, rotary);
         }
         return;
     }
     // K: the first threads, 8 pairs each; V: the last ones, a granule each
     constexpr int KUNITS = TOK * UNITS, VGRANULES = TOK * GR;
     static_assert(KUNITS <= kSmallThreads && VGRANULES <= kSmallThreads, "a round of loads");
-    const int kh = blockIdx.y, krow = tid / UNITS, unit = tid % UNITS;
+    const int kh = blockIdx.x, krow = tid / UNITS, unit = tid % UNITS;
     const int vg = kSmallThreads - 1 - tid, vrow = vg / GR;
     Unit xk;
     u32x4 xv = {0, 0, 0, 0};
     const bool has_k = tid < KUNITS && t0 + krow < P.T, has_v = vg < VGRANULES;
     if (has_k) xk = load_unit<LAYOUT>(P.k + (t0 + krow) * P.k_stride + kh * D, unit, rotary);
     if (has_v && t0 + vrow < P.T) xv = APPEND_LOAD(reinterpret_cast<const u32x4*>(P.v + (t0 + vrow) * P.v_stride + kh * D + vg % GR * 8));
-    const AppendWindow w = append_window<TOK>(P.slots, t0, P.T, P.num_pages, blockIdx.y == 0, P.err_flags);
+    const AppendWindow w = append_window<TOK>(P.slots, t0, P.T, P.num_pages, blockIdx.x == 0, P.err_flags);
     if (tid < w.extra * GR)
         *reinterpret_cast<u32x4*>(sv + (TOK + tid / GR) * VROW + (tid % GR) * 8) =
             APPEND_LOAD(reinterpret_cast<const u32x4*>(P.v + (t0 + TOK + tid / GR) * P.v_stride + kh * D + (tid % GR) * 8));
@@ -205,21 +230,16 @@ __global__ __launch_bounds__(kSmallThreads) void ppd_rotated_append_kernel(const
     if (has_k) {
         Elem* const row = sk + krow * KROW;
         if constexpr (FP8) {
-            const Rotated y = rotate<D, LAYOUT>(xk, unit, rotary, table + krow * 4 * UNITS);
+            const Rotated y = rotate<D, LAYOUT>(xk, unit, rotary, table + krow * 4 * UNITS, scratch);
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
                 u32x2 codes;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) codes[i] = e4m3_codes(y.v[g][4 * i], y.v[g][4 * i + 1], y.v[g][4 * i + 2], y.v[g][4 * i + 3], P.inv_k);
-                if constexpr (LAYOUT == HALF_ODD) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) row[element_of(unit * 8 + e, g, rotary)] = (uint8_t)(codes[e >> 2] >> ((e & 3) * 8));
-                } else {
-                    *reinterpret_cast<u32x2*>(row + granule_of<LAYOUT>(unit, g, rotary) * 8) = codes;
-                }
+                *reinterpret_cast<u32x2*>(row + granule_of<LAYOUT>(unit, g, rotary) * 8) = codes;
             }
         } else {
-            store_unit<LAYOUT>(row, rotate_bf16<D, LAYOUT>(xk, unit, rotary, table + krow * 4 * UNITS), unit, rotary);
+            store_unit<LAYOUT>(row, rotate_bf16<D, LAYOUT>(xk, unit, rotary, table + krow * 4 * UNITS, scratch), unit, rotary);
         }
     }
     __syncthreads();
@@ -256,7 +276,9 @@ void by_layout(const Rotation& rot, F go) {
 template <int D, int TOK, bool FP8>
 void append_launch(const RotatedAppendParams& p, hipStream_t hs) {
     const unsigned queries = p.q ? (unsigned)(p.Hq + kQueryHeads - 1) / kQueryHeads : 0u;
-    const dim3 grid((unsigned)((p.T + TOK - 1) / TOK), (unsigned)p.Hkv + queries);
+    // the heads of a token beside each other: their rows lie together
+    const int64_t tiles = (p.T + TOK - 1) / TOK;
+    const dim3 grid((unsigned)p.Hkv + queries, (unsigned)(tiles < kMaxGridY ? tiles : kMaxGridY), (unsigned)((tiles + kMaxGridY - 1) / kMaxGridY));
     by_layout(p.rot, [&](auto layout) { hipLaunchKernelGGL((ppd_rotated_append_kernel<D, TOK, FP8, decltype(layout)::value>), grid, dim3(kSmallThreads), 0, hs, p); });
 }
 
@@ -264,11 +286,14 @@ void append_launch(const RotatedAppendParams& p, hipStream_t hs) {
 
 int launch_rope(const RopeParams& p, int head_dim, void* stream) {
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    const dim3 grid((unsigned)((p.T + kRopeTokens - 1) / kRopeTokens));
+    // Four rows to a workgroup share its start and ask for the next while one is worked; few rows have workgroups to gain.
+    const bool wide = p.T >= 2048;
+    const dim3 grid((unsigned)(wide ? (p.T + 3) / 4 : p.T));
     by_layout(p.rot, [&](auto layout) {
         constexpr Layout LAYOUT = decltype(layout)::value;
-        if (head_dim == 128) hipLaunchKernelGGL((ppd_rope_kernel<128, LAYOUT>), grid, dim3(kSmallThreads), 0, hs, p);
-        else hipLaunchKernelGGL((ppd_rope_kernel<64, LAYOUT>), grid, dim3(kSmallThreads), 0, hs, p);
+        auto* const kernel = head_dim == 128 ? (wide ? &ppd_rope_kernel<128, 4, LAYOUT> : &ppd_rope_kernel<128, 1, LAYOUT>)
+                                             : (wide ? &ppd_rope_kernel<64, 4, LAYOUT> : &ppd_rope_kernel<64, 1, LAYOUT>);
+        hipLaunchKernelGGL(kernel, grid, dim3(kSmallThreads), 0, hs, p);
     });
     return (int)hipGetLastError();
 }
