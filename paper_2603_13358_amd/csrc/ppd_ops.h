@@ -67,25 +67,9 @@ struct TreePlan {
     int32_t rows = 0, join_cols = 0;
 };
 
-// What a kind of tile costs, in keys' time: `start_keys` is its start and end, `join_keys` the launch that joins partials and
-// `column_keys` a column of a partial, written and read again.  `slots` tiles are resident.
-struct TileKind {
-    int32_t max_chunk, step;
-    double start_keys, join_keys, column_keys;
-    int32_t slots;
-};
-
-// A sequence's key range: `tiles` tiles of `cols` query columns each have it, for every KV head.  `start_keys`: of them, beyond their kind's;
-// `partial`: its columns are joined with others', also where it is not cut.
-struct KeyRange {
-    int64_t keys;
-    int32_t tiles, cols;
-    double start_keys = 0;
-    bool partial = false;
-};
-
-// Keys per tile, about: every sequence's range is cut evenly into as many tiles as this needs.  *time: of the launch, in keys.
-int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, int32_t heads, double* time = nullptr);
+// How long tiles of these times take, the longest first and each where there is room next.  One KV head's tiles on its share of the slots:
+// the heads are alike.  `tiles` is sorted.
+double last_tile_end(std::vector<double>& tiles, int32_t slots);
 
 // Builds the tile list of a tree or weighted attention call, whose lengths the caller has checked; false if it has more than kMaxTiles tiles.
 bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int32_t B, bool weighted, int kv_elem_bytes, int num_cus, TreePlan* plan);

@@ -26,24 +26,19 @@ struct PrefixItem {
 // Waves of a tile that have the same columns, each with every waves-th slab of the keys.
 constexpr int prefix_key_waves(int ncols) { return ncols <= 32 ? 4 : ncols <= 64 ? 2 : 1; }
 
-// What a tile costs, in the time that one of few columns takes for a key: a key, and its start beyond theirs.
-struct TileCost { double key, start; };
-constexpr TileCost prefix_tile_cost(int ncols) {
-    return prefix_key_waves(ncols) == 4 ? TileCost{1.0, 0.0} : prefix_key_waves(ncols) == 2 ? TileCost{0.85, 200.0} : TileCost{1.65, 300.0};
-}
-
 // Partials of some columns: `nsplit` of ncols * D floats, the sums, then [ncols] (m, l) pairs, one behind the other, and behind these the next
-// KV head's.  The sums are [ncols][D] where they come from a row block; else [4 columns][D / 4][column][4], fewer columns in the last.
+// KV head's.  The sums are [ncols][D], or, of a tile whose waves have columns of their own, [4 columns][D / 4][column][4], fewer in the last.
 struct JoinSource {
     int64_t part_off;
     int32_t ncols, col0;       // col0: where the unit's first column is among them
     int32_t nsplit, by_rows;
 };
 
-// Rows whose columns have the same sources.
+// Rows whose columns have the same sources: those from the unit's number times `source_stride` on, so that unit and sources are asked for at
+// once.
 struct JoinUnit {
     int32_t grow0, nrows;
-    int32_t source0, nsources;
+    int32_t nsources, unused;
 };
 
 struct PrefixPlan {
@@ -53,12 +48,13 @@ struct PrefixPlan {
     std::vector<JoinSource> sources;
     int64_t partial_floats = 0;
     int32_t join_cols = 0;                 // most columns of a unit
+    int32_t source_stride = 0;             // most sources of one
     int64_t keys_read = 0, keys_alone = 0; // keys per KV head that tiles are over, and without sharing
 };
 
 // Builds the tile list of a prefix attention call, whose arguments the caller has checked (shared[i] of sequence i > 0: tokens it has in
 // common with the one before, at most what either has cached); false if it has more than kMaxTiles tiles.
-bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t* L, const int32_t* n, int32_t B, int num_cus, PrefixPlan* plan);
+bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t* L, const int32_t* n, int32_t B, int kv_elem_bytes, int num_cus, PrefixPlan* plan);
 
 struct PrefixParams {
     const uint16_t* q;
@@ -75,7 +71,7 @@ struct PrefixParams {
     int32_t max_pages;
     int32_t Hq, Hkv, G, invG;  // invG = 65536 / G + 1: col / G == (col * invG) >> 16
     int32_t n_items, n_units;
-    int32_t join_cols;
+    int32_t join_cols, source_stride;
     float scale_log2e;         // softmax scale * log2(e), times the K scale of FP8 pages
     float v_scale;
 };

@@ -76,7 +76,7 @@ void put(char* to, const std::vector<T>& v) {
 // Builds the plan, grows the workspace and enqueues the upload.
 ppd_status upload_prefix_plan(ppd_ctx* ctx, PrefixState* t, const int32_t* shared, const int32_t* L, const int32_t* n, int32_t B, hipStream_t hs) {
     t->on_device = false;
-    if (!ppd::build_prefix_plan(ctx->shape, shared, L, n, B, ctx->num_cus, &t->plan)) return fail(ctx, PPD_ERR_RANGE, "the batch has more tiles than one launch takes");
+    if (!ppd::build_prefix_plan(ctx->shape, shared, L, n, B, ctx->fp8_pages ? 1 : 2, ctx->num_cus, &t->plan)) return fail(ctx, PPD_ERR_RANGE, "the batch has more tiles than one launch takes");
     const ppd::PrefixPlan& plan = t->plan;
     const PlanLayout at(plan);
     Staging* sg = nullptr;
@@ -168,6 +168,7 @@ ppd_status prefix_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pag
     p.n_items = (int32_t)plan.items.size();
     p.n_units = (int32_t)plan.units.size();
     p.join_cols = plan.join_cols;
+    p.source_stride = plan.source_stride;
     // Strictly positive, so that a scale of 0 gives 2^(-inf * c) = 0 for keys that are not seen.
     p.scale_log2e = std::max(1e-30f, (float)((double)scale * (double)ctx->k_scale * 1.4426950408889634));
     p.v_scale = ctx->v_scale;

@@ -184,7 +184,8 @@ struct Lane {
                 }
         }
     }
-    // Waves that have the same columns meet in LDS, kStageCols columns at a time; the result leaves as a partial (partial_at) or as the rows'.
+    // Waves that have the same columns meet in LDS, kStageCols columns at a time; the result leaves as a partial, column after column, or as the
+    // rows'.
     template <int KEY_WAVES>
     __device__ __forceinline__ void finish(const Columns<HD>& acc, float* stage, f32x2* stage_ml) const {
         constexpr int ROW = HD + 4;  // the padding spreads the columns over the banks
@@ -207,9 +208,7 @@ struct Lane {
             for (int block = 0; block < BLOCKS; ++block) {
                 const int left = it.ncols - block * 32 - c0, cols = left < kStageCols ? left : kStageCols;
                 for (int idx = tid; idx < cols * (HD / 4); idx += kPrefixThreads) {
-                    // in the order in which partials lie, or results
-                    const int four = idx / HD * 4, width = cols - four < 4 ? cols - four : 4;
-                    const int cl = it.part_off >= 0 ? four + idx % HD % width : idx / (HD / 4), d = (it.part_off >= 0 ? idx % HD / width : idx % (HD / 4)) * 4;
+                    const int cl = idx / (HD / 4), d = idx % (HD / 4) * 4;
                     const int cc = block * 32 + c0 + cl;
                     float mm = NEG_INF;
 #pragma unroll
@@ -227,7 +226,7 @@ struct Lane {
                     }
                     if (it.part_off >= 0) {
                         float* to = P.partials + it.part_off;
-                        *reinterpret_cast<f32x4*>(to + partial_at<HD>(it.ncols, cc, d)) = o;
+                        *reinterpret_cast<f32x4*>(to + cc * HD + d) = o;
                         if (d == 0) *reinterpret_cast<f32x2*>(to + it.ncols * HD + cc * 2) = f32x2{mm, l};
                     } else {
                         store_result(cc, d, o, l);
@@ -536,8 +535,8 @@ __global__ __launch_bounds__(256) void ppd_prefix_join_kernel(const PrefixParams
     __shared__ f32x4 other[256];
     const JoinUnit u = P.units[blockIdx.x];
     const int tid = threadIdx.x, kvh = blockIdx.y, col0 = (int)blockIdx.z * COLS, cols = u.nrows * P.G - col0 < COLS ? u.nrows * P.G - col0 : COLS;
+    if (tid < P.source_stride) sources[tid] = P.sources[(int64_t)blockIdx.x * P.source_stride + tid];
     if (cols <= 0) return;
-    if (tid < u.nsources) sources[tid] = P.sources[u.source0 + tid];
     __syncthreads();
     int parts = 0;
     for (int i = 0; i < u.nsources; ++i) parts += sources[i].nsplit;
@@ -572,6 +571,7 @@ __global__ __launch_bounds__(256) void ppd_prefix_join_kernel(const PrefixParams
         auto ask = [&](int j0) {
 #pragma unroll
             for (int t = 0; t < AT_ONCE; ++t) {
+                if (j0 - mine + t * share >= count) break;  // for all threads alike; where it is for some, the first one's again
                 const int j = j0 + t * share < count ? j0 + t * share : 0;
                 const int cc = part_col0[j] + cl;
                 v[t] = *reinterpret_cast<const f32x4*>(P.partials + part_at[j] + (part_cols[j] < 0 ? cc * HD + d : partial_at<HD>(part_cols[j], cc, d)));

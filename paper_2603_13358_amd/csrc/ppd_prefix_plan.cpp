@@ -1,5 +1,6 @@
 // Tile list of attention over shared prefixes: which rows meet which keys in which workgroup, and whose partials make a row's result.
 #include <algorithm>
+#include <cmath>
 #include <tuple>
 
 #include "ppd_prefix.h"
@@ -15,10 +16,80 @@ struct Segment {
     bool own;
 };
 
-// Time of the tiles that have `cols` columns, for a key.
-double key_time(int64_t cols) {
-    const int64_t full = cols / kPrefixCols;
-    return full * prefix_tile_cost(kPrefixCols).key + (cols % kPrefixCols ? prefix_tile_cost((int)(cols % kPrefixCols)).key : 0);
+int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
+
+// What a tile takes, ns: its start and end, and a key while memory keeps up.  Measured over whole launches at D = 128 (start and end 3.6-4.2
+// us and 1.2 us for four slabs of few columns, 5-6 us and 0.98 us a slab of 128 columns on bf16 pages, 1.09 on FP8; row blocks 6.6 us and 1.2 us
+// for 64 keys); D = 64 by its share of the work.
+struct TileTime { double start, key; };
+TileTime tile_time(int ncols, int head_dim, int kv_elem_bytes) {
+    const int waves = prefix_key_waves(ncols);
+    const double half = head_dim == 64 ? 0.7 : 1.0;
+    if (waves == 4) return {3600, 10 * half};
+    if (waves == 2) return {6000, 20 * half};
+    return {5500, (kv_elem_bytes == 1 ? 34 : 31) * half};
+}
+constexpr TileTime kRowBlockTime = {6600, 19};
+// Over 19 batches (2 to 256 sequences, 300 to 60000 shared tokens) starts of 9 and 13 us for 128 columns, partials at 2.5 TB/s and reading added
+// to the tiles' time in part gave the same on average within 1 %; keys' times and starts that knew no bound by memory 2 % more.
+constexpr double kBytesPerNs = 6000, kPartialBytesPerNs = 4000, kJoinNs = 5000;
+
+// Work that tiles are made of: `tiles` column ranges of `cols` columns each go over `keys` keys, for every KV head.
+struct Range {
+    int64_t keys;
+    int32_t tiles, cols, max_keys;
+    TileTime time;
+    bool partial;  // its columns are joined with others', also where it is not cut
+};
+
+int32_t pieces_of(const Range& r, double slice) { return std::max(ceil_div(r.keys, r.max_keys), (int32_t)std::ceil(r.keys * r.time.key / slice)); }
+
+// The time of keys, ns, at which ranges are cut, and *time of the launch: fewer tiles start less often and leave fewer partials, more fill the
+// slots more evenly; and K and V have to be read, if only once for the column ranges side by side.
+double choose_slice(const std::vector<Range>& ranges, int32_t heads, int32_t slots, int head_dim, int kv_elem_bytes, double* time) {
+    double longest = 0, bytes = 0, best = -1, slice = 0;
+    for (const Range& r : ranges) {
+        longest = std::max(longest, r.keys * r.time.key);
+        bytes += (double)r.keys * 2 * head_dim * kv_elem_bytes * heads;
+    }
+    const int32_t share = std::max(1, slots / heads);
+    std::vector<double> tiles;
+    for (double c = longest + 1; c >= 1000; c *= 0.84) {
+        double count = 0, sum = 0, most = 0, joined = 0;
+        for (const Range& r : ranges) {
+            const double pieces = pieces_of(r, c), cost = r.keys * r.time.key / pieces + r.time.start;
+            count += pieces * r.tiles;
+            sum += pieces * r.tiles * cost;
+            most = std::max(most, cost);
+            if (pieces > 1 || r.partial) joined += pieces * r.tiles * r.cols * heads;
+        }
+        if (count * heads > kMaxTiles) break;
+        double est = count <= share ? most : sum / share + 0.5 * most;
+        if (count > share && count <= 4.0 * share) {
+            tiles.clear();
+            for (const Range& r : ranges) {
+                const int64_t pieces = pieces_of(r, c);
+                tiles.insert(tiles.end(), (size_t)(pieces * r.tiles), r.keys * r.time.key / pieces + r.time.start);
+            }
+            est = last_tile_end(tiles, share);
+        }
+        const double moved = joined * (head_dim + 2) * 4 / kPartialBytesPerNs;  // written, and read by the join
+        est = std::max(est, bytes / kBytesPerNs + 4000) + moved + (joined > 0 ? kJoinNs + moved : 0);
+        if (best < 0 || est < best) {
+            best = est;
+            slice = c;
+        }
+        if (count > 16.0 * share) break;
+    }
+    *time = std::max(0.0, best);
+    return slice > 0 ? slice : longest + 1;
+}
+
+// A tile's keys in throughput, relative to those of few columns.
+double key_cost(int64_t cols) {
+    const int64_t full = cols / kPrefixCols, rest = cols % kPrefixCols;
+    auto one = [](int64_t c) { return prefix_key_waves((int)c) == 4 ? 1.0 : prefix_key_waves((int)c) == 2 ? 0.85 : 1.65; };
+    return full * one(kPrefixCols) + (rest ? one(rest) : 0);
 }
 
 // The shared ranges of sequences [lo, hi] from key `start` on, and their own ends.  common[i] is what sequence i has in common with the one
@@ -41,11 +112,11 @@ public:
         double apart = -0.5;
         for (int32_t from = lo; from <= hi;) {
             const int32_t to = run_end(from, hi, least);
-            apart += key_time(columns(from, to)) + 0.5;
+            apart += key_cost(columns(from, to)) + 0.5;
             from = to + 1;
         }
         const int64_t cols = columns(lo, hi);
-        if ((least - start) * (apart - key_time(cols)) > 3.7 * cols + 200) {
+        if ((least - start) * (apart - key_cost(cols)) > 3.7 * cols + 200) {
             list.push_back({lo, hi, start, least, false});
             start = least;
             ++level;
@@ -69,8 +140,6 @@ private:
     const std::vector<int32_t>& row0_;
     int G_;
 };
-
-int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
 
 // The longest tiles first, and those of the same keys (the column ranges of one segment, head and piece) one after the other on one XCD:
 // workgroups go round the XCDs, each of which has an L2 of its own.
@@ -101,7 +170,7 @@ void order_for_xcds(std::vector<Item>& items, Time time) {
 
 }  // namespace
 
-bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t* L, const int32_t* n, int32_t B, int num_cus, PrefixPlan* plan) {
+bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t* L, const int32_t* n, int32_t B, int kv_elem_bytes, int num_cus, PrefixPlan* plan) {
     const int G = s.num_q_heads / s.num_kv_heads, Hkv = s.num_kv_heads, D = s.head_dim;
     *plan = PrefixPlan();
     std::vector<int32_t> common(B, 0), row0(B + 1, 0);
@@ -112,14 +181,13 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
     }
     auto rows_of = [&](const Segment& g) { return row0[g.hi + 1] - row0[g.lo]; };
     // How a segment is cut: `tiles` column ranges of `rows` rows each.
-    struct Cut { bool is_wide; int32_t tiles, rows, key_waves; TileCost cost; };
+    struct Cut { bool is_wide; int32_t tiles, rows, key_waves; TileTime time; };
     // A list of segments, how it is cut and its time.  Row blocks are a launch of their own: where a sequence has more columns than a tile
     // takes there is one, and it takes all segments of more than 32 columns.
     struct Choice {
         std::vector<Segment> segments;
         bool any_wide = false, possible = true;
-        int32_t narrow_chunk = 0, wide_chunk = 0;
-        double time = 0;
+        double narrow_slice = 0, wide_slice = 0, time = 0;
     };
     auto cut_of = [&](const Choice& x, const Segment& g) {
         const int32_t rows = rows_of(g);
@@ -129,27 +197,25 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
         c.tiles = ceil_div(rows, most);
         c.rows = ceil_div(rows, c.tiles);
         c.key_waves = prefix_key_waves(std::min<int32_t>(c.rows * G, kPrefixCols));
-        c.cost = c.is_wide ? TileCost{1, 0} : prefix_tile_cost(c.rows * G);
+        c.time = c.is_wide ? kRowBlockTime : tile_time(c.rows * G, D, kv_elem_bytes);
         return c;
     };
     auto weigh = [&](Choice& x) {
-        const TileKind narrow = {kMaxPrefixChunk * 2, kTreeStep, 200, 256, 0.012, 2 * num_cus};
-        const TileKind wide = {kMaxTreeBlockChunk, kTileTokens, 350, 500, 0.0114, num_cus};
         for (const Segment& g : x.segments) x.any_wide |= g.own && (int64_t)rows_of(g) * G > kPrefixCols;
         double fewest = 0;
-        std::vector<KeyRange> narrow_ranges, wide_ranges;
+        std::vector<Range> narrow, wide;
         for (const Segment& g : x.segments) {
             const Cut c = cut_of(x, g);
-            const int64_t keys = g.end - g.begin;
-            (c.is_wide ? wide_ranges : narrow_ranges).push_back({(int64_t)(keys * c.cost.key) + 1, c.tiles, c.rows * G, c.cost.start, !g.own || g.begin > 0});
-            fewest += (double)c.tiles * Hkv * ((double)keys / (c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk) + 1);
+            const int32_t max_keys = c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk;
+            (c.is_wide ? wide : narrow).push_back({g.end - g.begin, c.tiles, c.rows * G, max_keys, c.time, !g.own || g.begin > 0});
+            fewest += (double)c.tiles * Hkv * ((double)(g.end - g.begin) / max_keys + 1);
         }
         x.possible = fewest <= kMaxTiles;
         if (!x.possible) return;
-        double time = 0;
-        if (!narrow_ranges.empty()) x.narrow_chunk = choose_chunk(narrow, narrow_ranges, Hkv, &time);
-        x.time = time;
-        if (!wide_ranges.empty()) x.wide_chunk = choose_chunk(wide, wide_ranges, Hkv, &time), x.time += time;
+        double narrow_time = 0, wide_time = 0;
+        if (!narrow.empty()) x.narrow_slice = choose_slice(narrow, Hkv, 2 * num_cus, D, kv_elem_bytes, &narrow_time);
+        if (!wide.empty()) x.wide_slice = choose_slice(wide, Hkv, num_cus, D, kv_elem_bytes, &wide_time);
+        x.time = narrow_time + wide_time;
     };
     Choice choice;
     {
@@ -173,7 +239,8 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
     if (!choice.possible) return false;
 
     // Sources of the rows, in the order of the segments: a sequence's shared ranges come before its own end.
-    struct Placed { int32_t row0, rows, tile_rows, nsplit; bool by_rows; int64_t part_off; };
+    std::vector<std::vector<JoinSource>> unit_sources;
+    struct Placed { int32_t row0, rows, tile_rows, nsplit; bool is_wide; int64_t part_off; };
     std::vector<Placed> path;  // of the segment at hand: the shared ranges around it
     std::vector<const Segment*> around;
     for (const Segment& g : choice.segments) {
@@ -184,8 +251,7 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
         const Cut c = cut_of(choice, g);
         const int32_t keys = g.end - g.begin, total_rows = rows_of(g);
         const int32_t step = c.is_wide ? kTileTokens : kSlab * c.key_waves, most = c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk;
-        const int32_t chunk = std::max(step, std::min(most, (int32_t)((c.is_wide ? choice.wide_chunk : choice.narrow_chunk) / c.cost.key)));
-        const int32_t pieces = ceil_div(keys, chunk);
+        const int32_t pieces = pieces_of({keys, 0, 0, most, c.time, false}, c.is_wide ? choice.wide_slice : choice.narrow_slice);
         const int32_t piece = std::min(most, ceil_div(ceil_div(keys, pieces), step) * step);
         const int32_t nsplit = ceil_div(keys, piece);
         const bool direct = g.own && around.empty() && nsplit == 1;
@@ -231,18 +297,28 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
         for (int32_t r = row0[g.lo]; r < row0[g.lo + 1];) {
             int32_t end = row0[g.lo + 1];
             for (const Placed& x : path) end = std::min(end, x.row0 + ((r - x.row0) / x.tile_rows + 1) * x.tile_rows);
-            plan->units.push_back({r, end - r, (int32_t)plan->sources.size(), (int32_t)path.size()});
+            plan->units.push_back({r, end - r, (int32_t)path.size(), 0});
+            unit_sources.emplace_back();
+            plan->source_stride = std::max(plan->source_stride, (int32_t)path.size());
             plan->join_cols = std::max(plan->join_cols, (end - r) * G);
             for (const Placed& x : path) {
                 const int32_t tile = (r - x.row0) / x.tile_rows, first = tile * x.tile_rows;
                 const int32_t cols = std::min(x.tile_rows, x.rows - first) * G;
-                plan->sources.push_back({x.part_off + (int64_t)first * G * (D + 2) * x.nsplit * Hkv, cols, (r - x.row0 - first) * G, x.nsplit, x.by_rows});
+                unit_sources.back().push_back({x.part_off + (int64_t)first * G * (D + 2) * x.nsplit * Hkv, cols, (r - x.row0 - first) * G, x.nsplit, x.is_wide || prefix_key_waves(cols) > 1});
             }
             r = end;
         }
         path.pop_back();
     }
-    order_for_xcds(plan->items, [](const PrefixItem& x) { return (int64_t)((x.kv_end - x.kv_begin) * prefix_tile_cost(x.ncols).key + prefix_tile_cost(x.ncols).start); });
+    plan->sources.reserve(unit_sources.size() * plan->source_stride);
+    for (auto& of_unit : unit_sources) {
+        of_unit.resize(plan->source_stride, JoinSource{});
+        plan->sources.insert(plan->sources.end(), of_unit.begin(), of_unit.end());
+    }
+    order_for_xcds(plan->items, [&](const PrefixItem& x) { 
+        const TileTime t = tile_time(x.ncols, D, kv_elem_bytes);
+        return (int64_t)((x.kv_end - x.kv_begin) * t.key + t.start);
+    });
     order_for_xcds(plan->blocks, [](const ppd_work_item& x) { return (int64_t)(x.kv_end - x.kv_begin); });
     return true;
 }

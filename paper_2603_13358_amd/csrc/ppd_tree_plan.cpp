@@ -8,11 +8,24 @@ namespace ppd {
 
 namespace {
 
+// What a kind of tile costs, in keys' time: `start_keys` is its start and end, `join_keys` the launch that joins partials and
+// `column_keys` a column of a partial, written and read again.  `slots` tiles are resident.
+struct TileKind {
+    int32_t max_chunk, step;
+    double start_keys, join_keys, column_keys;
+    int32_t slots;
+};
+
+// A sequence's key range: `tiles` tiles of `cols` query columns each have it, for every KV head.
+struct KeyRange {
+    int32_t keys, tiles, cols;
+};
+
 // Rounded up; the sum may pass 32 bits.
 int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
 
-// How long the tiles take, the longest first and each where there is room next.  One KV head's tiles on its share of the slots: the
-// heads are alike.
+}  // namespace
+
 double last_tile_end(std::vector<double>& tiles, int32_t slots) {
     std::sort(tiles.begin(), tiles.end(), std::greater<double>());
     std::vector<double> ends;  // heap, the earliest on top
@@ -29,26 +42,27 @@ double last_tile_end(std::vector<double>& tiles, int32_t slots) {
     return *std::max_element(ends.begin(), ends.end());
 }
 
-}  // namespace
+namespace {
 
-// Fewer tiles start less often and leave fewer partials, more fill the slots more evenly.  Up to four rounds the tiles are laid out to
-// see how long they take; many short ones last about their even share and half of the longest.
-int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, int32_t heads, double* time) {
-    int64_t longest = 1;
+// Keys per tile, about: every sequence's range is cut evenly into as many tiles as this needs.  Fewer tiles start less often and leave
+// fewer partials, more fill the slots more evenly.  Up to four rounds the tiles are laid out to see how long they take; many short
+// ones last about their even share and half of the longest.
+int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, int32_t heads) {
+    int32_t longest = 1;
     for (const auto& r : ranges) longest = std::max(longest, r.keys);
     const int32_t slots = std::max(1, kind.slots / heads);
     int32_t chunk = kind.max_chunk;
     double best = -1;
     std::vector<double> tiles;
-    for (double c = std::min<double>(kind.max_chunk, (double)longest); c >= kind.step; c *= 0.84) {
+    for (double c = std::min<double>(kind.max_chunk, longest); c >= kind.step; c *= 0.84) {
         double count = 0, sum = 0, most = 0, joined = 0;
         for (const auto& r : ranges) {
             const double pieces = (double)ceil_div(r.keys, (int64_t)c);
-            const double cost = r.keys / pieces + kind.start_keys + r.start_keys;
+            const double cost = r.keys / pieces + kind.start_keys;
             count += pieces * r.tiles;
             sum += pieces * r.tiles * cost;
             most = std::max(most, cost);
-            if (pieces > 1 || r.partial) joined += pieces * r.tiles * r.cols;
+            if (pieces > 1) joined += pieces * r.tiles * r.cols;
         }
         if (count * heads > kMaxTiles) break;
         double est = count <= slots ? most : sum / slots + 0.5 * most;
@@ -56,7 +70,7 @@ int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, 
             tiles.clear();
             for (const auto& r : ranges) {
                 const int64_t pieces = ceil_div(r.keys, (int64_t)c);
-                tiles.insert(tiles.end(), (size_t)(pieces * r.tiles), (double)r.keys / pieces + kind.start_keys + r.start_keys);
+                tiles.insert(tiles.end(), (size_t)(pieces * r.tiles), (double)r.keys / pieces + kind.start_keys);
             }
             est = last_tile_end(tiles, slots);
         }
@@ -67,9 +81,10 @@ int32_t choose_chunk(const TileKind& kind, const std::vector<KeyRange>& ranges, 
         }
         if (count > 16.0 * slots) break;
     }
-    if (time) *time = std::max(0.0, best);
     return chunk;
 }
+
+}  // namespace
 
 bool build_tree_plan(const ppd_shape& s, const int32_t* L, const int32_t* n, int32_t B, bool weighted, int kv_elem_bytes, int num_cus, TreePlan* plan) {
     const int G = s.num_q_heads / s.num_kv_heads, Hkv = s.num_kv_heads, D = s.head_dim;

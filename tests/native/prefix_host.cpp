@@ -102,7 +102,7 @@ static void refusals() {
 // Every row meets each of its keys in one tile, the partials lie apart from each other, and the join finds them.
 static void check_plan(const ppd_shape& s, const std::vector<int32_t>& shared, const std::vector<int32_t>& L, const std::vector<int32_t>& n, ppd::PrefixPlan& plan) {
     const int B = (int)L.size(), G = s.num_q_heads / s.num_kv_heads, Hkv = s.num_kv_heads, D = s.head_dim;
-    CHECK(ppd::build_prefix_plan(s, shared.data(), L.data(), n.data(), B, 256, &plan));
+    CHECK(ppd::build_prefix_plan(s, shared.data(), L.data(), n.data(), B, 2, 256, &plan));
     std::vector<int32_t> row0(B + 1, 0), seq;
     for (int i = 0; i < B; ++i) {
         row0[i + 1] = row0[i] + n[i];
@@ -159,12 +159,13 @@ static void check_plan(const ppd_shape& s, const std::vector<int32_t>& shared, c
     std::vector<int> joined(row0[B], 0);
     std::vector<std::vector<int64_t>> found((size_t)row0[B] * Hkv), want = found;
     for (const auto& u : plan.units) {
-        CHECK(u.nrows * G <= plan.join_cols && u.nsources >= 1 && u.source0 + u.nsources <= (int)plan.sources.size());
+        const size_t source0 = (&u - plan.units.data()) * (size_t)plan.source_stride;
+        CHECK(u.nrows * G <= plan.join_cols && u.nsources >= 1 && u.nsources <= plan.source_stride && plan.sources.size() == plan.units.size() * plan.source_stride);
         for (int r = u.grow0; r < u.grow0 + u.nrows; ++r) {
             CHECK(r < row0[B] && !joined[r]++);
             for (int h = 0; h < Hkv; ++h)
                 for (int x = 0; x < u.nsources; ++x) {
-                    const ppd::JoinSource& src = plan.sources[u.source0 + x];
+                    const ppd::JoinSource& src = plan.sources[source0 + x];
                     for (int p = 0; p < src.nsplit; ++p)
                         found[(size_t)r * Hkv + h].push_back(src.part_off + ((int64_t)h * src.nsplit + p) * src.ncols * (D + 2) + (int64_t)(src.col0 + (r - u.grow0) * G) * D);
                     CHECK(src.col0 + u.nrows * G <= src.ncols);
@@ -222,16 +223,16 @@ static void plans() {
         for (int i = 0; i < B; ++i) L[i] = 64 * (down ? B - i : i + 1);
         for (int i = 1; i < B; ++i) shared[i] = std::min(L[i], L[i - 1]);
         ppd::PrefixPlan plan;
-        CHECK(ppd::build_prefix_plan({8, 1, 64, 16, 1 << 20}, shared.data(), L.data(), n.data(), B, 256, &plan));
+        CHECK(ppd::build_prefix_plan({8, 1, 64, 16, 1 << 20}, shared.data(), L.data(), n.data(), B, 2, 256, &plan));
         for (const auto& u : plan.units) CHECK(u.nsources <= ppd::kMaxNested + 1);
     }
     {
         const int B = 70000;
         std::vector<int32_t> shared(B, 0), L(B, 100), n(B, 1);
         ppd::PrefixPlan plan;
-        CHECK(!ppd::build_prefix_plan({64, 64, 64, 16, 1 << 20}, shared.data(), L.data(), n.data(), B, 256, &plan));
+        CHECK(!ppd::build_prefix_plan({64, 64, 64, 16, 1 << 20}, shared.data(), L.data(), n.data(), B, 2, 256, &plan));
         for (int i = 1; i < B; ++i) shared[i] = 64;
-        CHECK(!ppd::build_prefix_plan({64, 64, 64, 16, 1 << 20}, shared.data(), L.data(), n.data(), B, 256, &plan));
+        CHECK(!ppd::build_prefix_plan({64, 64, 64, 16, 1 << 20}, shared.data(), L.data(), n.data(), B, 2, 256, &plan));
     }
     {
         std::vector<int32_t> shared = {0, ppd::kMaxTreeTokens - 9}, L = {ppd::kMaxTreeTokens - 5, ppd::kMaxTreeTokens - 9}, n = {5, 9};
