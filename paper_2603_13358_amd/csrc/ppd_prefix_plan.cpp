@@ -46,12 +46,15 @@ int32_t pieces_of(const Range& r, double slice) { return std::max(ceil_div(r.key
 
 // The time of keys, ns, at which ranges are cut, and *time of the launch: fewer tiles start less often and leave fewer partials, more fill the
 // slots more evenly; and K and V have to be read, if only once for the column ranges side by side.
+double reading_time(double keys, int32_t heads, int head_dim, int kv_elem_bytes) { return keys * 2 * head_dim * kv_elem_bytes * heads / kBytesPerNs + 4000; }
+
 double choose_slice(const std::vector<Range>& ranges, int32_t heads, int32_t slots, int head_dim, int kv_elem_bytes, double* time) {
-    double longest = 0, bytes = 0, best = -1, slice = 0;
+    double longest = 0, keys = 0, best = -1, slice = 0;
     for (const Range& r : ranges) {
         longest = std::max(longest, r.keys * r.time.key);
-        bytes += (double)r.keys * 2 * head_dim * kv_elem_bytes * heads;
+        keys += (double)r.keys;
     }
+    const double reading = reading_time(keys, heads, head_dim, kv_elem_bytes);
     const int32_t share = std::max(1, slots / heads);
     std::vector<double> tiles;
     for (double c = longest + 1; c >= 1000; c *= 0.84) {
@@ -64,6 +67,12 @@ double choose_slice(const std::vector<Range>& ranges, int32_t heads, int32_t slo
             if (pieces > 1 || r.partial) joined += pieces * r.tiles * r.cols * heads;
         }
         if (count * heads > kMaxTiles) break;
+        const double moved = joined * (head_dim + 2) * 4 / kPartialBytesPerNs;  // written, and read by the join
+        const double behind = moved + (joined > 0 ? kJoinNs + moved : 0), least = std::max(std::max(most, sum / share), reading) + behind;
+        if (best >= 0 && least >= best) {
+            if (count > 16.0 * share) break;
+            continue;
+        }
         double est = count <= share ? most : sum / share + 0.5 * most;
         if (count > share && count <= 4.0 * share) {
             tiles.clear();
@@ -73,8 +82,7 @@ double choose_slice(const std::vector<Range>& ranges, int32_t heads, int32_t slo
             }
             est = last_tile_end(tiles, share);
         }
-        const double moved = joined * (head_dim + 2) * 4 / kPartialBytesPerNs;  // written, and read by the join
-        est = std::max(est, bytes / kBytesPerNs + 4000) + moved + (joined > 0 ? kJoinNs + moved : 0);
+        est = std::max(est, reading) + behind;
         if (best < 0 || est < best) {
             best = est;
             slice = c;
@@ -145,18 +153,25 @@ private:
 // workgroups go round the XCDs, each of which has an L2 of its own.
 template <class Item, class Time>
 void order_for_xcds(std::vector<Item>& items, Time time) {
-    auto same_keys = [](const Item& a, const Item& b) { return a.seq == b.seq && a.kvh == b.kvh && a.kv_begin == b.kv_begin && a.kv_end == b.kv_end && a.kv_total == b.kv_total; };
-    std::vector<size_t> index(items.size());
-    for (size_t i = 0; i < items.size(); ++i) index[i] = i;
-    auto key = [&](size_t i) { return std::make_tuple(-time(items[i]), items[i].seq, items[i].kvh, items[i].kv_begin, items[i].kv_total); };
-    std::stable_sort(index.begin(), index.end(), [&](size_t a, size_t b) { return key(a) < key(b); });
-    std::vector<size_t> lists[kXcds];
-    for (size_t i = 0; i < index.size();) {
+    struct Key {
+        int64_t time;
+        int32_t seq, kvh, begin, total;
+        uint32_t index;
+        bool same_keys(const Key& o) const { return seq == o.seq && kvh == o.kvh && begin == o.begin && total == o.total && time == o.time; }
+        bool operator<(const Key& o) const {
+            if (time != o.time) return time > o.time;
+            return std::tie(seq, kvh, begin, total, index) < std::tie(o.seq, o.kvh, o.begin, o.total, o.index);
+        }
+    };
+    std::vector<Key> keys(items.size());
+    for (size_t i = 0; i < items.size(); ++i) keys[i] = {time(items[i]), items[i].seq, items[i].kvh, items[i].kv_begin, items[i].kv_total, (uint32_t)i};
+    std::sort(keys.begin(), keys.end());
+    std::vector<uint32_t> lists[kXcds];
+    for (size_t i = 0; i < keys.size();) {
         size_t to = i + 1;
-        while (to < index.size() && same_keys(items[index[i]], items[index[to]])) ++to;
+        while (to < keys.size() && keys[i].same_keys(keys[to])) ++to;
         auto* const least = std::min_element(lists, lists + kXcds, [](const auto& a, const auto& b) { return a.size() < b.size(); });
-        least->insert(least->end(), index.begin() + i, index.begin() + to);
-        i = to;
+        for (; i < to; ++i) least->push_back(keys[i].index);
     }
     std::vector<Item> ordered;
     ordered.reserve(items.size());
@@ -229,7 +244,8 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
         choice.segments.swap(segments.list);
     }
     weigh(choice);
-    if (choice.segments.size() > (size_t)B) {
+    // (Keys that have to be read anyway, once for each sequence, may already say that it takes longer.)
+    if (choice.segments.size() > (size_t)B && (!choice.possible || reading_time((double)plan->keys_alone, Hkv, D, kv_elem_bytes) < choice.time)) {
         // Nothing shared, and where no range is cut either no join: small batches (three sequences of 231 keys, 200 of them shared, 8.3 -> 5.3 us).
         Choice apart;
         for (int32_t i = 0; i < B; ++i) apart.segments.push_back({i, i, 0, L[i] + n[i], true});
