@@ -222,7 +222,8 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
         for (const Segment& g : x.segments) {
             const Cut c = cut_of(x, g);
             const int32_t max_keys = c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk;
-            (c.is_wide ? wide : narrow).push_back({g.end - g.begin, c.tiles, c.rows * G, max_keys, c.time, !g.own || g.begin > 0});
+            const int64_t keys = g.end - g.begin - (g.own ? (rows_of(g) - c.rows) / 2 : 0);  // on average: a tile's last row sees none behind itself
+            (c.is_wide ? wide : narrow).push_back({keys, c.tiles, c.rows * G, max_keys, c.time, !g.own || g.begin > 0});
             fewest += (double)c.tiles * Hkv * ((double)(g.end - g.begin) / max_keys + 1);
         }
         x.possible = fewest <= kMaxTiles;
@@ -256,8 +257,9 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
 
     // Sources of the rows, in the order of the segments: a sequence's shared ranges come before its own end.
     std::vector<std::vector<JoinSource>> unit_sources;
-    struct Placed { int32_t row0, rows, tile_rows, nsplit; bool is_wide; int64_t part_off; };
-    std::vector<Placed> path;  // of the segment at hand: the shared ranges around it
+    struct PlacedTile { int32_t cols, nsplit; int64_t part_off; };  // a column range's; part_off -1: it writes the result
+    struct Placed { int32_t row0, tile_rows; bool is_wide; std::vector<PlacedTile> tiles; };
+    std::vector<Placed> path;  // the shared ranges around the segment at hand, and itself
     std::vector<const Segment*> around;
     for (const Segment& g : choice.segments) {
         while (!around.empty() && around.back()->hi < g.lo) {
@@ -265,30 +267,33 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
             path.pop_back();
         }
         const Cut c = cut_of(choice, g);
-        const int32_t keys = g.end - g.begin, total_rows = rows_of(g);
+        const int32_t total_rows = rows_of(g);
         const int32_t step = c.is_wide ? kTileTokens : kSlab * c.key_waves, most = c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk;
-        const int32_t pieces = pieces_of({keys, 0, 0, most, c.time, false}, c.is_wide ? choice.wide_slice : choice.narrow_slice);
-        const int32_t piece = std::min(most, ceil_div(ceil_div(keys, pieces), step) * step);
-        const int32_t nsplit = ceil_div(keys, piece);
-        const bool direct = g.own && around.empty() && nsplit == 1;
-        const Placed placed = {row0[g.lo], total_rows, c.rows, nsplit, c.is_wide, plan->partial_floats};
-        plan->keys_read += (int64_t)keys * c.tiles;
+        path.push_back({row0[g.lo], c.rows, c.is_wide, {}});
         for (int32_t r = 0; r < total_rows; r += c.rows) {
             const int32_t nrows = std::min(c.rows, total_rows - r), cols = nrows * G;
+            // its last row sees no keys behind itself
+            const int32_t last = g.own ? std::min(g.end, L[g.lo] + r + nrows) : g.end, keys = last - g.begin;
+            const int32_t pieces = pieces_of({keys, 0, 0, most, c.time, false}, c.is_wide ? choice.wide_slice : choice.narrow_slice);
+            const int32_t piece = std::min(most, ceil_div(ceil_div(keys, pieces), step) * step);
+            const int32_t nsplit = ceil_div(keys, piece);
+            const bool direct = g.own && around.empty() && nsplit == 1;
+            const int32_t cached = g.own ? L[g.lo] + r : g.end;  // the new tokens before the tile's rows are seen by all of them
             const int64_t stride = (int64_t)cols * (D + 2);
+            path.back().tiles.push_back({cols, nsplit, direct ? -1 : plan->partial_floats});
+            plan->keys_read += keys;
             for (int h = 0; h < Hkv; ++h)
                 for (int32_t p = 0; p < nsplit; ++p) {
-                    const int32_t begin = g.begin + p * piece, end = std::min(g.end, begin + piece);
+                    const int32_t begin = g.begin + p * piece, end = std::min(last, begin + piece);
                     const int64_t part = direct ? -1 : plan->partial_floats + ((int64_t)h * nsplit + p) * stride;
                     if (c.is_wide) {
                         ppd_work_item it{};
                         it.kind = 1;
                         it.seq = g.lo;
                         it.kvh = h;
-                        it.row0 = g.own ? r : 0;
                         it.nrows = nrows;
                         it.grow0 = row0[g.lo] + r;
-                        it.L = g.own ? L[g.lo] : g.end;
+                        it.L = cached;
                         it.kv_total = g.end;
                         it.kv_begin = begin;
                         it.kv_end = end;
@@ -296,7 +301,7 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
                         it.part_off = part;
                         plan->blocks.push_back(it);
                     } else {
-                        plan->items.push_back({g.lo, h, row0[g.lo] + r, cols, g.own ? L[g.lo] + r : g.end, g.end, begin, end, part});
+                        plan->items.push_back({g.lo, h, row0[g.lo] + r, cols, cached, g.end, begin, end, part});
                     }
                 }
             if (!direct) plan->partial_floats += stride * nsplit * Hkv;
@@ -304,23 +309,22 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
         }
         if (!g.own) {
             around.push_back(&g);
-            path.push_back(placed);
             continue;
         }
-        if (direct) continue;
         // The sequence's rows, cut where a tile of any of its ranges ends.
-        path.push_back(placed);
         for (int32_t r = row0[g.lo]; r < row0[g.lo + 1];) {
             int32_t end = row0[g.lo + 1];
             for (const Placed& x : path) end = std::min(end, x.row0 + ((r - x.row0) / x.tile_rows + 1) * x.tile_rows);
-            plan->units.push_back({r, end - r, (int32_t)path.size(), 0});
-            unit_sources.emplace_back();
-            plan->source_stride = std::max(plan->source_stride, (int32_t)path.size());
-            plan->join_cols = std::max(plan->join_cols, (end - r) * G);
-            for (const Placed& x : path) {
-                const int32_t tile = (r - x.row0) / x.tile_rows, first = tile * x.tile_rows;
-                const int32_t cols = std::min(x.tile_rows, x.rows - first) * G;
-                unit_sources.back().push_back({x.part_off + (int64_t)first * G * (D + 2) * x.nsplit * Hkv, cols, (r - x.row0 - first) * G, x.nsplit, x.is_wide || prefix_key_waves(cols) > 1});
+            if (path.back().tiles[(r - path.back().row0) / c.rows].part_off >= 0) {
+                plan->units.push_back({r, end - r, (int32_t)path.size(), 0});
+                unit_sources.emplace_back();
+                plan->source_stride = std::max(plan->source_stride, (int32_t)path.size());
+                plan->join_cols = std::max(plan->join_cols, (end - r) * G);
+                for (const Placed& x : path) {
+                    const int32_t tile = (r - x.row0) / x.tile_rows;
+                    const PlacedTile& t = x.tiles[tile];
+                    unit_sources.back().push_back({t.part_off, t.cols, (r - x.row0 - tile * x.tile_rows) * G, t.nsplit, x.is_wide || prefix_key_waves(t.cols) > 1});
+                }
             }
             r = end;
         }

@@ -132,7 +132,7 @@ static void check_plan(const ppd_shape& s, const std::vector<int32_t>& shared, c
         for (int r = 0; r < t.ncols / G; ++r) {
             const int i = seq[t.grow0 + r];
             keys[(size_t)(t.grow0 + r) * Hkv + t.kvh].push_back({t.begin, t.end});
-            const bool own = t.total == L[i] + n[i] && i == t.seq;
+            const bool own = t.total == L[i] + n[i] && i == t.seq && t.total > L[i];
             if (own) CHECK(t.L + r == L[i] + (t.grow0 + r - row0[i]));
             else CHECK(t.L >= t.total && t.end <= L[i] && t.end <= L[t.seq] && (i == t.seq || t.end <= common(i, t.seq)));
         }
@@ -152,8 +152,8 @@ static void check_plan(const ppd_shape& s, const std::vector<int32_t>& shared, c
             CHECK(r.first == to);
             to = r.second;
         }
-        const int i = seq[k / Hkv];
-        CHECK(to == L[i] + n[i]);
+        const int row = (int)(k / Hkv), i = seq[row];
+        CHECK(to > L[i] + row - row0[i] && to <= L[i] + n[i]);  // itself among them
     }
     // the join: of each row the same partials that its tiles write
     std::vector<int> joined(row0[B], 0);
