@@ -222,8 +222,13 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
         for (const Segment& g : x.segments) {
             const Cut c = cut_of(x, g);
             const int32_t max_keys = c.is_wide ? kMaxTreeBlockChunk : kMaxPrefixChunk;
-            const int64_t keys = g.end - g.begin - (g.own ? (rows_of(g) - c.rows) / 2 : 0);  // on average: a tile's last row sees none behind itself
-            (c.is_wide ? wide : narrow).push_back({keys, c.tiles, c.rows * G, max_keys, c.time, !g.own || g.begin > 0});
+            std::vector<Range>& list = c.is_wide ? wide : narrow;
+            if (!g.own || c.tiles == 1) {
+                list.push_back({g.end - g.begin, c.tiles, c.rows * G, max_keys, c.time, !g.own || g.begin > 0});
+            } else {  // a tile's last row sees no keys behind itself
+                for (int32_t r = 0; r < rows_of(g); r += c.rows)
+                    list.push_back({std::min(g.end, L[g.lo] + r + c.rows) - g.begin, 1, c.rows * G, max_keys, c.time, g.begin > 0});
+            }
             fewest += (double)c.tiles * Hkv * ((double)(g.end - g.begin) / max_keys + 1);
         }
         x.possible = fewest <= kMaxTiles;
