@@ -148,8 +148,9 @@ static int row_stride32(PyObject* o, PyObject* stride, const char* name, const c
     return 1;
 }
 // A tensor [rows][heads][dim] whose heads lie side by side: its row stride (as given, or the tensor's), and its heads.  It has to have `rows` rows at
-// least, and *heads heads of `dim` elements where these are known (not 0).  An address needs its stride given.
-static int head_rows(PyObject* o, PyObject* given, const char* name, int64_t rows, int64_t dim, int64_t* heads, int64_t* stride, PyObject** why) {
+// least, and *heads heads of `dim` elements where these are known (not 0).  *width, where asked for: elements of a row.  An address needs its
+// stride given.
+static int head_rows(PyObject* o, PyObject* given, const char* name, int64_t rows, int64_t dim, int64_t* heads, int64_t* stride, int64_t* width, PyObject** why) {
     if (o == Py_None || PyLong_Check(o)) {
         *stride = 0;
         if (given != Py_None) return to_int(given, stride);
@@ -186,18 +187,17 @@ static int head_rows(PyObject* o, PyObject* given, const char* name, int64_t row
     }
     *heads = shape[1];
     *stride = strides[0];
+    if (width) *width = shape[1] * shape[2];
     return 1;
 }
-// The same of a contiguous tensor, or an address
+// The same of rows without gaps, or an address
 static int dense_rows(PyObject* o, const char* name, int64_t rows, int64_t dim, int64_t* heads, PyObject** why) {
-    int64_t stride;
+    int64_t stride, width;
     if (o == Py_None || PyLong_Check(o)) return 1;
-    if (!head_rows(o, Py_None, name, rows, dim, heads, &stride, why)) return 0;
-    PyObject* v = PyObject_CallMethodNoArgs(o, s_is_contiguous);
-    const int dense = v ? PyObject_IsTrue(v) : -1;
-    Py_XDECREF(v);
-    if (dense == 0) *why = PyUnicode_FromFormat("%s has to be contiguous", name);
-    return dense > 0;
+    if (!head_rows(o, Py_None, name, rows, dim, heads, &stride, &width, why)) return 0;
+    if (rows <= 1 || stride == width) return 1;
+    *why = PyUnicode_FromFormat("%s has to be contiguous", name);
+    return 0;
 }
 // A contiguous int64 tensor of `rows` elements at least, or an address
 static int int64_vector(PyObject* o, const char* name, int64_t rows, PyObject** why) {
@@ -465,7 +465,7 @@ static PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     }
     const int transpose = PyObject_IsTrue(a[7]);
     if (transpose >= 0 && to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_count(a[6], a[5], "positions", &T, &why) && int64_vector(a[5], "positions", T, &why) &&
-        head_rows(a[2], a[3], "x", T, dim, &heads, &x_stride, &why) && head_rows(a[8], a[9], "out", T, dim, &heads, &out_stride, &why) &&
+        head_rows(a[2], a[3], "x", T, dim, &heads, &x_stride, NULL, &why) && head_rows(a[8], a[9], "out", T, dim, &heads, &out_stride, NULL, &why) &&
         to_address(a[2], &x) && to_address(a[5], &positions) && to_address(a[8], &out) && to_handle(a[10], &stream)) {
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
@@ -486,9 +486,9 @@ static PyObject* call_append_rotated(PyObject* self, PyObject* const* a, Py_ssiz
     const int64_t dim = shape_of(a[1], s_head_dim);
     int64_t hq = shape_of(a[1], s_num_q_heads), hkv = shape_of(a[1], s_num_kv_heads);
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_count(a[11], a[10], "slot_mapping", &T, &why) && int64_vector(a[10], "slot_mapping", T, &why) &&
-        int64_vector(a[8], "positions", T, &why) && head_rows(a[2], a[3], "q", T, dim, &hq, &q_stride, &why) &&
+        int64_vector(a[8], "positions", T, &why) && head_rows(a[2], a[3], "q", T, dim, &hq, &q_stride, NULL, &why) &&
         dense_rows(a[12], "q_out", T, dim, &hq, &why) &&
-        head_rows(a[4], a[5], "k", T, dim, &hkv, &k_stride, &why) && head_rows(a[6], a[7], "v", T, dim, &hkv, &v_stride, &why) &&
+        head_rows(a[4], a[5], "k", T, dim, &hkv, &k_stride, NULL, &why) && head_rows(a[6], a[7], "v", T, dim, &hkv, &v_stride, NULL, &why) &&
         to_address(a[2], &q) && to_address(a[4], &k) && to_address(a[6], &v) && to_address(a[8], &positions) && to_address(a[9], &pages) &&
         to_address(a[10], &slots) && to_address(a[12], &q_out) && to_handle(a[13], &stream)) {
         int32_t status;
