@@ -264,8 +264,8 @@ struct Lane {
 // Up to 32 columns, which all waves have: each takes every fourth slab of 32 keys from the pool straight into registers in the layouts of
 // the matrix instructions' operands: no LDS, no barrier, until the waves' results meet.  Probabilities enter the second product as bf16
 // numbers, as the matrix instruction takes them (their sum is of the 32-bit ones); everything else is held in 32 bits.
-// Start and end take 3.6-4.2 us (the wait for the slowest wave among them), four slabs 1.2 us alone and 2.8 where the chip is full of tiles:
-// memory.
+// 512 tiles of 72-679 keys beside others (64 decodes behind 8000 tokens): 4.5-17 us each, a line through them 5.7 us and 2.4 for every 128
+// keys; 18-192 keys on an empty chip 2.5 us and 0.4: memory.
 template <int HD, bool FP8>
 __device__ __forceinline__ void few_columns(const PrefixParams& P, const PrefixItem& it, const int* ids, float* stage, f32x2* stage_ml) {
     typedef Lane<HD, FP8> At;
@@ -350,11 +350,11 @@ __device__ __forceinline__ void few_columns(const PrefixParams& P, const PrefixI
 }
 
 // 33 to 128 columns: KEY_WAVES waves have the same 32, each with every KEY_WAVES-th slab of 32 keys.  A slab's K and V go from the pool
-// straight to a ring in LDS, a quarter by each wave, and are read from there by all (each wave for itself from L2: 64 decodes behind 8000
-// tokens 48 us, this way 39 with all else the same).
-// A slab of 128 columns takes 0.98 us with two workgroups to a unit (0.75 PFLOP/s; the row blocks' loop reaches 0.95), FP8 pages 1.09: LDS, matrix and
-// vector instructions take half of it each, one after the other in a wave, and two waves to a SIMD overlap them in part; 0.68 where the
-// loads are left out, 0.9 where the conversions of FP8 are.
+// straight to a ring in LDS, a quarter by each wave, and are read from there by all (64 decodes behind 8000 tokens
+// 44 us as first built, 49 with each wave reading for itself from L2; on two boxes).
+// A slab of 128 columns takes 1.02 us with two workgroups to a unit, 1.07 on FP8 pages; three documents of 18000 tokens with 256 columns each
+// 73 us for 57 GFLOP, 0.78 PFLOP/s, matrix pipes 30 % busy.  LDS, matrix and vector instructions follow each other in a wave, and two waves to a
+// SIMD overlap them in part.  Without the loads the same batch took 71 us a call instead of 93, without the conversions of FP8 84 instead of 90.
 template <int HD, bool FP8>
 struct Ring {
     static constexpr int SLAB = 4 * Lane<HD, FP8>::BLOCK;  // bytes: K of two pages, V of two pages
