@@ -34,10 +34,11 @@ ppd_status frequencies_impl(int32_t rotary_dim, double base, int32_t scaling, do
     if (scaling == PPD_ROPE_SCALE_BASE && rotary_dim < 4) return fail(nullptr, PPD_ERR_SHAPE, "a stretched base needs a rotary_dim of 4 or more");
     if (scaling == PPD_ROPE_SCALE_BY_PARTS && (!(original_length > 0) || !std::isfinite(original_length) || !(low_turns >= 0) || !(high_turns > low_turns) || !std::isfinite(high_turns)))
         return fail(nullptr, PPD_ERR_RANGE, "original_length must be finite and > 0, 0 <= low_turns < high_turns");
-    if (scaling == PPD_ROPE_SCALE_BASE) base *= std::pow(factor, rotary_dim / (rotary_dim - 2.0));
     double f[ppd::kMaxPairs];
     for (int i = 0; i < rotary_dim / 2; ++i) {
         f[i] = std::pow(base, -2.0 * i / rotary_dim);
+        // (base * factor^(rotary_dim / (rotary_dim - 2)) itself may be beyond the largest number)
+        if (scaling == PPD_ROPE_SCALE_BASE) f[i] *= std::pow(factor, -2.0 * i / (rotary_dim - 2));
         if (scaling == PPD_ROPE_SCALE_LINEAR) f[i] /= factor;
         if (scaling == PPD_ROPE_SCALE_BY_PARTS) {
             const double turns = original_length * f[i] / (double)kTwoPi;

@@ -123,3 +123,11 @@ def test_frequencies_and_settings():
         ppd.ppd_rope_frequencies(64, -1.0)
     assert e.value.status == -3 and "base" in str(e.value)
     assert status(ppd.ppd_set_rope, None, f) == -1
+
+
+def test_a_stretched_base_beyond_the_largest_number():
+    """base * factor^(d / (d - 2)) is 1e300 * 1e10^(8/6), more than a binary64 holds; the frequencies are not.  Each is a product of two powers:
+    some roundings, and exponents' roundings times |ln base| < 700: 1e-12 is far above 700 * 2^-52."""
+    f = ppd.ppd_rope_frequencies(8, 1e300, ppd.PPD_ROPE_SCALE_BASE, 1e10)
+    want = 10.0 ** np.array([-(300.0 * 2 * i / 8 + 10.0 * 2 * i / 6) for i in range(4)])
+    np.testing.assert_allclose(f, want, rtol=1e-12)
