@@ -110,29 +110,39 @@ public:
 
     // A shared range has to save more than it costs: the tiles of the runs that have fewer columns, and their reading the keys each for
     // itself (half a key's time), against a partial's columns more to be written and read (3.7 keys' time each, 1040 bytes) and a tile's start.
-    // Every level shares 64 keys at least, so runs that are not worth it are short, and with kMaxNested the levels are few.
-    void add(int32_t lo, int32_t hi, int32_t start, int level) {
-        if (lo == hi || level == kMaxNested) {
-            for (int32_t i = lo; i <= hi; ++i) list.push_back({i, i, start, L_[i] + n_[i], true});
-            return;
-        }
-        const int32_t least = *std::min_element(common_.begin() + lo + 1, common_.begin() + hi + 1);
-        double apart = -0.5;
-        for (int32_t from = lo; from <= hi;) {
-            const int32_t to = run_end(from, hi, least);
-            apart += key_cost(columns(from, to)) + 0.5;
-            from = to + 1;
-        }
-        const int64_t cols = columns(lo, hi);
-        if ((least - start) * (apart - key_cost(cols)) > 3.7 * cols + 200) {
-            list.push_back({lo, hi, start, least, false});
-            start = least;
-            ++level;
-        }
-        for (int32_t from = lo; from <= hi;) {
-            const int32_t to = run_end(from, hi, least);
-            add(from, to, start, level);
-            from = to + 1;
+    // Ranges that are shared nest at most kMaxNested deep.  Runs that are not worth it may fall apart as often as there are lengths in common,
+    // so what is left to do is kept in a list (the first run last) and not on the stack.
+    void add(int32_t first, int32_t last) {
+        struct Run { int32_t lo, hi, start, level; };
+        std::vector<Run> todo{{first, last, 0, 0}};
+        while (!todo.empty()) {
+            const int32_t lo = todo.back().lo, hi = todo.back().hi;
+            int32_t start = todo.back().start, level = todo.back().level;
+            todo.pop_back();
+            if (lo == hi || level == kMaxNested) {
+                for (int32_t i = lo; i <= hi; ++i) list.push_back({i, i, start, L_[i] + n_[i], true});
+                continue;
+            }
+            const int32_t least = *std::min_element(common_.begin() + lo + 1, common_.begin() + hi + 1);
+            double apart = -0.5;
+            for (int32_t from = lo; from <= hi;) {
+                const int32_t to = run_end(from, hi, least);
+                apart += key_cost(columns(from, to)) + 0.5;
+                from = to + 1;
+            }
+            const int64_t cols = columns(lo, hi);
+            if ((least - start) * (apart - key_cost(cols)) > 3.7 * cols + 200) {
+                list.push_back({lo, hi, start, least, false});
+                start = least;
+                ++level;
+            }
+            const size_t at = todo.size();
+            for (int32_t from = lo; from <= hi;) {
+                const int32_t to = run_end(from, hi, least);
+                todo.push_back({from, to, start, level});
+                from = to + 1;
+            }
+            std::reverse(todo.begin() + at, todo.end());
         }
     }
 
@@ -244,7 +254,7 @@ bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t*
         for (int32_t from = 0; from < B;) {  // what shares nothing stands alone
             int32_t to = from;
             while (to + 1 < B && common[to + 1] > 0) ++to;
-            segments.add(from, to, 0, 0);
+            segments.add(from, to);
             from = to + 1;
         }
         choice.segments.swap(segments.list);

@@ -2,6 +2,8 @@
 // stand-in runtime of host_runtime/, whose launches are recorded instead of run.
 #include <hip/hip_runtime.h>
 
+#include <pthread.h>
+
 #include <cmath>
 #include <cstdio>
 #include <limits>
@@ -241,6 +243,28 @@ static void plans() {
     }
 }
 
+// Every sequence shares 64 tokens more with its neighbour than the one before: as many lengths in common as sequences, few of them worth a
+// tile.  Planned by a thread with 256 KB of stack.
+static void* staircase_on(void* arg) {
+    const int B = *static_cast<int*>(arg);
+    std::vector<int32_t> shared(B), L(B), n(B, 1);
+    for (int i = 0; i < B; ++i) L[i] = 64 * (i + 1), shared[i] = 64 * i;
+    ppd::PrefixPlan plan;
+    CHECK(ppd::build_prefix_plan({32, 8, 128, 16, 1 << 20}, shared.data(), L.data(), n.data(), B, 2, 256, &plan));
+    CHECK(plan.keys_read < plan.keys_alone && plan.units.size() <= (size_t)B);
+    if (B <= 700) check_plan({32, 8, 128, 16, 1 << 20}, shared, L, n, plan);
+    return nullptr;
+}
+static void staircase() {
+    for (int B : {700, 8000}) {
+        pthread_attr_t attr;
+        pthread_t thread;
+        CHECK(pthread_attr_init(&attr) == 0 && pthread_attr_setstacksize(&attr, 256 << 10) == 0);
+        CHECK(pthread_create(&thread, &attr, staircase_on, &B) == 0 && pthread_join(thread, nullptr) == 0);
+        pthread_attr_destroy(&attr);
+    }
+}
+
 // Which calls plan anew, what a capture refuses, and that staging buffers are waited for.
 static void streams() {
     ppd_ctx* ctx = make(8, 2, 64);
@@ -278,6 +302,7 @@ int main(int argc, char** argv) {
     if (what == "refusals") refusals();
     else if (what == "plans") plans();
     else if (what == "streams") streams();
+    else if (what == "staircase") staircase();
     else return 2;
     std::printf("ok\n");
     return 0;

@@ -25,7 +25,7 @@ def exe(tmp_path_factory):
     return path
 
 
-@pytest.mark.parametrize("what", ["refusals", "plans", "streams"])
+@pytest.mark.parametrize("what", ["refusals", "plans", "streams", "staircase"])
 def test_host_side(exe, what):
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0")
     env.pop("LD_PRELOAD", None)
