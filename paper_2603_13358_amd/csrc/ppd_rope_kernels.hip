@@ -140,6 +140,8 @@ __device__ __forceinline__ void fill_table(const Rotation& rot, const int64_t* p
 
 }  // namespace
 
+constexpr int kMaxGridX = 1 << 22;  // workgroups: a dimension of a launch has to stay below 2^32 threads
+
 // A workgroup has TOK rows, whose cosines and sines its threads make together and leave in LDS; 16 elements of a head to a thread, the next
 // ones on their way while they are turned.  Bound by memory: 7931 rows of 32 heads, D = 128, from a packed projection 27 us, 4.8 TB/s read and
 // written (a copy 4.9), 16132 of 40 heads 69.5 us, 4.75 TB/s; by halves without whole granules (20 pairs) 30 us for the former, where reading
@@ -150,7 +152,8 @@ __global__ __launch_bounds__(kSmallThreads) void ppd_rope_kernel(const RopeParam
     constexpr int UNITS = D / 16;
     __shared__ f32x4 table[TOK * 4 * UNITS];
     __shared__ __attribute__((aligned(16))) uint16_t scratch[Scratch<D, LAYOUT>::ELEMS];
-    const int64_t t0 = (int64_t)blockIdx.x * TOK;
+    const int64_t t0 = ((int64_t)blockIdx.y * kMaxGridX + blockIdx.x) * TOK;
+    if (t0 >= P.T) return;
     const int unit = threadIdx.x % UNITS, rotary = P.rot.rotary_dim;
     const int rows = P.T - t0 < TOK ? (int)(P.T - t0) : TOK;
     int row = 0, head = threadIdx.x / UNITS;
@@ -297,7 +300,8 @@ int launch_rope(const RopeParams& p, int head_dim, void* stream) {
     // Four rows to a workgroup share its start and ask for the next while one is worked; few rows have workgroups to gain (64 rows of 32 heads
     // 3.8 us in the kernel with four, 2.6 with one).
     const bool wide = p.T >= 2048;
-    const dim3 grid((unsigned)(wide ? (p.T + 3) / 4 : p.T));
+    const int64_t groups = wide ? (p.T + 3) / 4 : p.T;
+    const dim3 grid((unsigned)(groups < kMaxGridX ? groups : kMaxGridX), (unsigned)((groups + kMaxGridX - 1) / kMaxGridX));
     by_layout(p.rot, [&](auto layout) {
         constexpr Layout LAYOUT = decltype(layout)::value;
         auto* const kernel = head_dim == 128 ? (wide ? &ppd_rope_kernel<128, 4, LAYOUT> : &ppd_rope_kernel<128, 1, LAYOUT>)

@@ -192,6 +192,24 @@ def test_rope_beyond_32_bit_offsets():
     near(x, *rotated(before, positions, inv_freq, 0), True)
 
 
+def test_rope_of_more_rows_than_one_dimension_of_a_launch_has_threads():
+    """2^26 rows and some, four to a workgroup of 256 threads: more than 2^32 threads.  Rows around each 2^24 (and the ends) are checked, those between
+    are zeros and stay so."""
+    T = 2 ** 26 + 5
+    ctx = ppd.Context(8, 2, 64, 4)
+    inv_freq = ppd.ppd_rope_frequencies(64)
+    ctx.set_rope(inv_freq)
+    rows = np.unique(np.concatenate([at + np.arange(-6, 6) for at in range(0, T + 8, 2 ** 24)] + [np.arange(T - 6, T)]))
+    rows = rows[(rows >= 0) & (rows < T)]
+    x = torch.zeros((T, 1, 64), dtype=torch.bfloat16, device="cuda")
+    before = bf16(np.random.default_rng(6).standard_normal((len(rows), 1, 64))).cuda()
+    x[dev(rows)] = before
+    ctx.rope(x, torch.arange(T, device="cuda"), x)
+    near(x[dev(rows)], *rotated(before, rows, inv_freq, 0), True)
+    x[dev(rows)] = 0
+    assert not any(part.any() for part in x.split(2 ** 22))
+
+
 # ---- the append ----
 
 def pool_bits(ctx, fp8):
