@@ -277,6 +277,18 @@ def test_streams_graphs_and_plans():
     assert torch.equal(last, eager) and b.flags() == 0
 
 
+def test_the_page_format_changes_between_calls_of_one_plan():
+    b, c = (Batch(*CASES["nested"][:6], seed=13, fp8=fp8) for fp8 in (False, True))
+    want = b.attend(), c.attend()
+    ctx = b.ctx
+    for fp8 in (True, False, True):  # one context, whose plan is that of the same lengths
+        ctx.set_kv_format(*((ppd.PPD_KV_FP8_E4M3, SCALE8, SCALE8) if fp8 else (ppd.PPD_KV_BF16, 1.0, 1.0)))
+        it = c if fp8 else b
+        out = torch.empty_like(want[fp8])
+        ctx.prefix_attention(it.q_dev, it.pool, it.table_dev, it.shared, it.L, it.n, it.scale, out)
+        within(out, *it.reference())
+
+
 def test_an_empty_batch_does_nothing():
     ctx = ppd.Context(8, 2, 64, 4)
     none, zero = torch.zeros((0, 8, 64), dtype=torch.bfloat16, device="cuda"), np.zeros(0, np.int32)
