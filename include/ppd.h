@@ -359,9 +359,9 @@ ppd_status ppd_kv_append_rotated(ppd_ctx *ctx, const void *q, int64_t q_stride, 
  *                 from the row of the first sequence that has it; sharing is used in steps of 64 tokens
  *   the rest      as for ppd_mixed_attention; L and n count all tokens of a sequence, shared ones too
  * The result is that of ppd_mixed_attention but for rounding, bitwise the same from run to run.  A row whose scores are all minus infinity
- * gives zeros; infinities and NaN of new tokens that a row does not see do not reach it.  As for the other attention calls a plan is
- * kept while shared, L and n do not change; one that changes under capture is refused, and a captured graph may be replayed until a
- * call of ppd_prefix_attention on the same context has planned another batch. */
+ * gives zeros, one that has NaN among its scores is NaN; infinities and NaN of new tokens that a row does not see do not reach it.  As for
+ * the other attention calls a plan is kept while shared, L and n do not change; one that changes under capture is refused, and a
+ * captured graph may be replayed until a call of ppd_prefix_attention on the same context has planned another batch. */
 ppd_status ppd_prefix_attention(ppd_ctx *ctx, const void *q, const void *kv_pages, const int32_t *page_tables,
                                 int32_t max_pages, const int32_t *shared, const int32_t *L, const int32_t *n, int32_t B,
                                 float scale, void *out, void *stream);

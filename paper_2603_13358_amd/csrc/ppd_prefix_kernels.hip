@@ -219,7 +219,10 @@ struct Lane {
                     for (int w = 0; w < KEY_WAVES; ++w) {
                         const int from = (block * KEY_WAVES + w) * kStageCols + cl;
                         const f32x2 ml = stage_ml[from];
-                        if (ml[0] == NEG_INF) continue;
+                        if (ml[0] == NEG_INF) {  // no key, or none but scores of minus infinity; the sum is 0, or NaN where one was NaN
+                            l += ml[1];
+                            continue;
+                        }
                         const float f = fast_exp2((ml[0] - mm) * c);
                         l += f * ml[1];
                         o += f * *reinterpret_cast<const f32x4*>(stage + from * ROW + d);
@@ -594,7 +597,7 @@ __global__ __launch_bounds__(256) void ppd_prefix_join_kernel(const PrefixParams
         m = top;
         for (int j = 0; j < count; ++j) {
             const f32x2 w = ml[j * cols + cl];
-            if (w[0] != NEG_INF) l += fast_exp2((w[0] - top) * c) * w[1];
+            l += w[0] != NEG_INF ? fast_exp2((w[0] - top) * c) * w[1] : w[1];  // 0, or NaN where a score was NaN
         }
         if (works) {
             for (int j0 = mine; j0 < count; j0 += AT_ONCE * share) {
