@@ -241,7 +241,8 @@ ppd_status ppd_mixed_attention_static(ppd_ctx *ctx, const void *q, const void *k
 /* Attention for a tree of drafted tokens over the cache.  Sequence i has L_i cached tokens and n_i drafted nodes, whose K/V have been
  * appended at positions L_i .. L_i + n_i - 1 (in any order in which the caller numbers them).  Row j sees the keys 0 .. L_i - 1 and
  * node k exactly if bit k of its mask is set; a row does not see itself unless its own bit is.  A row that sees nothing (L_i = 0
- * and no bit) gives zeros.  What a row does not see has no influence on it, infinities and NaN among the nodes included.
+ * and no bit) gives zeros, one that has NaN among its scores is NaN.  What a row does not see has no influence on it, infinities and NaN
+ * among the nodes included.
  *   q, out        device bf16 [T][Hq][D], T = sum n_i, rows grouped by sequence in batch order
  *   tree_mask     device uint64 [T][mask_words], 8-byte aligned; bit k % 64 of word k / 64 of a row is node k; bits from n_i on are
  *                 ignored; 1 <= mask_words <= 16 and n_i <= 64 * mask_words
@@ -254,7 +255,7 @@ ppd_status ppd_tree_attention(ppd_ctx *ctx, const void *q, const void *kv_pages,
  * every key of the sequence was looked at, for each KV head over the rows and the G query heads of its group:
  *   weights[i][h][t] = (t < L_i ? weights[i][h][t] : 0) + sum over rows j and heads of the group of the probability of key t
  * for t < L_i + n_i; entries behind are not touched, so appended tokens need no clearing.  A row whose scores are all minus infinity
- * gives zeros and adds nothing.
+ * gives zeros and adds nothing; one that has NaN among its scores is NaN, and so are the weights that it adds to.
  *   weights       device float [B][Hkv][weight_stride], 4-byte aligned, weight_stride >= L_i + n_i
  *   the rest      as for ppd_mixed_attention
  * Sums are binary32 in a fixed order: bitwise the same from run to run.  Sequences of few query columns (n_i * G * 8 bytes at most one

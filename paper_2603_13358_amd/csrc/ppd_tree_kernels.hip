@@ -339,7 +339,10 @@ __device__ __forceinline__ void join_columns(const TreeParams& P, int group, int
         for (int t = 0; t < AT_ONCE; ++t) {
             if (j0 + t >= g.nsplit) continue;
             const f32x2 w = pair(j0 + t);
-            if (w[0] == NEG_INF) continue;
+            if (w[0] == NEG_INF) {  // no key that the row sees, or none but scores of minus infinity; the sum is 0, or NaN where a score was NaN
+                l += w[1];
+                continue;
+            }
             const float f = fast_exp2((w[0] - mm) * c);
             l += f * w[1];
             o += f * v[t];
@@ -482,7 +485,10 @@ __device__ __forceinline__ void weigh_scores(const TreeParams& P, const WeighIte
             for (int j = part; j < g.nsplit; j += PARTS) {
                 const f32x2 w = *reinterpret_cast<const f32x2*>(pairs + g.part_stride * j);
                 const float top = fmaxf(m, w[0]);
-                if (w[0] == NEG_INF) continue;
+                if (w[0] == NEG_INF) {  // as in join_columns
+                    l += w[1];
+                    continue;
+                }
                 l = l * fast_exp2((m - top) * c) + w[1] * fast_exp2((w[0] - top) * c);
                 m = top;
             }
@@ -497,7 +503,7 @@ __device__ __forceinline__ void weigh_scores(const TreeParams& P, const WeighIte
 #pragma unroll
             for (int k = 0; k < PARTS; ++k) {
                 const f32x2 w = ml[k * kTreeCols + tid];
-                if (w[0] != NEG_INF) l += w[1] * fast_exp2((w[0] - m) * c);
+                l += w[0] != NEG_INF ? w[1] * fast_exp2((w[0] - m) * c) : w[1];
             }
         }
         __syncthreads();

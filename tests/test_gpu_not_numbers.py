@@ -6,6 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+import test_gpu_operators as operators  # noqa: E402
 import test_gpu_prefix as prefix  # noqa: E402
 
 
@@ -95,3 +96,50 @@ def test_prefix_rows_that_see_a_new_token_of_nan(rows):
     bad = np.zeros((len(dirty.q), 8), bool)
     bad[2 * rows + 1:3 * rows, :4] = True
     assert np.array_equal(nan_rows(dirty.attend()), bad)
+
+
+@pytest.mark.parametrize("L,n,hq,hkv,dim,fp8,words", operators.TREES, ids=lambda x: str(x).replace(" ", ""))
+@pytest.mark.parametrize("what", ["query", "key", "node"])
+def test_tree_rows_with_a_score_that_is_nan(L, n, hq, hkv, dim, fp8, words, what):
+    """A NaN query; NaN in the last cached key, which all rows of the sequence see; NaN in a node, which some see."""
+    i, G = len(L) - 1, hq // hkv
+    at = L[i] + n[i] // 2 if what == "node" else max(L[i] - 1, 0)
+
+    def fill(b):
+        if what != "query":
+            b.k[i][at, 0, 7] = np.nan
+    clean, dirty = (operators.Batch(L, n, hq, hkv, dim, fp8, seed=40, kv=kv) for kv in (None, fill))
+    mask = operators.random_mask(clean, words, seed=41)
+    bad = np.zeros((len(clean.q), hq), bool)
+    if what == "query":
+        bad[0, 0] = bad[-1, -1] = True
+        dirty.q_dev[dev_mask(bad)] = float("nan")
+    else:
+        bad[int(clean.n[:i].sum()):, :G] = clean.sees(i, mask)[:, at, None]
+    got = dirty.tree(mask)
+    assert np.array_equal(nan_rows(got), bad)
+    assert torch.equal(got[dev_mask(~bad)], clean.tree(mask)[dev_mask(~bad)])
+
+
+@pytest.mark.parametrize("L,n,hq,hkv,dim,fp8", operators.WEIGHTED, ids=lambda x: str(x).replace(" ", ""))
+@pytest.mark.parametrize("what", ["query", "key"])
+def test_weights_of_rows_with_a_score_that_is_nan(L, n, hq, hkv, dim, fp8, what):
+    """Keys that such a row sees have no weight that is a number; other KV heads and sequences keep theirs."""
+    i, G = len(L) - 1, hq // hkv
+    row = int(n[i]) - 1  # of the sequence: it sees all keys
+    at = L[i] + row
+
+    def fill(b):
+        if what == "key":
+            b.k[i][at, 0, 7] = np.nan
+    clean, dirty = (operators.Batch(L, n, hq, hkv, dim, fp8, seed=42, kv=kv) for kv in (None, fill))
+    bad = np.zeros((len(clean.q), hq), bool)
+    bad[-1, :G if what == "key" else 1] = True
+    if what == "query":
+        dirty.q_dev[dev_mask(bad)] = float("nan")
+    want, w = (torch.zeros((len(L), hkv, max(x + y for x, y in zip(L, n))), device="cuda") for _ in range(2))
+    clean_out, got = clean.weighted(want), dirty.weighted(w)
+    assert np.array_equal(nan_rows(got), bad)
+    assert torch.equal(got[dev_mask(~bad)], clean_out[dev_mask(~bad)])
+    assert torch.isnan(w[i, 0, :at + 1]).all()
+    assert torch.equal(w[:i], want[:i]) and torch.equal(w[i, 1:], want[i, 1:])
