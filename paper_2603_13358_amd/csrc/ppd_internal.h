@@ -81,6 +81,8 @@ constexpr int kCursorBase = 64;    // word index of cursor 0
 constexpr int kCursorStride = 32;  // words between cursors
 constexpr int kCounterWords = kCursorBase + kCursors * kCursorStride;
 constexpr int kMergeCols = 16;     // columns of a merge group one block of the merge kernel takes
+// Floats that a partial starts at a multiple of: it takes D + 2 for each of its columns, D is a multiple of 4, and the columns may be odd in number.
+constexpr int kPartialAlign = 2;
 
 // The rotation of queries and keys by their positions (ppd_set_rope).  Angles are counted in turns: pair i advances by turns[i] / 2^64
 // of one per position.

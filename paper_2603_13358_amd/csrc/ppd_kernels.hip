@@ -698,7 +698,7 @@ __device__ __forceinline__ void mfma_item(const KP& P, const ppd_work_item& it, 
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4) {
                     f32x4 w = {oacc[db][i4 * 4 + 0], oacc[db][i4 * 4 + 1], oacc[db][i4 * 4 + 2], oacc[db][i4 * 4 + 3]};
-                    *reinterpret_cast<f32x4*>(po + db * 32 + i4 * 8) = w;
+                    *reinterpret_cast<partial4*>(po + db * 32 + i4 * 8) = w;
                 }
             if (h == 0) {
                 float* ml = pp + (int64_t)ncols * HD + col * 2;
@@ -1001,7 +1001,7 @@ __device__ __forceinline__ void narrow_item(const KParams& P, const ppd_work_ite
                 float* pp = P.partials + it.part_off;
 #pragma unroll
                 for (int db = 0; db < DBN; ++db)
-                    *reinterpret_cast<f32x4*>(pp + (int64_t)c16 * HD + db * 16 + 4 * g4) = oacc[db];
+                    *reinterpret_cast<partial4*>(pp + (int64_t)c16 * HD + db * 16 + 4 * g4) = oacc[db];
                 if (g4 == 0) {
                     pp[(int64_t)ncols * HD + c16 * 2] = m_run;
                     pp[(int64_t)ncols * HD + c16 * 2 + 1] = l_run;
@@ -1244,7 +1244,7 @@ __device__ __forceinline__ void narrow_item_wide(const KParams& P, const ppd_wor
 #pragma unroll
                     for (int i4 = 0; i4 < 4; ++i4) {
                         const f32x4 w = {oacc[db][i4 * 4 + 0], oacc[db][i4 * 4 + 1], oacc[db][i4 * 4 + 2], oacc[db][i4 * 4 + 3]};
-                        *reinterpret_cast<f32x4*>(po + db * 32 + i4 * 8) = w;
+                        *reinterpret_cast<partial4*>(po + db * 32 + i4 * 8) = w;
                     }
                 if (h == 0) {
                     pp[(int64_t)ncols * HD + r * 2] = m_run;

@@ -229,7 +229,7 @@ struct Lane {
                     }
                     if (it.part_off >= 0) {
                         float* to = P.partials + it.part_off;
-                        *reinterpret_cast<f32x4*>(to + cc * HD + d) = o;
+                        *reinterpret_cast<partial4*>(to + cc * HD + d) = o;
                         if (d == 0) *reinterpret_cast<f32x2*>(to + it.ncols * HD + cc * 2) = f32x2{mm, l};
                     } else {
                         store_result(cc, d, o, l);
@@ -257,7 +257,7 @@ struct Lane {
             for (int i = 0; i < 4; ++i) {
                 const f32x4 o = {acc.o[db][4 * i], acc.o[db][4 * i + 1], acc.o[db][4 * i + 2], acc.o[db][4 * i + 3]};
                 const int d = db * 32 + i * 8 + h * 4;
-                if (it.part_off >= 0) *reinterpret_cast<f32x4*>(to + partial_at<HD>(it.ncols, cc, d)) = o;
+                if (it.part_off >= 0) *reinterpret_cast<partial4*>(to + partial_at<HD>(it.ncols, cc, d)) = o;
                 else store_result(cc, d, o, l_tot);
             }
         if (it.part_off >= 0 && h == 0) *reinterpret_cast<f32x2*>(to + it.ncols * HD + cc * 2) = f32x2{acc.m, l_tot};
@@ -584,7 +584,7 @@ __global__ __launch_bounds__(256) void ppd_prefix_join_kernel(const PrefixParams
                 if (j0 - mine + t * share >= count) break;  // for all threads alike; where it is for some, the first one's again
                 const int j = j0 + t * share < count ? j0 + t * share : 0;
                 const int cc = part_col0[j] + cl;
-                v[t] = *reinterpret_cast<const f32x4*>(P.partials + part_at[j] + (part_cols[j] < 0 ? cc * HD + d : partial_at<HD>(part_cols[j], cc, d)));
+                v[t] = *reinterpret_cast<const partial4*>(P.partials + part_at[j] + (part_cols[j] < 0 ? cc * HD + d : partial_at<HD>(part_cols[j], cc, d)));
             }
         };
         ask(mine);

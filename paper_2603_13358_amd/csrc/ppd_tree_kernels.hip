@@ -277,7 +277,7 @@ __device__ __forceinline__ void tree_tile(const TreeParams& P) {
             const int cc = c0 + cl;
             if (it.part_off >= 0) {
                 float* to = P.partials + it.part_off;
-                *reinterpret_cast<f32x4*>(to + cc * HD + d) = o;
+                *reinterpret_cast<partial4*>(to + cc * HD + d) = o;
                 if (d == 0) *reinterpret_cast<f32x2*>(to + it.ncols * HD + cc * 2) = f32x2{mm, l};
             } else {
                 const int row = cc / P.G;
@@ -314,7 +314,7 @@ __device__ __forceinline__ void join_columns(const TreeParams& P, int group, int
     const float* values = base + (int64_t)(col < g.ncols ? col : g.ncols - 1) * HD + d;
     auto ask = [&](int j0) {
 #pragma unroll
-        for (int t = 0; t < AT_ONCE; ++t) v[t] = *reinterpret_cast<const f32x4*>(values + g.part_stride * (j0 + t < g.nsplit ? j0 + t : j0));
+        for (int t = 0; t < AT_ONCE; ++t) v[t] = *reinterpret_cast<const partial4*>(values + g.part_stride * (j0 + t < g.nsplit ? j0 + t : j0));
     };
     auto staged_pair = [&](int i) {
         const int cc = c0 + i % COLS;
