@@ -362,7 +362,9 @@ ppd_status ppd_kv_append_rotated(ppd_ctx *ctx, const void *q, int64_t q_stride, 
  * The result is that of ppd_mixed_attention but for rounding, bitwise the same from run to run.  A row whose scores are all minus infinity
  * gives zeros, one that has NaN among its scores is NaN; infinities and NaN of new tokens that a row does not see do not reach it.  As for
  * the other attention calls a plan is kept while shared, L and n do not change; one that changes under capture is refused, and a
- * captured graph may be replayed until a call of ppd_prefix_attention on the same context has planned another batch. */
+ * captured graph may be replayed until a call of ppd_prefix_attention on the same context has planned another batch.
+ * Partial results take up to 1 GiB of workspace and a quarter on top, less where that cannot be allocated: a batch that needs more runs in
+ * parts, one after the other, and only a single sequence may take more. */
 ppd_status ppd_prefix_attention(ppd_ctx *ctx, const void *q, const void *kv_pages, const int32_t *page_tables,
                                 int32_t max_pages, const int32_t *shared, const int32_t *L, const int32_t *n, int32_t B,
                                 float scale, void *out, void *stream);

@@ -41,12 +41,20 @@ struct JoinUnit {
     int32_t nsources, unused;
 };
 
+// Neighbouring sequences that are planned together, and run before the next ones: where its lists begin in the plan's, and how long they are.
+struct PrefixPart {
+    int64_t item0, block0, unit0, source0;
+    int32_t n_items, n_blocks, n_units;
+    int32_t join_cols, source_stride;
+};
+
 struct PrefixPlan {
     std::vector<PrefixItem> items;
     std::vector<ppd_work_item> blocks;     // row blocks: columns beyond kPrefixCols
     std::vector<JoinUnit> units;
     std::vector<JoinSource> sources;
-    int64_t partial_floats = 0;
+    std::vector<PrefixPart> parts;         // of build_prefix_parts
+    int64_t partial_floats = 0;            // of the part that has most
     int32_t join_cols = 0;                 // most columns of a unit
     int32_t source_stride = 0;             // most sources of one
     int64_t keys_read = 0, keys_alone = 0; // keys per KV head that tiles are over, and without sharing
@@ -55,6 +63,13 @@ struct PrefixPlan {
 // Builds the tile list of a prefix attention call, whose arguments the caller has checked (shared[i] of sequence i > 0: tokens it has in
 // common with the one before, at most what either has cached); false if it has more than kMaxTiles tiles.
 bool build_prefix_plan(const ppd_shape& s, const int32_t* shared, const int32_t* L, const int32_t* n, int32_t B, int kv_elem_bytes, int num_cus, PrefixPlan* plan);
+
+// The same of a batch whose partials may not take more than `most_floats`: sequences that need more are halved until they do not, or there is one
+// left (which then takes what it takes).  The parts run one after the other in the same workspace.
+constexpr int64_t kMostPartialFloats = int64_t(1) << 28;
+constexpr int64_t kFewestPartialFloats = int64_t(1) << 22;  // as little as is tried where memory is short
+bool build_prefix_parts(const ppd_shape& s, const int32_t* shared, const int32_t* L, const int32_t* n, int32_t B, int kv_elem_bytes, int num_cus, int64_t most_floats,
+                        PrefixPlan* plan);
 
 struct PrefixParams {
     const uint16_t* q;

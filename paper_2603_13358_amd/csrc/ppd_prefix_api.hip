@@ -76,13 +76,22 @@ void put(char* to, const std::vector<T>& v) {
 // Builds the plan, grows the workspace and enqueues the upload.
 ppd_status upload_prefix_plan(ppd_ctx* ctx, PrefixState* t, const int32_t* shared, const int32_t* L, const int32_t* n, int32_t B, hipStream_t hs) {
     t->on_device = false;
-    if (!ppd::build_prefix_plan(ctx->shape, shared, L, n, B, ctx->fp8_pages ? 1 : 2, ctx->num_cus, &t->plan)) return fail(ctx, PPD_ERR_RANGE, "the batch has more tiles than one launch takes");
+    ppd_status st = PPD_OK;
+    const std::string error = ctx->error;
+    for (int64_t most = ppd::kMostPartialFloats;; most /= 4) {
+        if (!ppd::build_prefix_parts(ctx->shape, shared, L, n, B, ctx->fp8_pages ? 1 : 2, ctx->num_cus, most, &t->plan))
+            return fail(ctx, PPD_ERR_RANGE, "the batch has more tiles than one launch takes");
+        st = grow_device(ctx, &t->d_partials, &t->d_partials_bytes, (size_t)t->plan.partial_floats * sizeof(float), hs);
+        // Where memory is short the batch is cut into more parts.
+        if (st != PPD_ERR_WORKSPACE || most <= ppd::kFewestPartialFloats) break;
+    }
+    if (st != PPD_OK) return st;
+    ctx->error = error;  // that of the last call that failed
     const ppd::PrefixPlan& plan = t->plan;
     const PlanLayout at(plan);
     Staging* sg = nullptr;
-    ppd_status st = next_staging(ctx, t->staging, &t->next_slot, at.total, &sg);
+    st = next_staging(ctx, t->staging, &t->next_slot, at.total, &sg);
     if (st == PPD_OK) st = grow_device(ctx, &t->d_plan, &t->d_plan_bytes, at.total, hs);
-    if (st == PPD_OK) st = grow_device(ctx, &t->d_partials, &t->d_partials_bytes, (size_t)plan.partial_floats * sizeof(float), hs);
     if (st != PPD_OK) return st;
     char* host = static_cast<char*>(sg->host);
     std::memset(host, 0, at.total);
@@ -153,9 +162,6 @@ ppd_status prefix_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pag
     p.out = static_cast<uint16_t*>(out);
     p.pool = kv_pages;
     p.page_tables = page_tables;
-    p.items = reinterpret_cast<const ppd::PrefixItem*>(d_plan);
-    p.units = reinterpret_cast<const ppd::JoinUnit*>(d_plan + at.units);
-    p.sources = reinterpret_cast<const ppd::JoinSource*>(d_plan + at.sources);
     p.partials = static_cast<float*>(t->d_partials);
     p.err_flags = ctx->d_counters + 9;
     p.num_pages = ctx->shape.num_pages;
@@ -165,49 +171,53 @@ ppd_status prefix_attention_impl(ppd_ctx* ctx, const void* q, const void* kv_pag
     p.Hkv = ctx->shape.num_kv_heads;
     p.G = p.Hq / p.Hkv;
     p.invG = 65536 / p.G + 1;
-    p.n_items = (int32_t)plan.items.size();
-    p.n_units = (int32_t)plan.units.size();
-    p.join_cols = plan.join_cols;
-    p.source_stride = plan.source_stride;
     // Strictly positive, so that a scale of 0 gives 2^(-inf * c) = 0 for keys that are not seen.
     p.scale_log2e = std::max(1e-30f, (float)((double)scale * (double)ctx->k_scale * 1.4426950408889634));
     p.v_scale = ctx->v_scale;
     const int D = ctx->shape.head_dim;
-    int rc = 0;
-    if (!plan.blocks.empty()) {
-        ppd::TreeBlockParams b;
-        std::memset(&b, 0, sizeof b);
-        b.q = p.q;
-        b.out = p.out;
-        b.pool = static_cast<const uint16_t*>(kv_pages);
-        b.page_tables = page_tables;
-        b.items = reinterpret_cast<const ppd_work_item*>(d_plan + at.blocks);
-        b.partials = p.partials;
-        b.counters = ctx->d_counters;
-        b.num_pages = p.num_pages;
-        b.page_stride = p.page_stride;
-        b.n_items = (int32_t)plan.blocks.size();
-        b.max_pages = max_pages;
-        b.Hq = p.Hq;
-        b.Hkv = p.Hkv;
-        b.G = p.G;
-        b.invG = p.invG;
-        b.scale_log2e = p.scale_log2e;
-        b.v_scale = p.v_scale;
-        rc = ppd::launch_tree_blocks(b, D, ctx->fp8_pages, stream);
-        if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch prefix row blocks");
-    }
-    if (p.n_items > 0) {
-        rc = ppd::launch_prefix(p, D, ctx->fp8_pages, stream);
-        if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch prefix attention");
-    }
-    if (p.n_units > 0) {
-        rc = ppd::launch_prefix_join(p, D, stream);
-        if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch join of prefix tiles");
+    for (const ppd::PrefixPart& part : plan.parts) {
+        p.items = reinterpret_cast<const ppd::PrefixItem*>(d_plan) + part.item0;
+        p.units = reinterpret_cast<const ppd::JoinUnit*>(d_plan + at.units) + part.unit0;
+        p.sources = reinterpret_cast<const ppd::JoinSource*>(d_plan + at.sources) + part.source0;
+        p.n_items = part.n_items;
+        p.n_units = part.n_units;
+        p.join_cols = part.join_cols;
+        p.source_stride = part.source_stride;
+        if (part.n_blocks > 0) {
+            ppd::TreeBlockParams b;
+            std::memset(&b, 0, sizeof b);
+            b.q = p.q;
+            b.out = p.out;
+            b.pool = static_cast<const uint16_t*>(kv_pages);
+            b.page_tables = page_tables;
+            b.items = reinterpret_cast<const ppd_work_item*>(d_plan + at.blocks) + part.block0;
+            b.partials = p.partials;
+            b.counters = ctx->d_counters;
+            b.num_pages = p.num_pages;
+            b.page_stride = p.page_stride;
+            b.n_items = part.n_blocks;
+            b.max_pages = max_pages;
+            b.Hq = p.Hq;
+            b.Hkv = p.Hkv;
+            b.G = p.G;
+            b.invG = p.invG;
+            b.scale_log2e = p.scale_log2e;
+            b.v_scale = p.v_scale;
+            const int rc = ppd::launch_tree_blocks(b, D, ctx->fp8_pages, stream);
+            if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch prefix row blocks");
+        }
+        if (p.n_items > 0) {
+            const int rc = ppd::launch_prefix(p, D, ctx->fp8_pages, stream);
+            if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch prefix attention");
+        }
+        if (p.n_units > 0) {
+            const int rc = ppd::launch_prefix_join(p, D, stream);
+            if (rc != 0) return hip_fail(ctx, (hipError_t)rc, "launch join of prefix tiles");
+        }
     }
     if (ctx->log_calls)
-        std::fprintf(stderr, "ppd: prefix_attention%s B=%d tiles=%d row blocks=%d joined units=%d keys=%lld of %lld plan=%s\n", ctx->fp8_pages ? " (FP8 pages)" : "", (int)B,
-                     (int)p.n_items, (int)plan.blocks.size(), (int)p.n_units, (long long)plan.keys_read, (long long)plan.keys_alone, reuse ? "reused" : "built");
+        std::fprintf(stderr, "ppd: prefix_attention%s B=%d parts=%d tiles=%d row blocks=%d joined units=%d keys=%lld of %lld plan=%s\n", ctx->fp8_pages ? " (FP8 pages)" : "",
+                     (int)B, (int)plan.parts.size(), (int)plan.items.size(), (int)plan.blocks.size(), (int)plan.units.size(), (long long)plan.keys_read, (long long)plan.keys_alone, reuse ? "reused" : "built");
     return PPD_OK;
 }
 
