@@ -277,6 +277,7 @@ def ppd_kv_compact(ctx, kv_pages, page_tables, keep, first, count, layer_stride_
         _check_call(status, ctx)
 
 
+# The calls of positions and shared prefixes take tensors of the GPU, or of pinned memory, and refuse others of the host.
 PPD_ROPE_HALF, PPD_ROPE_INTERLEAVED = 0, 1
 PPD_ROPE_SCALE_NONE, PPD_ROPE_SCALE_LINEAR, PPD_ROPE_SCALE_BASE, PPD_ROPE_SCALE_BY_PARTS = 0, 1, 2, 3
 

@@ -7,7 +7,7 @@
 #include <Python.h>
 #include <stdint.h>
 
-static PyObject *s_data_ptr, *s_value, *s_shape, *s_stride, *s_dtype, *s_torch, *s_is_contiguous, *s_num_q_heads, *s_num_kv_heads, *s_head_dim;
+static PyObject *s_data_ptr, *s_value, *s_shape, *s_stride, *s_dtype, *s_torch, *s_is_contiguous, *s_is_cuda, *s_is_pinned, *s_num_q_heads, *s_num_kv_heads, *s_head_dim;
 static PyObject *t_void_p, *f_cast;  // ctypes.c_void_p and ctypes.cast
 
 // What a ctypes parameter of type c_void_p takes: None, an int and a c_void_p (a context's handle) here, anything else --
@@ -199,11 +199,12 @@ static int dense_rows(PyObject* o, const char* name, int64_t rows, int64_t dim, 
     *why = PyUnicode_FromFormat("%s has to be contiguous", name);
     return 0;
 }
-// A contiguous int64 tensor of `rows` elements at least, or an address
-static int int64_vector(PyObject* o, const char* name, int64_t rows, PyObject** why) {
-    int64_t have;
+// A contiguous int64 tensor of `rows` elements at least (`counted`: these are as many as it says itself), or an address
+static int int64_vector(PyObject* o, const char* name, int64_t rows, int counted, PyObject** why) {
+    int64_t have = rows;
     if (o == Py_None || PyLong_Check(o)) return 1;
-    if (!has_elements(o, name, &t_int64, why) || !to_int_or_shape(Py_None, o, 0, &have)) return 0;
+    if (!has_elements(o, name, &t_int64, why) || (!counted && !to_int_or_shape(Py_None, o, 0, &have))) return 0;
+    if (have >= rows && rows <= 1) return 1;
     PyObject* v = PyObject_CallMethodNoArgs(o, s_is_contiguous);
     const int dense = v ? PyObject_IsTrue(v) : -1;
     Py_XDECREF(v);
@@ -219,6 +220,24 @@ static int row_count(PyObject* o, PyObject* x, const char* name, int64_t* out, P
         return 0;
     }
     return to_int_or_shape(o, x, 0, out);
+}
+// Whether the GPU reaches a tensor's memory: kernels that were given other host memory's addresses would fault.  An address or None is taken on
+// trust; so is everything where there is no context, which the library refuses.
+static int on_gpu(void* ctx, PyObject* o, const char* name, PyObject** why) {
+    if (!ctx || o == Py_None || PyLong_Check(o)) return 1;
+    PyObject* v = PyObject_GetAttr(o, s_is_cuda);
+    if (!v) {
+        PyErr_Clear();  // not one of torch's tensors
+        return 1;
+    }
+    int ok = v == Py_True;
+    Py_DECREF(v);
+    if (ok) return 1;
+    v = PyObject_CallMethodNoArgs(o, s_is_pinned);
+    ok = v ? PyObject_IsTrue(v) : -1;
+    Py_XDECREF(v);
+    if (ok == 0) *why = PyUnicode_FromFormat("%s has to be on the GPU", name);
+    return ok > 0;
 }
 static int expect(Py_ssize_t have, Py_ssize_t want) {
     if (have == want) return 1;
@@ -464,8 +483,9 @@ static PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         heads = heads32;
     }
     const int transpose = PyObject_IsTrue(a[7]);
-    if (transpose >= 0 && to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_count(a[6], a[5], "positions", &T, &why) && int64_vector(a[5], "positions", T, &why) &&
+    if (transpose >= 0 && to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_count(a[6], a[5], "positions", &T, &why) && int64_vector(a[5], "positions", T, a[6] == Py_None, &why) &&
         head_rows(a[2], a[3], "x", T, dim, &heads, &x_stride, NULL, &why) && head_rows(a[8], a[9], "out", T, dim, &heads, &out_stride, NULL, &why) &&
+        on_gpu(ctx, a[2], "x", &why) && on_gpu(ctx, a[5], "positions", &why) && on_gpu(ctx, a[8], "out", &why) &&
         to_address(a[2], &x) && to_address(a[5], &positions) && to_address(a[8], &out) && to_handle(a[10], &stream)) {
         int32_t status;
         Py_BEGIN_ALLOW_THREADS
@@ -485,10 +505,12 @@ static PyObject* call_append_rotated(PyObject* self, PyObject* const* a, Py_ssiz
     if (!expect(n, 14)) return NULL;
     const int64_t dim = shape_of(a[1], s_head_dim);
     int64_t hq = shape_of(a[1], s_num_q_heads), hkv = shape_of(a[1], s_num_kv_heads);
-    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_count(a[11], a[10], "slot_mapping", &T, &why) && int64_vector(a[10], "slot_mapping", T, &why) &&
-        int64_vector(a[8], "positions", T, &why) && head_rows(a[2], a[3], "q", T, dim, &hq, &q_stride, NULL, &why) &&
+    if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_count(a[11], a[10], "slot_mapping", &T, &why) && int64_vector(a[10], "slot_mapping", T, a[11] == Py_None, &why) &&
+        int64_vector(a[8], "positions", T, 0, &why) && head_rows(a[2], a[3], "q", T, dim, &hq, &q_stride, NULL, &why) &&
         dense_rows(a[12], "q_out", T, dim, &hq, &why) &&
         head_rows(a[4], a[5], "k", T, dim, &hkv, &k_stride, NULL, &why) && head_rows(a[6], a[7], "v", T, dim, &hkv, &v_stride, NULL, &why) &&
+        on_gpu(ctx, a[2], "q", &why) && on_gpu(ctx, a[4], "k", &why) && on_gpu(ctx, a[6], "v", &why) && on_gpu(ctx, a[8], "positions", &why) &&
+        on_gpu(ctx, a[10], "slot_mapping", &why) && on_gpu(ctx, a[12], "q_out", &why) &&
         to_address(a[2], &q) && to_address(a[4], &k) && to_address(a[6], &v) && to_address(a[8], &positions) && to_address(a[9], &pages) &&
         to_address(a[10], &slots) && to_address(a[12], &q_out) && to_handle(a[13], &stream)) {
         int32_t status;
@@ -526,6 +548,7 @@ static PyObject* call_prefix(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     for (Py_ssize_t i = 0; i < nn.shape[0]; ++i) rows += ((const int32_t*)nn.buf)[i];
     if (to_handle(a[0], &fn) && to_handle(a[1], &ctx) && row_stride32(a[4], a[5], "page_tables", "max_pages", L.shape[0], &max_pages, &why) &&
         has_elements(a[4], "page_tables", &t_int32, &why) && dense_rows(a[2], "q", rows, dim, &hq, &why) && dense_rows(a[10], "out", rows, dim, &hq, &why) &&
+        on_gpu(ctx, a[2], "q", &why) && on_gpu(ctx, a[4], "page_tables", &why) && on_gpu(ctx, a[10], "out", &why) &&
         to_address(a[2], &q) && to_address(a[3], &pages) && to_address(a[4], &tables) && (scale = PyNumber_Float(a[9])) && to_address(a[10], &out) &&
         to_handle(a[11], &stream)) {
         const float s = (float)PyFloat_AS_DOUBLE(scale);
@@ -565,6 +588,8 @@ PyMODINIT_FUNC PyInit_ppd_call(void) {
     s_dtype = PyUnicode_InternFromString("dtype");
     s_torch = PyUnicode_InternFromString("torch");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    s_is_cuda = PyUnicode_InternFromString("is_cuda");
+    s_is_pinned = PyUnicode_InternFromString("is_pinned");
     s_num_kv_heads = PyUnicode_InternFromString("num_kv_heads");
     s_num_q_heads = PyUnicode_InternFromString("num_q_heads");
     s_head_dim = PyUnicode_InternFromString("head_dim");
@@ -574,6 +599,6 @@ PyMODINIT_FUNC PyInit_ppd_call(void) {
     t_void_p = PyObject_GetAttrString(ctypes, "c_void_p");
     f_cast = PyObject_GetAttrString(ctypes, "cast");
     Py_DECREF(ctypes);
-    if (!s_data_ptr || !s_value || !s_shape || !s_dtype || !s_torch || !s_is_contiguous || !s_num_kv_heads || !s_num_q_heads || !s_head_dim || !s_stride || !t_void_p || !f_cast) return NULL;
+    if (!s_data_ptr || !s_value || !s_shape || !s_dtype || !s_torch || !s_is_contiguous || !s_is_cuda || !s_is_pinned || !s_num_kv_heads || !s_num_q_heads || !s_head_dim || !s_stride || !t_void_p || !f_cast) return NULL;
     return PyModule_Create(&kModule);
 }
