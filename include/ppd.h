@@ -21,7 +21,8 @@
  *    softmax, probabilities rounded to bf16 before the PV product (two forms of decode-only launches enter each
  *    as two bf16 numbers, with less error: option "narrow_kernel" below), bf16 output (round to nearest even).
  *  - A visible V element that is infinite makes its output column infinite, and NaN where infinities of both signs
- *    meet or the element's probability is zero; NaN stays NaN.
+ *    meet or the element's probability is zero (of a new token, in tree, weighted and prefix attention: infinite or
+ *    NaN); NaN stays NaN.
  *  - Both calls are asynchronous on `stream` (a hipStream_t passed as void*; NULL = the default stream);
  *    the caller synchronises.  Host-side argument checks are complete before anything is enqueued: a
  *    negative return value means no device side effect.
@@ -328,8 +329,8 @@ ppd_status ppd_set_rope(ppd_ctx *ctx, const double *inv_freq, int32_t rotary_dim
 ppd_status ppd_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double original_length,
                                 double low_turns, double high_turns, double *inv_freq);
 
-/* Rotates the heads of T rows by their positions.  transpose != 0: by the transposed matrices, which are the gradient (and, over
- * amplitude^2, the inverse).
+/* Rotates the heads of T rows by their positions.  transpose != 0: by the transposed matrices, which are the gradient (and, the rotated
+ * elements over amplitude^2, the inverse).
  *   x, out        device bf16 [T][heads][head_dim], rows x_stride and out_stride elements apart (multiples of 8, at least
  *                 heads * head_dim; ignored for T = 1), 16-byte aligned.  out may be x with the same stride; any other overlap of the
  *                 rows' ranges is refused.  What lies between out's rows is not touched

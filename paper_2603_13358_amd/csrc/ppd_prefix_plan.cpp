@@ -20,7 +20,8 @@ int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
 
 // What a tile takes, ns: its start and end, and a key while memory keeps up.  Measured over whole launches at D = 128 (start and end 3.6-4.2
 // us and 1.2 us for four slabs of few columns, 5-6 us and 0.98 us a slab of 128 columns on bf16 pages, 1.09 on FP8; row blocks 6.6 us and 1.2 us
-// for 64 keys); D = 64 by its share of the work.
+// for 64 keys, of launches that leave units idle: where every unit has one they are slower, and the 680 blocks of 18 next turns, which add up to
+// 104 us over 256 units at this price, take 164-171); D = 64 by its share of the work.
 struct TileTime { double start, key; };
 TileTime tile_time(int ncols, int head_dim, int kv_elem_bytes) {
     const int waves = prefix_key_waves(ncols);

@@ -3,9 +3,10 @@
 //   (a, b) -> A (a cos t - b sin t, b cos t + a sin t),   t = position * frequency of the pair
 //
 // The angle is an integer: a frequency is a fraction of a turn in units of 2^-64, so position * frequency modulo 2^64 is the angle
-// without its whole turns, off by position * 2^-65 turns at most, for every 64-bit position.  Its upper 32 bits become a binary32
-// fraction of a turn in [-1/2, 1/2), which is what the sine and cosine instructions take: of all 2^32 such fractions none is off by more than
-// 2^-22.9 (against 64 bits).
+// without its whole turns, for every 64-bit position.  It is off by position * 2^-64 turns at most where a frequency is at most one radian: 2^-65
+// is the rounding to units, and 0.7 * 2^-65 what the division by 2 pi in 64-bit significands leaves (2^-63 of the turns).  Its upper 32
+// bits become a binary32 fraction of a turn in [-1/2, 1/2), which is what the sine and cosine instructions take: of all 2^32 such fractions
+// none is off by more than 2^-22.9 (against 64 bits).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -297,8 +298,10 @@ void append_launch(const RotatedAppendParams& p, hipStream_t hs) {
 
 int launch_rope(const RopeParams& p, int head_dim, void* stream) {
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    // Four rows to a workgroup share its start and ask for the next while one is worked; few rows have workgroups to gain (64 rows of 32 heads
-    // 3.8 us in the kernel with four, 2.6 with one).
+    // Four rows to a workgroup share its start and ask for the next while one is worked; few rows have workgroups to gain.  us with four and with
+    // one, D = 128, 20 calls in a replayed graph: 256 rows of 32 heads 3.9 and 2.7, 1024 4.8 and 4.0, 2047 7.0 and 6.4, 3000 9.9 and 9.7, 8192 23.9
+    // and 23.4; of 8 heads 1024 rows 2.9 and 3.0, 2047 3.3 and 3.4, 8192 6.9 and 8.4; of 2 heads 1024 3.1 and 3.3, 2047 3.3 and 3.8, 8192 4.5 and
+    // 8.5.
     const bool wide = p.T >= 2048;
     const int64_t groups = wide ? (p.T + 3) / 4 : p.T;
     const dim3 grid((unsigned)(groups < kMaxGridX ? groups : kMaxGridX), (unsigned)((groups + kMaxGridX - 1) / kMaxGridX));
