@@ -71,6 +71,16 @@ static int to_int32(PyObject* o, const char* name, int32_t* out, PyObject** why)
     *out = (int32_t)wide;
     return 1;
 }
+// The same of 64 bits.
+static int to_int64(PyObject* o, const char* name, int64_t* out, PyObject** why) {
+    PyObject* v = PyNumber_Long(o);
+    if (!v) return 0;
+    int over;
+    *out = PyLong_AsLongLongAndOverflow(v, &over);
+    Py_DECREF(v);
+    if (over) *why = PyUnicode_FromFormat("%s does not fit 64 bits", name);
+    return !over && !PyErr_Occurred();
+}
 // Whether a tensor's elements are of one of two of torch's types (an address or None is taken on trust): 0 with *why set if not.  `types` holds the
 // type objects once torch has been found.
 typedef struct { const char* names[2]; PyObject* types[2]; } elem_types;
@@ -153,7 +163,7 @@ static int row_stride32(PyObject* o, PyObject* stride, const char* name, const c
 static int head_rows(PyObject* o, PyObject* given, const char* name, int64_t rows, int64_t dim, int64_t* heads, int64_t* stride, int64_t* width, PyObject** why) {
     if (o == Py_None || PyLong_Check(o)) {
         *stride = 0;
-        if (given != Py_None) return to_int(given, stride);
+        if (given != Py_None) return to_int64(given, "a stride", stride, why);
         if (o == Py_None || rows <= 1) return 1;
         *why = PyUnicode_FromFormat("%s is an address: its stride has to be given", name);
         return 0;
@@ -219,7 +229,7 @@ static int row_count(PyObject* o, PyObject* x, const char* name, int64_t* out, P
         *why = PyUnicode_FromFormat("%s is an address: T has to be given", name);
         return 0;
     }
-    return to_int_or_shape(o, x, 0, out);
+    return o != Py_None ? to_int64(o, "T", out, why) : to_int_or_shape(o, x, 0, out);
 }
 // Whether the GPU reaches a tensor's memory: kernels that were given other host memory's addresses would fault.  An address or None is taken on
 // trust; so is everything where there is no context, which the library refuses.

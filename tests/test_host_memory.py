@@ -1,5 +1,5 @@
-"""Tensors in memory that the GPU does not reach: the calls of positions and shared prefixes refuse them in Python (the entry point is a stand-in
-that counts what is passed on, the context an address that nothing reads)."""
+"""What the calls of positions and shared prefixes refuse in Python: tensors in memory that the GPU does not reach (the entry point is a stand-in that
+counts what is passed on, the context an address that nothing reads), and integers of more than 64 bits."""
 import ctypes
 
 import numpy as np
@@ -97,3 +97,18 @@ def test_tensors_of_the_host_are_refused(kind, passed_on):
     addresses = dict(good, **{name: 1 << 21 for name in good if name in ("out", "q_out", "page_tables")})
     if kind == "append":
         assert call(kind, h, addresses).status == PASSED_ON
+
+
+@pytest.mark.parametrize("far", [1 << 63, (1 << 64) + 5, -(1 << 63) - 1])
+def test_integers_are_not_cut_to_64_bits(far):
+    """Counts and strides; the context is NULL, which the library itself would refuse with PPD_ERR_NULL."""
+    def refused(what, f, *args, **kw):
+        with pytest.raises(ppd.PPDError) as e:
+            f(None, *args, **kw)
+        return e.value.status == -3 and what in str(e.value)
+    address = 1 << 20
+    assert refused("T", ppd.ppd_rope, rows(5, 8), index(5), rows(5, 8), T=far)
+    assert refused("T", ppd.ppd_kv_append_rotated, None, rows(5, 2), rows(5, 2), index(5), address, index(5), None, T=far)
+    assert refused("stride", ppd.ppd_rope, address, index(5), address, heads=8, x_stride=far, out_stride=512)
+    assert refused("stride", ppd.ppd_rope, address, index(5), address, heads=8, x_stride=512, out_stride=far)
+    assert refused("stride", ppd.ppd_kv_append_rotated, None, address, address, index(5), address, index(5), None, k_stride=128, v_stride=far)
